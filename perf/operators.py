@@ -284,7 +284,7 @@ def _run_own(s):
             return s["y"], s["n"], s["rstd1"], s["rstd2"], s["back1"], s["back2"]
         return (s["y"], s["n"], s["rstd1"], s["rstd2"], *_seen(*s["kept1"], "f8")[:1], s["kept1"][1].view(torch.float8_e8m0fnu),
                 *_seen(*s["kept2"], "f8")[:1], s["kept2"][1].view(torch.float8_e8m0fnu))
-    grads = apm.make_norm_join_grads(dn=s["dn"], dy=s["dy"], dx=s["dx"], dbranch=s["dbranch"], dgate=s["dgate"], dpre_weight=s["dw1"],
+    grads = apm.make_norm_join_grads(join, dn=s["dn"], dy=s["dy"], dx=s["dx"], dbranch=s["dbranch"], dgate=s["dgate"], dpre_weight=s["dw1"],
                                      dpre_bias=s["db1"], dpost_weight=s["dw2"], dpost_bias=s["db2"])
     room = torch.empty(apm.apm_norm_join_workspace_bytes(s["rows"], s["cols"]), dtype=torch.uint8, device=DEV)
     apm.apm_norm_join_backward(join, grads, room)
