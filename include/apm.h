@@ -652,6 +652,158 @@ int64_t apm_delayed_applied(const apm_pool* pool);
  * update kernels of later apm_step_delayed calls write, indexed like their page list. */
 int apm_delayed_set_outputs(apm_pool* pool, float* grad_norm, uint8_t* skip_mask);
 
+/* ---- activations: kept in 8 bits between the forward and the backward pass, and used from there --------
+ *
+ * What else a training step holds in HBM beside the model states.  These calls need no pool.  They work on row-major
+ * matrices of `rows` tokens and `cols` channels on the calling thread's current HIP device, whose memory every pointer
+ * must be of; they keep nothing and allocate nothing, so that all of them may be captured into a HIP graph.  Matrices
+ * that a call writes must not overlap what else it reads or writes, except where that is said to be allowed.
+ * Errors: APM_EINVAL (missing or contradictory arguments, a type or size that is not supported, a misaligned pointer,
+ * a stride below the width), APM_ENOMEM (workspace too small), APM_EDEVICE. */
+
+/* rows x cols elements of `dtype`; a row starts `stride` elements after the one before, its elements are contiguous.
+ * `data` is aligned to its elements at least (16 bytes, and rows of a multiple of 16 bytes, are fastest).  The rows of
+ * a matrix that is only read may overlap (stride 0: one row for all tokens).  data == NULL: not given. */
+typedef struct {
+    void* data;
+    int64_t stride;
+    int32_t dtype; /* apm_dtype */
+    int32_t reserved;
+} apm_matrix;
+
+/* cols contiguous elements; data == NULL: not given. */
+typedef struct {
+    void* data;
+    int32_t dtype; /* apm_dtype */
+    int32_t reserved;
+} apm_vector;
+
+enum apm_ckpt_format {
+    APM_CKPT_I8 = 0, /* element e, a whole number -127 .. 127, stands for e / 64 */
+    APM_CKPT_F8 = 1  /* element: a float of 4 exponent and 3 mantissa bits (E4M3 without infinities, largest 448) */
+};
+#define APM_CKPT_BLOCK 32
+
+/*
+ * A matrix in 8 bits: one byte per element, and one byte s for each APM_CKPT_BLOCK consecutive channels of a token (a
+ * row's last block may be shorter), which multiplies the block by 2^(s-127).  s is the smallest byte with which no
+ * element of the block is rounded to a value out of range (none is saturated; s = 254 at most, where the largest
+ * floats are).  A block that holds an infinity or a NaN has s = 255 and stands for NaN throughout.  Elements are rounded
+ * to nearest, ties to even: I8 elements are off by at most 1/255 to 1/127 of the block's largest (by where that lies between two
+ * powers of two), F8 elements by 2^-4 of their own size, or less than 2^-17 of the block's largest.  The values are bf16 numbers.
+ * q: rows of cols bytes, q_stride >= cols apart.  scale: rows of ceil(cols / 32) bytes, scale_stride apart.
+ */
+typedef struct {
+    void* q;
+    void* scale;
+    int64_t q_stride;
+    int64_t scale_stride;
+    int32_t format; /* apm_ckpt_format */
+    int32_t reserved;
+} apm_ckpt;
+
+/* x (bf16 or fp32) into 8 bits, and back, rounded to x's type: exact, but that 2^128, to which F8 rounds the very largest floats, is
+ * read as an infinity.  rows == 0 does nothing. */
+int apm_ckpt_write(int64_t rows, int64_t cols, const apm_matrix* x, const apm_ckpt* c, void* stream);
+int apm_ckpt_read(int64_t rows, int64_t cols, const apm_ckpt* c, const apm_matrix* x, void* stream);
+
+enum apm_norm_kind {
+    APM_NORM_NONE = 0, /* hat(v) = v, r = 1 */
+    APM_NORM_RMS = 1,  /* r = 1 / sqrt(mean(v^2) + eps), hat(v) = v r */
+    APM_NORM_LAYER = 2 /* r = 1 / sqrt(mean((v - mean(v))^2) + eps), hat(v) = (v - mean(v)) r */
+};
+enum apm_gate_kind {
+    APM_GATE_NONE = 0,    /* 1 */
+    APM_GATE_CHANNEL = 1, /* one row, for all tokens */
+    APM_GATE_TOKEN = 2,   /* one element per row */
+    APM_GATE_FULL = 3     /* rows x cols */
+};
+
+/* norm(v) = hat(v) weight + bias over a token's channels, each of the two vectors optional. */
+typedef struct {
+    int32_t kind; /* apm_norm_kind */
+    int32_t reserved;
+    double eps; /* >= 0 */
+    apm_vector weight;
+    apm_vector bias;
+    apm_ckpt ckpt; /* hat(v); q == NULL: not kept */
+    float* rstd;   /* r of every row; NULL: not kept (needed by the backward pass unless kind is NONE) */
+} apm_norm;
+
+/*
+ * Where a block of a residual network ends and the next one begins:
+ *     y = residual_scale x + gate post(branch),        n = pre(y)
+ * x and y are the residual stream, branch is what the block computed, n goes into the next block.  The statistics and n are
+ * those of y before it is rounded to its type; all arithmetic is fp32.
+ * x and y have one type, branch and n have one: bf16 and bf16, fp32 and bf16, or fp32 and fp32.  cols <= APM_JOIN_MAX_COLS.
+ * branch not given: y = residual_scale x; there must be no gate then, and post.kind APM_NORM_NONE.
+ * y, n, the kept tensors and rstd are written if they are given.  y may be x itself, n may be branch itself (same address and stride).
+ */
+#define APM_JOIN_MAX_COLS 16384
+typedef struct {
+    int64_t rows, cols;
+    double residual_scale;
+    apm_matrix x, branch, y, n, gate;
+    int32_t gate_kind; /* apm_gate_kind */
+    int32_t reserved;
+    apm_norm pre, post;
+} apm_norm_join;
+
+int apm_norm_join_forward(const apm_norm_join* j, void* stream);
+
+/*
+ * The gradients, out of the kept tensors (hat1 = pre.ckpt, hat2 = post.ckpt) and r: with t = dn pre.weight,
+ *     D = dy + r1 (t - [mean(t)] - hat1 mean(t hat1))      (the gradient of y; [..] with APM_NORM_LAYER; kind NONE: D = dy + t)
+ *     dx = residual_scale D;   dpre_weight = sum over rows of dn hat1;   dpre_bias = sum of dn
+ *     dgate = D (hat2 post.weight + post.bias), summed over what the gate's elements are shared by
+ *     u = gate D post.weight;  dbranch = r2 (u - [mean(u)] - hat2 mean(u hat2))
+ *     dpost_weight = sum of gate D hat2;   dpost_bias = sum of gate D
+ * dn or dy may be missing (0), not both.  Every output is written if it is given.  Types: dy and dx as x and y, dn and dbranch as
+ * branch and n; dgate, and each vector, bf16 or fp32.  dx may be dy itself, dbranch may be dn itself.
+ * Of `j` the call reads rows, cols, residual_scale, the gate, and in pre and post what the formulas name: the kept tensors that are
+ * needed must be there (pre.ckpt if dn is given, unless pre.kind is NONE and dpre_weight is not asked for; post.ckpt for dgate,
+ * dpost_weight, or dbranch through a norm).  Sums over rows are held in fp32 and do not depend on anything but the arguments: a second call
+ * gives the same bits.  rows == 0 writes zeros into the sums.
+ * workspace: apm_norm_join_workspace_bytes(rows, cols) bytes, 16-byte aligned, in use until the call's work is done.
+ */
+typedef struct {
+    apm_matrix dn, dy, dx, dbranch, dgate;
+    apm_vector dpre_weight, dpre_bias, dpost_weight, dpost_bias;
+} apm_norm_join_grads;
+
+size_t apm_norm_join_workspace_bytes(int64_t rows, int64_t cols);
+int apm_norm_join_backward(const apm_norm_join* j, const apm_norm_join_grads* g, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/*
+ * The gradient of the weights of a linear layer whose input was kept in 8 bits: with z[t, k] = kept[t, k] weight[k] + bias[k]
+ * (the norm's two vectors, where what is kept is its hat; each optional),
+ *     dw[o, k] = sum over tokens t of dy[t, o] z[t, k],        db[o] = sum over t of dy[t, o]
+ * dy: bf16 [tokens, out].  kept: [tokens, in].  dw: [out, in], bf16 or fp32, the type that the update reads.  db (optional): bf16 or fp32.
+ * n_groups > 0: that many such products, each over the tokens of its group: group g has tokens offsets[g] .. offsets[g+1] - 1
+ * (n_groups + 1 device int64; read on the device, where anything outside [0, tokens] is taken as the end next to it and a group that would end before it
+ * starts as empty).  dw is then [n_groups][out, in], dw_group_stride elements apart, db [n_groups][out] contiguous.  A group without tokens gets zeros.
+ * accumulate: added to what dw and db hold, with one rounding.
+ * Products are exact (kept values are bf16 numbers), sums fp32; weight and bias enter after the sum.  A second call gives the same bits.
+ * workspace: apm_ckpt_weight_grad_workspace_bytes(w) bytes (may be 0), 16-byte aligned, in use until the call's work is done.
+ */
+typedef struct {
+    int64_t tokens, out, in;
+    int64_t n_groups;       /* 0: one product over all tokens */
+    const int64_t* offsets; /* NULL if n_groups is 0 */
+    apm_matrix dy;
+    apm_ckpt kept;
+    apm_vector weight, bias;
+    apm_matrix dw;
+    int64_t dw_group_stride; /* only with n_groups > 1 */
+    apm_vector db;
+    int32_t accumulate;
+    int32_t reserved;
+} apm_weight_grad;
+
+size_t apm_ckpt_weight_grad_workspace_bytes(const apm_weight_grad* w);
+int apm_ckpt_weight_grad(const apm_weight_grad* w, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

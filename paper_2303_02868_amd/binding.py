@@ -22,6 +22,10 @@ APM_POOL_NO_ZERO = 1
 APM_POOL_FILE_DIRECT = 2
 APM_STREAM_STAGED, APM_STREAM_DIRECT, APM_STREAM_STAGED_DMA = 0, 1, 2
 APM_K_REDUCE, APM_K_UPDATE, APM_K_SEGCOPY, APM_N_KERNEL_CLASSES = 0, 1, 2, 3
+APM_CKPT_I8, APM_CKPT_F8, APM_CKPT_BLOCK = 0, 1, 32
+APM_NORM_NONE, APM_NORM_RMS, APM_NORM_LAYER = 0, 1, 2
+APM_GATE_NONE, APM_GATE_CHANNEL, APM_GATE_TOKEN, APM_GATE_FULL = 0, 1, 2, 3
+APM_JOIN_MAX_COLS = 16384
 ALL_STATES = 0b11111
 FP32_STATES = 0b00111
 B16_STATES = 0b11000
@@ -36,6 +40,8 @@ EXPORTS = [
     "apm_page_adamw_step_noalloc", "apm_noalloc_scratch_bytes", "apm_noalloc_max_pages",
     "apm_streamer_overlap_report",
     "apm_streamer_set_host_write_through",
+    "apm_ckpt_write", "apm_ckpt_read", "apm_norm_join_forward", "apm_norm_join_backward",
+    "apm_norm_join_workspace_bytes", "apm_ckpt_weight_grad", "apm_ckpt_weight_grad_workspace_bytes",
 ]
 
 
@@ -75,6 +81,43 @@ class apm_hyper(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
                 ("eps", C.c_double), ("weight_decay", C.c_double), ("max_grad_norm", C.c_double),
                 ("skip_mode", C.c_int32), ("reserved", C.c_int32)]
+
+
+class apm_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class apm_vector(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class apm_ckpt(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("q_stride", C.c_int64), ("scale_stride", C.c_int64),
+                ("format", C.c_int32), ("reserved", C.c_int32)]
+
+
+class apm_norm(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("eps", C.c_double), ("weight", apm_vector),
+                ("bias", apm_vector), ("ckpt", apm_ckpt), ("rstd", C.c_void_p)]
+
+
+class apm_norm_join(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("residual_scale", C.c_double), ("x", apm_matrix),
+                ("branch", apm_matrix), ("y", apm_matrix), ("n", apm_matrix), ("gate", apm_matrix),
+                ("gate_kind", C.c_int32), ("reserved", C.c_int32), ("pre", apm_norm), ("post", apm_norm)]
+
+
+class apm_norm_join_grads(C.Structure):
+    _fields_ = [("dn", apm_matrix), ("dy", apm_matrix), ("dx", apm_matrix), ("dbranch", apm_matrix),
+                ("dgate", apm_matrix), ("dpre_weight", apm_vector), ("dpre_bias", apm_vector),
+                ("dpost_weight", apm_vector), ("dpost_bias", apm_vector)]
+
+
+class apm_weight_grad(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("out", C.c_int64), ("in", C.c_int64), ("n_groups", C.c_int64),
+                ("offsets", C.c_void_p), ("dy", apm_matrix), ("kept", apm_ckpt), ("weight", apm_vector),
+                ("bias", apm_vector), ("dw", apm_matrix), ("dw_group_stride", C.c_int64), ("db", apm_vector),
+                ("accumulate", C.c_int32), ("reserved", C.c_int32)]
 
 
 class ApmError(RuntimeError):
@@ -152,6 +195,15 @@ def lib() -> C.CDLL:
     L.apm_delayed_set_outputs.argtypes = [vp, vp, vp]
     L.apm_pool_set_timing.argtypes = [vp, i32]
     L.apm_pool_read_timing.argtypes = [vp, P(C.c_double), P(i64)]
+    L.apm_ckpt_write.argtypes = [i64, i64, P(apm_matrix), P(apm_ckpt), vp]
+    L.apm_ckpt_read.argtypes = [i64, i64, P(apm_ckpt), P(apm_matrix), vp]
+    L.apm_norm_join_forward.argtypes = [P(apm_norm_join), vp]
+    L.apm_norm_join_backward.argtypes = [P(apm_norm_join), P(apm_norm_join_grads), vp, C.c_size_t, vp]
+    L.apm_norm_join_workspace_bytes.argtypes = [i64, i64]
+    L.apm_norm_join_workspace_bytes.restype = C.c_size_t
+    L.apm_ckpt_weight_grad.argtypes = [P(apm_weight_grad), vp, C.c_size_t, vp]
+    L.apm_ckpt_weight_grad_workspace_bytes.argtypes = [P(apm_weight_grad)]
+    L.apm_ckpt_weight_grad_workspace_bytes.restype = C.c_size_t
     for name in EXPORTS:
         getattr(L, name)              # every declared entry point must be exported
     _lib = L
@@ -568,3 +620,142 @@ def apm_pool_read_timing(pool: Pool):
     n = (C.c_int64 * APM_N_KERNEL_CLASSES)()
     _check(lib().apm_pool_read_timing(pool.handle, ms, n))
     return list(ms), list(n)
+
+
+# ---- activations --------------------------------------------------------------------------------
+# Tensors in, raw structures out: these look at shapes, strides and types, which the structures do not all carry.
+
+_DTYPES: dict = {}
+
+
+def _dtype(t) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        code = {"torch.float32": APM_F32, "torch.bfloat16": APM_BF16}.get(str(t.dtype))
+        if code is None:
+            raise ValueError(f"a tensor of {t.dtype}: float32 or bfloat16 is needed")
+        _DTYPES[t.dtype] = code
+    return code
+
+
+def _on_gpu(name, t):
+    if not t.is_cuda and not t.is_pinned():
+        raise ValueError(f"{name} is in memory that the GPU cannot address")
+    return t.data_ptr() or None
+
+
+def make_matrix(name: str, t, rows: int, cols: int) -> apm_matrix:
+    """The apm_matrix of a two-dimensional tensor (None: not given) that has to be rows x cols."""
+    if t is None:
+        return apm_matrix()
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()}, {rows} rows of {cols} contiguous elements are needed")
+    return apm_matrix(_on_gpu(name, t), t.stride(0), _dtype(t), 0)
+
+
+def make_vector(name: str, t, n: int) -> apm_vector:
+    if t is None:
+        return apm_vector()
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()}, {n} contiguous elements are needed")
+    return apm_vector(_on_gpu(name, t), _dtype(t), 0)
+
+
+def make_ckpt(q, scale, format: int) -> apm_ckpt:
+    """q: rows x cols of one byte each (any type), scale: rows x ceil(cols / 32) likewise."""
+    rows, cols = q.shape
+    nb = -(-cols // APM_CKPT_BLOCK)
+    if q.element_size() != 1 or scale.element_size() != 1 or scale.dim() != 2 or scale.shape[0] != rows or scale.shape[1] != nb \
+            or (cols > 1 and q.stride(1) != 1) or (nb > 1 and scale.stride(1) != 1):
+        raise ValueError(f"an 8-bit matrix of {tuple(q.shape)} needs bytes, and scales of {(rows, nb)}: got {tuple(scale.shape)}")
+    c = apm_ckpt(_on_gpu("q", q), _on_gpu("scale", scale), q.stride(0), scale.stride(0), format, 0)
+    c.shape, c.tensors = (rows, cols), (q, scale)
+    return c
+
+
+def _ckpt_of(name, c, rows, cols) -> apm_ckpt:
+    if c is None:
+        return apm_ckpt()
+    if c.shape != (rows, cols):
+        raise ValueError(f"{name}: {c.shape}, {(rows, cols)} is needed")
+    return c
+
+
+def apm_ckpt_write(x, ckpt: apm_ckpt, stream=None) -> None:
+    rows, cols = ckpt.shape
+    _check(lib().apm_ckpt_write(rows, cols, make_matrix("x", x, rows, cols), ckpt, _stream(stream)))
+
+
+def apm_ckpt_read(ckpt: apm_ckpt, x, stream=None) -> None:
+    rows, cols = ckpt.shape
+    _check(lib().apm_ckpt_read(rows, cols, ckpt, make_matrix("x", x, rows, cols), _stream(stream)))
+
+
+def make_norm_join(rows: int, cols: int, *, x=None, branch=None, y=None, n=None, residual_scale=1.0, gate_kind=APM_GATE_NONE, gate=None,
+                   pre_norm=APM_NORM_NONE, pre_eps=0.0, pre_weight=None, pre_bias=None, pre_ckpt=None, pre_rstd=None,
+                   post_norm=APM_NORM_NONE, post_eps=0.0, post_weight=None, post_bias=None, post_ckpt=None, post_rstd=None) -> apm_norm_join:
+    """What apm_norm_join_forward and _backward work on.  The tensors are kept alive by it."""
+    def norm(name, kind, eps, weight, bias, ckpt, rstd):
+        if rstd is not None and _dtype(rstd) != APM_F32:
+            raise ValueError(f"{name}_rstd must be float32")
+        return apm_norm(kind, 0, eps, make_vector(name + "_weight", weight, cols), make_vector(name + "_bias", bias, cols),
+                        _ckpt_of(name + "_ckpt", ckpt, rows, cols), make_vector(name + "_rstd", rstd, rows).data)
+
+    gate_rows, gate_cols = {APM_GATE_CHANNEL: (1, cols), APM_GATE_TOKEN: (rows, 1)}.get(gate_kind, (rows, cols))
+    j = apm_norm_join(rows, cols, residual_scale, make_matrix("x", x, rows, cols), make_matrix("branch", branch, rows, cols),
+                      make_matrix("y", y, rows, cols), make_matrix("n", n, rows, cols), make_matrix("gate", gate, gate_rows, gate_cols),
+                      gate_kind, 0, norm("pre", pre_norm, pre_eps, pre_weight, pre_bias, pre_ckpt, pre_rstd),
+                      norm("post", post_norm, post_eps, post_weight, post_bias, post_ckpt, post_rstd))
+    j.tensors = (x, branch, y, n, gate, pre_weight, pre_bias, pre_ckpt, pre_rstd, post_weight, post_bias, post_ckpt, post_rstd)
+    return j
+
+
+def make_norm_join_grads(join: apm_norm_join, *, dn=None, dy=None, dx=None, dbranch=None, dgate=None, dpre_weight=None, dpre_bias=None,
+                         dpost_weight=None, dpost_bias=None) -> apm_norm_join_grads:
+    rows, cols = join.rows, join.cols
+    gate_rows, gate_cols = {APM_GATE_CHANNEL: (1, cols), APM_GATE_TOKEN: (rows, 1)}.get(join.gate_kind, (rows, cols))
+    g = apm_norm_join_grads(make_matrix("dn", dn, rows, cols), make_matrix("dy", dy, rows, cols), make_matrix("dx", dx, rows, cols),
+                            make_matrix("dbranch", dbranch, rows, cols), make_matrix("dgate", dgate, gate_rows, gate_cols),
+                            make_vector("dpre_weight", dpre_weight, cols), make_vector("dpre_bias", dpre_bias, cols),
+                            make_vector("dpost_weight", dpost_weight, cols), make_vector("dpost_bias", dpost_bias, cols))
+    g.tensors = (dn, dy, dx, dbranch, dgate, dpre_weight, dpre_bias, dpost_weight, dpost_bias)
+    return g
+
+
+def apm_norm_join_forward(join: apm_norm_join, stream=None) -> None:
+    _check(lib().apm_norm_join_forward(join, _stream(stream)))
+
+
+def apm_norm_join_workspace_bytes(rows: int, cols: int) -> int:
+    return lib().apm_norm_join_workspace_bytes(rows, cols)
+
+
+def _room(workspace):
+    return (None, 0) if workspace is None else (_on_gpu("workspace", workspace), workspace.numel() * workspace.element_size())
+
+
+def apm_norm_join_backward(join: apm_norm_join, grads: apm_norm_join_grads, workspace, stream=None) -> None:
+    _check(lib().apm_norm_join_backward(join, grads, *_room(workspace), _stream(stream)))
+
+
+def make_weight_grad(dy, kept: apm_ckpt, dw, *, db=None, weight=None, bias=None, offsets=None, accumulate=False) -> apm_weight_grad:
+    """dw: [out, in], or with offsets (int64, groups + 1) [groups, out, in]; db: [out] or [groups, out]."""
+    tokens, k = kept.shape
+    out, groups = dy.shape[1], 0
+    if offsets is not None:
+        groups = offsets.numel() - 1
+        if str(offsets.dtype) != "torch.int64" or not offsets.is_contiguous() or groups < 1 or dw.dim() != 3 or dw.shape[0] != groups:
+            raise ValueError(f"offsets {offsets.dtype} of {tuple(offsets.shape)} for gradients of {tuple(dw.shape)}")
+    w = apm_weight_grad(tokens, out, k, groups, None if offsets is None else _on_gpu("offsets", offsets), make_matrix("dy", dy, tokens, out), kept,
+                        make_vector("weight", weight, k), make_vector("bias", bias, k), make_matrix("dw", dw[0] if groups else dw, out, k),
+                        dw.stride(0) if groups else 0, make_vector("db", db, max(1, groups) * out), int(accumulate), 0)
+    w.tensors = (dy, kept, dw, db, weight, bias, offsets)
+    return w
+
+
+def apm_ckpt_weight_grad_workspace_bytes(grad: apm_weight_grad) -> int:
+    return lib().apm_ckpt_weight_grad_workspace_bytes(grad)
+
+
+def apm_ckpt_weight_grad(grad: apm_weight_grad, workspace=None, stream=None) -> None:
+    _check(lib().apm_ckpt_weight_grad(grad, *_room(workspace), _stream(stream)))
