@@ -662,8 +662,9 @@ int apm_delayed_set_outputs(apm_pool* pool, float* grad_norm, uint8_t* skip_mask
  * a stride below the width), APM_ENOMEM (workspace too small), APM_EDEVICE. */
 
 /* rows x cols elements of `dtype`; a row starts `stride` elements after the one before, its elements are contiguous.
- * `data` is aligned to its elements at least (16 bytes, and rows of a multiple of 16 bytes, are fastest).  The rows of
- * a matrix that is only read may overlap (stride 0: one row for all tokens).  data == NULL: not given. */
+ * `data` is aligned to its elements at least (16 bytes, and rows of a multiple of 16 bytes, are fastest).  All of it lies in
+ * one allocation: what is between two rows may be read.  The rows of a matrix that is only read may overlap (stride 0: one row
+ * for all tokens).  data == NULL: not given. */
 typedef struct {
     void* data;
     int64_t stride;

@@ -16,11 +16,23 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kThreads = 256, kWave = 64;
-constexpr int kTile = 128, kTokens = 32;  // a workgroup's tile of dw, and the tokens that it takes at a time
-constexpr int kFrag = 32;                 // a matrix instruction's tile, over 16 tokens
-constexpr int kPerWave = kTile / 2 / kFrag;
-constexpr int kRowBytes = kTile * 2;
+constexpr int kWave = 64;
+constexpr int kFrag = 32, kStep = 16;  // a matrix instruction's tile, and the tokens that it takes
+
+// A workgroup's tile of dw: WO x WK wavefronts of FO x FK fragments, 64 tokens at a time.  What comes from memory for a later tile of
+// tokens waits in DEPTH sets of registers.
+template <int WO_, int WK_, int FO_, int FK_, int DEPTH_>
+struct Tile {
+    static constexpr int WO = WO_, WK = WK_, FO = FO_, FK = FK_, kDepth = DEPTH_, kTokens = 64;
+    static constexpr int kOut = WO * FO * kFrag, kIn = WK * FK * kFrag, kThreads = WO * WK * kWave;
+    static constexpr int kA = kTokens * kOut / kVec / kThreads;       // vectors of dy that a thread brings
+    static constexpr int kB = kTokens * kIn / (2 * kVec) / kThreads;  // 16 kept bytes each
+};
+// 256 x 256: a byte that comes in is used most often, and one workgroup fills a CU's registers.  128 x 128: four times as many tiles, for small
+// dw; one set of registers more hides what the shorter work on a tile does not (256 x 256 over 16384 tokens by one workgroup each, us: 206
+// with one set, 181 with two).
+typedef Tile<4, 2, 2, 4, 1> Large;
+typedef Tile<4, 2, 1, 2, 2> Small;
 
 struct WgradArgs {
     const char* dy;
@@ -35,57 +47,133 @@ struct WgradArgs {
     int64_t tokens, out, in;
     int32_t groups, splits, tiles_in, tiles;
     int32_t first_group;
-    int32_t format, dw_type, accumulate;
+    int32_t near_rows;  // rows lie so near to each other that a tile's addresses are 32-bit offsets
+    int32_t dw_type, accumulate;
 };
 
-// LDS: row t of a tile is kRowBytes, its 64-byte chunks exchanged by t mod 4, so that the four rows that a transposing load
+// LDS: the 64-byte chunks of a tile's row t are exchanged by t mod 4, so that the four rows that a transposing load
 // takes a chunk of lie in different banks.
-__device__ __forceinline__ int lds_at(int t, int byte) { return t * kRowBytes + ((((byte >> 6) ^ (t & 3)) << 6) | (byte & 63)); }
+template <int ROW> __device__ __forceinline__ int lds_at(int t, int byte) { return t * ROW + ((((byte >> 6) ^ (t & 3)) << 6) | (byte & 63)); }
 
-struct Stage {
-    u32x4 a[2];
-    u32x2 b[2];
-    uint32_t s;
-    int b_row;
-};
-
-__device__ __forceinline__ bf16x8 read_fragment(const char* tile, int frag, int t0, int lane) {
+// A fragment of one operand: lane l gets column l mod 32, eight tokens from 8 (l / 32) on.  A transposing load gives each of 16 lanes a column of
+// four rows that they bring together, eight bytes each.
+template <int ROW> __device__ __forceinline__ bf16x8 read_fragment(const char* tile, int frag, int t0, int lane) {
     typedef __attribute__((address_space(3))) s16x4* lds_ptr;
     const int row = t0 + 8 * (lane / 32) + (lane % 16) / 4;
-    const char* p = tile + row * kRowBytes + ((frag ^ (row & 3)) << 6) + ((lane / 16) & 1) * 32 + (lane & 3) * 8;
+    const char* p = tile + row * ROW + ((frag ^ (row & 3)) << 6) + ((lane / 16) & 1) * 32 + (lane & 3) * 8;
     union {
         s16x4 h[2];
         bf16x8 v;
     } u;
     u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
-    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * kRowBytes));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * ROW));
     return u.v;
 }
 
-__device__ __forceinline__ void finish(const WgradArgs& a, int64_t group, int64_t o, int64_t k, float v, float sum) {
-    if (a.weight.data) v *= load1(a.weight.data, a.weight.dtype, k);
-    if (a.bias.data) v = fmaf(load1(a.bias.data, a.bias.dtype, k), sum, v);
-    const int64_t at = group * a.group_stride + o * a.dw_stride + k;
-    if (a.accumulate) v += load1(a.dw, a.dw_type, at);
-    store1(a.dw, a.dw_type, at, v);
+// Eight kept bytes as bf16.
+__device__ __forceinline__ u32x4 to_bf16x8(u32x2 q, uint32_t s, int32_t format) {
+    u32x4 w;
+    if (format == APM_CKPT_I8) {
+        float v[kVec];
+        decode8(q, scale_of(s, APM_CKPT_I8), APM_CKPT_I8, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = to_bf16x2(v[2 * i], v[2 * i + 1]);
+    } else {
+        const float m = __builtin_bit_cast(float, s << 23);  // the instruction takes the exponent's byte alone, 255 for NaN
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            w[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[h], m, false));
+            w[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[h], m, true));
+        }
+    }
+    return w;
 }
+
+__device__ __forceinline__ void tokens_of(const WgradArgs& a, int64_t group, int64_t* begin, int64_t* end) {
+    *begin = 0, *end = a.tokens;
+    if (!a.offsets) return;
+    *begin = min(max(a.offsets[group], (int64_t)0), a.tokens);
+    *end = min(max(a.offsets[group + 1], *begin), a.tokens);
+}
+
 __device__ __forceinline__ void finish_sum(const WgradArgs& a, int64_t group, int64_t o, float sum) {
     const int64_t at = group * a.out + o;
     if (a.accumulate) sum += load1(a.db.data, a.db.dtype, at);
     store1(a.db.data, a.db.dtype, at, sum);
 }
+// Eight sums of row o from column k on, n of them there, become dw: v weight + bias (sum of dy), added to what is there if asked for.
+struct Columns {
+    float w[kVec], b[kVec];
+    __device__ __forceinline__ void load(const WgradArgs& a, int64_t k, int n, bool with_bias) {
+        const int64_t at = n > 0 ? k : 0;
+        RawAny raw;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) w[e] = 1.0f, b[e] = 0.0f;
+        if (a.weight.data) {
+            raw.load(a.weight.data, a.weight.dtype, (int)at, n);
+            raw.get(a.weight.dtype, w);
+        }
+        if (with_bias && a.bias.data) {
+            raw.load(a.bias.data, a.bias.dtype, (int)at, n);
+            raw.get(a.bias.dtype, b);
+        }
+    }
+};
+__device__ __forceinline__ void finish(const WgradArgs& a, const Columns& c, int64_t group, int64_t o, int64_t k, int n, float (&v)[kVec], float sum) {
+    char* row = a.dw + (group * a.group_stride + o * a.dw_stride) * (a.dw_type == APM_F32 ? 4 : 2);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) v[e] = fmaf(v[e], c.w[e], c.b[e] * sum);
+    if (a.accumulate) {
+        RawAny old;
+        old.load(row, a.dw_type, (int)k, n);
+        float f[kVec];
+        old.get(a.dw_type, f);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] += f[e];
+    }
+    if (a.dw_type == APM_F32) store8<float>(row, (int)k, n, v);
+    else store8<bf16>(row, (int)k, n, v);
+}
 
-template <bool SUMS>
-__global__ __launch_bounds__(kThreads) void apm_wgrad_kernel(WgradArgs a) {
-    __shared__ __attribute__((aligned(16))) char tile_a[2][kTokens * kRowBytes], tile_b[2][kTokens * kRowBytes];
+constexpr int kXcds = 8;
+constexpr int kStrip = 4;  // rows of tiles that are walked together
+
+// Bound by what LDS gives (a fragment is read by transposing loads, at about 120 bytes a clock) beside the matrix cores, which are busy half the
+// time at 1.9 GHz: 1100 (I8) to 1180 TFLOP/s (F8) at 16384 tokens x 8192 x 2048, 515 and 495 us with sums; a library product of bf16 matrices in this
+// order reaches 960, in the order that suits it 1300.
+template <class T, int FORMAT, bool SUMS>
+__global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
+    constexpr int kRowA = T::kOut * 2, kRowB = T::kIn * 2, kTokens = T::kTokens, FO = T::FO, FK = T::FK, D = T::kDepth, kSteps = kTokens / kStep;
+    constexpr int kTileA = kTokens * kRowA, kTileB = kTokens * kRowB;
+    __shared__ __attribute__((aligned(16))) char lds[2 * (kTileA + kTileB)];
+    __shared__ float row_sum[SUMS ? T::kOut : 1];
+    auto tile_a = [&](int buf) -> char* { return lds + buf * kTileA; };
+    auto tile_b = [&](int buf) -> char* { return lds + 2 * kTileA + buf * kTileB; };
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int tile = (int)(blockIdx.x % (uint32_t)a.tiles), rest = (int)(blockIdx.x / (uint32_t)a.tiles);
-    const int split = rest % a.splits, group = a.first_group + rest / a.splits;
-    const int64_t o0 = (int64_t)(tile / a.tiles_in) * kTile, k0 = (int64_t)(tile % a.tiles_in) * kTile;
-    int64_t begin = 0, end = a.tokens;
-    if (a.offsets) {
-        begin = min(max(a.offsets[group], (int64_t)0), a.tokens);
-        end = min(max(a.offsets[group + 1], begin), a.tokens);
+    // Workgroups go to the XCDs in turn.  Each XCD takes a stretch of the order, in which tiles come strip by strip, so that its L2 meets few
+    // rows and columns (16384 x 8192 x 2048, TFLOP/s: 930 in launch order, 970 with strips of 4 rows, 920 of 16).
+    // Groups one after the other on all XCDs: they have different numbers of tokens.
+    const uint32_t in_group = (uint32_t)(a.tiles * a.splits), nth = blockIdx.x % in_group, x = nth % kXcds;
+    const uint32_t id = x * (in_group / kXcds) + min(x, in_group % kXcds) + nth / kXcds;
+    const int group = a.first_group + (int)(blockIdx.x / in_group), split = (int)(id / (uint32_t)a.tiles), tile = (int)(id % (uint32_t)a.tiles);
+    const int strip = tile / (kStrip * a.tiles_in), in_strip = tile - strip * kStrip * a.tiles_in, high = min(kStrip, a.tiles / a.tiles_in - strip * kStrip);
+    const int64_t o0 = (int64_t)(strip * kStrip + in_strip % high) * T::kOut, k0 = (int64_t)(in_strip / high) * T::kIn;
+    int64_t begin, end;
+    tokens_of(a, group, &begin, &end);
+    if (begin == end && a.splits == 1) {  // no sum at all: not even weight times it
+        if (a.accumulate) return;
+        const float none[kVec] = {};
+        const int size = a.dw_type == APM_F32 ? 4 : 2;
+#pragma unroll 4
+        for (int i = tid; i < T::kOut * T::kIn / kVec; i += T::kThreads) {
+            const int64_t o = o0 + i / (T::kIn / kVec), k = k0 + i % (T::kIn / kVec) * kVec;
+            char* row = a.dw + (group * a.group_stride + o * a.dw_stride) * size;
+            const int n = o < a.out ? (int)max((int64_t)0, min((int64_t)kVec, a.in - k)) : 0;
+            if (a.dw_type == APM_F32) store8<float>(row, (int)k, n, none);
+            else store8<bf16>(row, (int)k, n, none);
+        }
+        if (SUMS && a.db.data && k0 == 0 && tid < T::kOut && o0 + tid < a.out) finish_sum(a, group, o0 + tid, 0.0f);
+        return;
     }
     if (a.splits > 1) {
         const int64_t each = (end - begin + (int64_t)a.splits * kTokens - 1) / ((int64_t)a.splits * kTokens) * kTokens;
@@ -93,142 +181,286 @@ __global__ __launch_bounds__(kThreads) void apm_wgrad_kernel(WgradArgs a) {
         end = min(begin + each, end);
     }
 
-    auto load = [&](Stage& s, int64_t t0) {
+    u32x4 sa[D][T::kA] = {}, sb[D][T::kB] = {};
+    uint32_t ss[D][T::kB] = {};
+    constexpr int kPerRowA = T::kOut / kVec, kRowsA = T::kThreads / kPerRowA, kPerRowB = T::kIn / (2 * kVec), kRowsB = T::kThreads / kPerRowB;
+    const int row_a = tid / kPerRowA, col_a = tid % kPerRowA * kVec, row_b = tid / kPerRowB, col_b = tid % kPerRowB * 2 * kVec;
+    // Whole tiles of tokens whose loads end inside the matrices; columns beyond a tile's edge then are the next row's, and land in what is not stored.
+    auto load = [&](int set, int64_t t0) {
+        const char* pa = a.dy + (t0 * a.dy_stride + o0) * 2;
+        const char* pq = a.q + t0 * a.q_stride + k0;
+        const uint8_t* ps = a.scale + t0 * a.scale_stride + k0 / APM_CKPT_BLOCK;
+        const uint32_t da = ((uint32_t)row_a * (uint32_t)a.dy_stride + (uint32_t)col_a) * 2u, dq = (uint32_t)row_b * (uint32_t)a.q_stride + (uint32_t)col_b,
+                       ds = (uint32_t)row_b * (uint32_t)a.scale_stride + (uint32_t)col_b / APM_CKPT_BLOCK;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int id = i * kThreads + tid, row = id / (kTile / kVec), c = id % (kTile / kVec) * kVec;
-            const int64_t t = t0 + row;
-            Raw<bf16> r;
-            r.load(a.dy + t * a.dy_stride * 2, (int)(o0 + c), t < end ? (int)min((int64_t)kVec, a.out - (o0 + c)) : 0);
-            s.a[i] = r.a;
+        for (int i = 0; i < T::kA; ++i) sa[set][i] = *(const u32x4_any*)(pa + i * kRowsA * a.dy_stride * 2 + da);
+#pragma unroll
+        for (int i = 0; i < T::kB; ++i) {
+            sb[set][i] = *(const u32x4_any*)(pq + i * kRowsB * a.q_stride + dq);
+            ss[set][i] = ps[i * kRowsB * a.scale_stride + ds];
         }
-        const int row = tid / 8, c = tid % 8 * 16;
-        const int64_t t = t0 + row;
-        const int n = t < end ? (int)min((int64_t)16, a.in - (k0 + c)) : 0;
-        s.b[0] = load_q(a.q + t * a.q_stride, (int)(k0 + c), n);
-        s.b[1] = load_q(a.q + t * a.q_stride, (int)(k0 + c) + kVec, n - kVec);
-        s.s = n > 0 ? a.scale[t * a.scale_stride + (k0 + c) / APM_CKPT_BLOCK] : 0u;
     };
-    auto put = [&](const Stage& s, int buf) {
+    auto load_guarded = [&](int set, int64_t t0) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int id = i * kThreads + tid, row = id / (kTile / kVec), c = id % (kTile / kVec) * kVec;
-            *(u32x4*)(tile_a[buf] + lds_at(row, c * 2)) = s.a[i];
+        for (int i = 0; i < T::kA; ++i) {
+            const int64_t t = t0 + row_a + i * kRowsA, o = o0 + col_a;
+            Raw<bf16> r;
+            r.load(a.dy + t * a.dy_stride * 2, (int)o, t < end ? (int)min((int64_t)kVec, a.out - o) : 0);
+            sa[set][i] = r.a;
         }
-        const int row = tid / 8, c = tid % 8 * 16;
-        const float m = scale_of(s.s, a.format);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float v[kVec];
-            decode8(s.b[h], m, a.format, v);
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = to_bf16x2(v[2 * i], v[2 * i + 1]);
-            *(u32x4*)(tile_b[buf] + lds_at(row, (c + h * kVec) * 2)) = w;
+        for (int i = 0; i < T::kB; ++i) {
+            const int64_t t = t0 + row_b + i * kRowsB, k = k0 + col_b;
+            const int n = t < end ? (int)min((int64_t)(2 * kVec), a.in - k) : 0;
+            const u32x2 lo = load_q(a.q + t * a.q_stride, (int)k, n), hi = load_q(a.q + t * a.q_stride, (int)k + kVec, n - kVec);
+            sb[set][i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+            ss[set][i] = n > 0 ? a.scale[t * a.scale_stride + k / APM_CKPT_BLOCK] : 0u;
         }
+    };
+    auto put_a = [&](int buf, int set, int i) { *(u32x4*)(tile_a(buf) + lds_at<kRowA>(row_a + i * kRowsA, col_a * 2)) = sa[set][i]; };
+    auto put_b = [&](int buf, int set, int i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            *(u32x4*)(tile_b(buf) + lds_at<kRowB>(row_b + i * kRowsB, (col_b + h * kVec) * 2)) =
+                to_bf16x8(u32x2{sb[set][i][2 * h], sb[set][i][2 * h + 1]}, ss[set][i], FORMAT);
     };
 
-    f32x16 acc[kPerWave][kPerWave];
-    float sum[kPerWave];
+    f32x16 acc[FO][FK];
+    float sum[FO];
 #pragma unroll
-    for (int m = 0; m < kPerWave; ++m) {
+    for (int m = 0; m < FO; ++m) {
         sum[m] = 0.0f;
 #pragma unroll
-        for (int n = 0; n < kPerWave; ++n)
+        for (int n = 0; n < FK; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.0f;
     }
-    const int wm = wave / 2 * kPerWave, wn = wave % 2 * kPerWave;  // the wavefront's first fragments
-    Stage s;
-    if (begin < end) {
-        load(s, begin);
-        put(s, 0);
-    }
-    __syncthreads();
-    int buf = 0;
-    for (int64_t t0 = begin; t0 < end; t0 += kTokens, buf ^= 1) {
-        const bool more = t0 + kTokens < end;
-        if (more) load(s, t0 + kTokens);
+    const int wm = wave / T::WK * FO, wn = wave % T::WK * FK;  // the wavefront's first fragments
+    bf16x8 fa[2][FO], fb[2][FK];
+    auto read = [&](int buf, int step) {
 #pragma unroll
-        for (int t = 0; t < kTokens; t += 16) {
-            bf16x8 fa[kPerWave], fb[kPerWave];
+        for (int m = 0; m < FO; ++m) fa[step & 1][m] = read_fragment<kRowA>(tile_a(buf), wm + m, step * kStep, lane);
 #pragma unroll
-            for (int m = 0; m < kPerWave; ++m) fa[m] = read_fragment(tile_a[buf], wm + m, t, lane);
+        for (int n = 0; n < FK; ++n) fb[step & 1][n] = read_fragment<kRowB>(tile_b(buf), wn + n, step * kStep, lane);
+    };
+    auto multiply = [&](int step) {
 #pragma unroll
-            for (int n = 0; n < kPerWave; ++n) fb[n] = read_fragment(tile_b[buf], wn + n, t, lane);
+        for (int m = 0; m < FO; ++m) {
 #pragma unroll
-            for (int m = 0; m < kPerWave; ++m) {
+            for (int n = 0; n < FK; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[step & 1][m], fb[step & 1][n], acc[m][n], 0, 0, 0);
+            if constexpr (SUMS) {
+                const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-                for (int n = 0; n < kPerWave; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[m], fb[n], acc[m][n], 0, 0, 0);
-                if constexpr (SUMS)
-#pragma unroll
-                    for (int i = 0; i < kVec; ++i) sum[m] += (float)fa[m][i];
+                for (int i = 0; i < kVec; i += 2) sum[m] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{fa[step & 1][m][i], fa[step & 1][m][i + 1]}, one, sum[m], false);
             }
         }
-        if (more) put(s, buf ^ 1);
+    };
+    // A tile of tokens, in steps.  Fragments are read a step ahead.  In the middle steps what a set of registers holds of the next tile goes into the
+    // other buffer; before the last one everybody has read this buffer, so that the set is filled anew and the next tile's first fragments are read.
+    auto turn = [&](int buf, int set, auto&& fetch) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s == kSteps - 1) {
+                __syncthreads();
+                fetch();
+            }
+            read(s == kSteps - 1 ? buf ^ 1 : buf, (s + 1) % kSteps);
+            multiply(s);
+            if (s > 0 && s < kSteps - 1) {
+#pragma unroll
+                for (int i = s - 1; i < T::kA; i += kSteps - 2) put_a(buf ^ 1, set, i);
+#pragma unroll
+                for (int i = s - 1; i < T::kB; i += kSteps - 2) put_b(buf ^ 1, set, i);
+            }
+            if constexpr (FO * FK == 8) {  // the order that the scheduler is to keep: between two products a part of everything else
+#pragma unroll
+                for (int i = 0; i < FO * FK; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);  // LDS reads
+                    __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // vector arithmetic
+                    __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // LDS writes
+                    __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // memory reads
+                }
+            }
+        }
+    };
+    const int64_t n_tiles = (end - begin + kTokens - 1) / kTokens;
+    int64_t whole = 0;  // tiles that `load` may take
+    if (a.near_rows) {
+        auto reach = [&](int64_t stride, int64_t width, int64_t first, int64_t take) {  // tokens of whose rows `take` columns from `first` on may be read
+            const int64_t over = first + take - width;
+            return over <= 0 ? a.tokens : stride > 0 ? a.tokens - (over + stride - 1) / stride : (int64_t)0;
+        };
+        const int64_t last = min(end, min(min(reach(a.dy_stride, a.out, o0, T::kOut), reach(a.q_stride, a.in, k0, T::kIn)),
+                                          reach(a.scale_stride, (a.in + APM_CKPT_BLOCK - 1) / APM_CKPT_BLOCK, k0 / APM_CKPT_BLOCK, T::kIn / APM_CKPT_BLOCK)));
+        whole = max((last - begin) / kTokens, (int64_t)0);
+    }
+    auto fetch = [&](int set, int64_t i) {
+        if (i < whole) load(set, begin + i * kTokens);
+        else if (i < n_tiles) load_guarded(set, begin + i * kTokens);
+    };
+    if (n_tiles > 0) {  // the last turns put and read what is not used
+        fetch(0, 0);
+#pragma unroll
+        for (int i = 0; i < T::kA; ++i) put_a(0, 0, i);
+#pragma unroll
+        for (int i = 0; i < T::kB; ++i) put_b(0, 0, i);
+#pragma unroll
+        for (int i = 1; i <= D; ++i) fetch(i % D, i);
+        __syncthreads();
+        read(0, 0);
+        int64_t i = 0;
+        if constexpr (D == 1) {
+            int buf = 0;
+            for (; i + 2 < whole; ++i, buf ^= 1) turn(buf, 0, [&] { load(0, begin + (i + 2) * kTokens); });
+            for (; i < n_tiles; ++i, buf ^= 1) turn(buf, 0, [&] { fetch(0, i + 2); });
+        } else {
+            for (; i + 4 < whole; i += 2) {
+                turn(0, 1, [&] { load(1, begin + (i + 3) * kTokens); });
+                turn(1, 0, [&] { load(0, begin + (i + 4) * kTokens); });
+            }
+            for (; i < n_tiles; i += 2) {
+                turn(0, 1, [&] { fetch(1, i + 3); });
+                if (i + 1 < n_tiles) turn(1, 0, [&] { fetch(0, i + 4); });
+            }
+        }
         __syncthreads();
     }
 
     // Lane l has column l mod 32 of a fragment's tile, rows 8 (r / 4) + 4 (l / 32) + r mod 4 in register r; a row's sum over the tokens of
     // one half of the lanes each.
     const int64_t gs = (int64_t)split * a.groups + group;
+    if constexpr (SUMS) {
 #pragma unroll
-    for (int m = 0; m < kPerWave; ++m) {
-        if constexpr (SUMS) {
+        for (int m = 0; m < FO; ++m) {
             sum[m] += __shfl_xor(sum[m], 32);
-            const int64_t o = o0 + (wm + m) * kFrag + lane;
-            if (k0 == 0 && wn == 0 && lane < kFrag && o < a.out) {
-                if (a.splits > 1) a.sums[gs * a.out + o] = sum[m];
-                else if (a.db.data) finish_sum(a, group, o, sum[m]);
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int in_tile = 8 * (r / 4) + 4 * (lane / 32) + r % 4;
-            const int64_t o = o0 + (wm + m) * kFrag + in_tile;
-            const float of_row = SUMS ? __shfl(sum[m], in_tile) : 0.0f;
-#pragma unroll
-            for (int n = 0; n < kPerWave; ++n) {
-                const int64_t k = k0 + (wn + n) * kFrag + lane % 32;
-                if (o < a.out && k < a.in) {
-                    if (a.splits > 1) a.part[(gs * a.out + o) * a.in + k] = acc[m][n][r];
-                    else finish(a, group, o, k, acc[m][n][r], of_row);
+            if (wn == 0 && lane < kFrag) {
+                row_sum[(wm + m) * kFrag + lane] = sum[m];
+                const int64_t o = o0 + (wm + m) * kFrag + lane;
+                if (k0 == 0 && o < a.out) {
+                    if (a.splits > 1) a.sums[gs * a.out + o] = sum[m];
+                    else if (a.db.data) finish_sum(a, group, o, sum[m]);
                 }
             }
         }
+        __syncthreads();
     }
+    if (a.splits > 1) {
+#pragma unroll
+        for (int m = 0; m < FO; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int64_t o = o0 + (wm + m) * kFrag + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
+                float* row = a.part + (gs * a.out + o) * a.in;
+#pragma unroll
+                for (int n = 0; n < FK; ++n) {
+                    const int64_t k = k0 + (wn + n) * kFrag + lane % 32;
+                    if (o < a.out && k < a.in) row[k] = acc[m][n][r];
+                }
+            }
+        return;
+    }
+    // Rows are stored in whole vectors: half a fragment's rows at a time go through LDS, each wavefront for itself.
+    constexpr int kRow = FK * kFrag + 4, kPer = FK * kFrag / kVec, kRowsAtOnce = kWave / kPer;
+    static_assert(T::WO * T::WK * 16 * kRow * 4 <= (int)sizeof lds, "the wavefronts' rows fit");
+    float* mine = (float*)lds + wave * 16 * kRow;
+    const int c = lane % kPer * kVec;
+    const int64_t k = k0 + wn * kFrag + c;
+    const int there = (int)max((int64_t)0, min((int64_t)kVec, a.in - k));
+    Columns cols;
+    cols.load(a, k, there, SUMS);
+#pragma unroll
+    for (int m = 0; m < FO; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // registers 8 h .. 8 h + 7: rows 16 h .. 16 h + 15
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+#pragma unroll
+                for (int n = 0; n < FK; ++n) mine[(8 * (r / 4) + 4 * (lane / 32) + r % 4) * kRow + n * kFrag + lane % 32] = acc[m][n][8 * h + r];
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
+                const int row = i * kRowsAtOnce + lane / kPer, in_tile = (wm + m) * kFrag + 16 * h + row;
+                const int64_t o = o0 + in_tile;
+                float v[kVec];
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) v[e] = mine[row * kRow + c + e];
+                finish(a, cols, group, o, k, o < a.out ? there : 0, v, SUMS ? row_sum[in_tile] : 0.0f);
+            }
+        }
 }
 
-// The splits' parts, added in order.
+// The splits' parts, added in order: eight columns of a row a thread, four parts under way at a time.
+constexpr int kJoinThreads = 256;
 template <bool SUMS>
-__global__ __launch_bounds__(kThreads) void apm_wgrad_join_kernel(WgradArgs a) {
-    const int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t go = blockIdx.y, group = go / a.out, o = go - group * a.out;
-    float sum = 0.0f;
-    if constexpr (SUMS)
-        for (int s = 0; s < a.splits; ++s) sum += a.sums[((int64_t)s * a.groups + group) * a.out + o];
-    if (k < a.in) {
-        float v = 0.0f;
-        for (int s = 0; s < a.splits; ++s) v += a.part[(((int64_t)s * a.groups + group) * a.out + o) * a.in + k];
-        finish(a, group, o, k, v, sum);
+__global__ __launch_bounds__(kJoinThreads) void apm_wgrad_join_kernel(WgradArgs a) {
+    const uint32_t per_row = (uint32_t)((a.in + kVec - 1) / kVec), id = blockIdx.x * kJoinThreads + threadIdx.x, row = id / per_row;
+    const int64_t rows = (int64_t)a.groups * a.out;
+    if (row >= rows) return;
+    const int k = (int)(id - row * per_row) * kVec, n = (int)min((int64_t)kVec, a.in - k);
+    const int64_t group = row / (uint32_t)a.out, o = row - (uint32_t)group * (uint32_t)a.out;
+    int64_t begin, end;
+    tokens_of(a, group, &begin, &end);
+    Columns cols;
+    cols.load(a, k, begin < end ? n : 0, SUMS);
+    float v[kVec] = {};
+    for (int s = 0; s < a.splits; s += 4) {
+        Raw<float> part[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[i].load(a.part + ((s + i) * rows + row) * a.in, k, s + i < a.splits ? n : 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[e] += part[i][e];
     }
-    if (SUMS && k == 0 && a.db.data) finish_sum(a, group, o, sum);
+    float sum = 0.0f;
+    if constexpr (SUMS) {
+        for (int s = 0; s < a.splits; ++s) sum += a.sums[s * rows + row];
+        if (k == 0 && a.db.data) finish_sum(a, group, o, sum);
+    }
+    finish(a, cols, group, o, k, n, v, sum);
 }
 
+// Which tile, and into how many parts the tokens are split, so that few tiles fill the chip.  Estimated in us, from calls that were timed: a round of
+// workgroups, one a CU, costs `start` and `tile` for each 64 tokens (256 x 256: 515 us for 256 of them, 140 for 64, 18.7 for one; 128 x 128: 181 for 256, 18.9 for
+// 16); parts are written and read at 4 TB/s, by one kernel more.  With one part and the better split (tokens x out x in): 1000 x 768 x 768 18.9 / 17.8,
+// 8192 x 768 x 768 94.6 / 30.3, 8192 x 2048 x 2048 by 256 x 256 209 / 91, by 128 x 128 102 / 112.
+constexpr int64_t kCus = 256, kMostSplits = 64;
 struct WgradShape {
+    bool large;
     int64_t tiles_out, tiles_in, groups;
     int32_t splits;
 };
+template <class T>
+double best_split(const apm_weight_grad& w, double start, double tile, WgradShape* s) {
+    s->tiles_out = div_up(w.out, T::kOut), s->tiles_in = div_up(w.in, T::kIn), s->groups = std::max<int64_t>(1, w.n_groups);
+    const int64_t tiles = s->tiles_out * s->tiles_in * s->groups, each = div_up(w.tokens, s->groups);
+    double best = 0.0;
+    s->splits = 1;
+    for (int64_t n = 1; n <= kMostSplits && (n == 1 || (tiles * n <= 2 * kCus && n <= div_up(each, 2 * T::kTokens))); ++n) {
+        const double rounds = (double)div_up(tiles * n, kCus), turns = (double)div_up(div_up(each, n), T::kTokens);
+        const double parts = n > 1 ? 4.0 + 8.0 * (double)n * (double)s->groups * (double)w.out * (double)w.in / 4e6 : 0.0;
+        const double cost = rounds * (start + turns * tile) + parts;
+        if (n == 1 || cost < best) best = cost, s->splits = (int32_t)n;
+    }
+    return best;
+}
 WgradShape wgrad_shape(const apm_weight_grad& w) {
-    WgradShape s;
-    s.tiles_out = div_up(w.out, kTile), s.tiles_in = div_up(w.in, kTile);
-    s.groups = std::max<int64_t>(1, w.n_groups);
-    const int64_t tiles = s.tiles_out * s.tiles_in * s.groups;
-    s.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, div_up(w.tokens, 4 * kTokens), 64}));
-    return s;
+    WgradShape large, small;
+    large.large = true, small.large = false;
+    return best_split<Large>(w, 14.0, 1.95, &large) < best_split<Small>(w, 8.0, 0.7, &small) ? large : small;
 }
 size_t workspace_of(const apm_weight_grad& w, const WgradShape& s) {
     return s.splits > 1 ? (size_t)s.splits * s.groups * w.out * (w.in + 1) * sizeof(float) : 0;
+}
+
+template <class T>
+hipError_t launch_wgrad(const WgradArgs& a, int32_t format, bool sums, unsigned workgroups, hipStream_t s) {
+    auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(workgroups), dim3(T::kThreads), 0, s, a); };
+    if (format == APM_CKPT_I8) sums ? start(apm_wgrad_kernel<T, APM_CKPT_I8, true>) : start(apm_wgrad_kernel<T, APM_CKPT_I8, false>);
+    else sums ? start(apm_wgrad_kernel<T, APM_CKPT_F8, true>) : start(apm_wgrad_kernel<T, APM_CKPT_F8, false>);
+    return hipGetLastError();
 }
 
 int check_grad(const apm_weight_grad& w) {
@@ -264,8 +496,9 @@ int weight_grad(const apm_weight_grad* wp, void* workspace, size_t workspace_byt
     a.dw_stride = w.dw.stride, a.group_stride = w.dw_group_stride;
     a.tokens = w.tokens, a.out = w.out, a.in = w.in;
     a.groups = (int32_t)s.groups, a.splits = s.splits, a.tiles_in = (int32_t)s.tiles_in;
-    a.format = w.kept.format, a.dw_type = w.dw.dtype, a.accumulate = w.accumulate;
-    const int64_t tiles = s.tiles_out * s.tiles_in, most = max_workgroups(kThreads);
+    a.near_rows = std::max({w.dy.stride, w.kept.q_stride, w.kept.scale_stride}) < (1 << 24);
+    a.dw_type = w.dw.dtype, a.accumulate = w.accumulate;
+    const int64_t tiles = s.tiles_out * s.tiles_in, most = max_workgroups(std::max(Large::kThreads, Small::kThreads));
     if (tiles > most / s.splits) return fail(APM_EINVAL, "dw is too large for one product");
     a.tiles = (int32_t)tiles;
     const bool sums = w.bias.data || w.db.data;
@@ -273,15 +506,13 @@ int weight_grad(const apm_weight_grad* wp, void* workspace, size_t workspace_byt
     const int64_t groups_per_launch = most / (tiles * s.splits);
     for (int64_t g = 0; g < s.groups; g += groups_per_launch) {
         a.first_group = (int32_t)g;
-        const dim3 grid((unsigned)(tiles * s.splits * std::min(groups_per_launch, s.groups - g)));
-        if (sums) hipLaunchKernelGGL(apm_wgrad_kernel<true>, grid, dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL(apm_wgrad_kernel<false>, grid, dim3(kThreads), 0, st, a);
-        APM_HIP(hipGetLastError());
+        const unsigned n = (unsigned)(tiles * s.splits * std::min(groups_per_launch, s.groups - g));
+        APM_HIP(s.large ? launch_wgrad<Large>(a, w.kept.format, sums, n, st) : launch_wgrad<Small>(a, w.kept.format, sums, n, st));
     }
-    if (s.splits > 1) {  // so that there are few tiles, and few rows of dw
-        const dim3 grid((unsigned)div_up(w.in, kThreads), (unsigned)(s.groups * w.out));
-        if (sums) hipLaunchKernelGGL(apm_wgrad_join_kernel<true>, grid, dim3(kThreads), 0, st, a);
-        else hipLaunchKernelGGL(apm_wgrad_join_kernel<false>, grid, dim3(kThreads), 0, st, a);
+    if (s.splits > 1) {  // so that there are few tiles: under 2^32 vectors
+        const dim3 grid((unsigned)div_up(div_up(w.in, kVec) * s.groups * w.out, kJoinThreads));
+        if (sums) hipLaunchKernelGGL(apm_wgrad_join_kernel<true>, grid, dim3(kJoinThreads), 0, st, a);
+        else hipLaunchKernelGGL(apm_wgrad_join_kernel<false>, grid, dim3(kJoinThreads), 0, st, a);
         APM_HIP(hipGetLastError());
     }
     return APM_OK;

@@ -552,6 +552,48 @@ def test_weight_gradient_of_groups(offsets, out, k):
     check_weight_grad(100, out, k, A.F8, offsets=offsets, bias=False, weight=False, accumulate=True, pad=1)
 
 
+@pytest.mark.parametrize("tokens,out,k,pad,shift", [(130, 4096, 4096, 0, 0), (70, 4001, 4007, 1, 3), (300, 3900, 4100, 8, 8), (64, 4097, 4090, 0, 0)])
+def test_weight_gradient_of_large_matrices(tokens, out, k, pad, shift):
+    check_weight_grad(tokens, out, k, A.I8, BF16, pad=pad, shift=shift)
+    check_weight_grad(tokens, out, k, A.F8, BF16, weight=False, bias=False, db=False, pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_weight_gradient_of_groups_of_large_matrices(accumulate):
+    check_weight_grad(300, 1100, 1030, A.F8, BF16, offsets=[0, 0, 129, 130, 130, 300, 300] + [300] * 10, accumulate=accumulate)
+    check_weight_grad(2000, 1100, 1030, A.I8, F32, offsets=[0, 700, 700, 2000], accumulate=accumulate)
+
+
+def test_weight_gradient_without_tokens_is_zero_whatever_the_weight():
+    kept, _ = random_kept(600, 64, A.I8, 2)
+    dy = torch.randn(600, 40, device=DEV).bfloat16()
+    w = torch.full((64,), float("inf"), device=DEV)
+    for offsets in ([0, 0, 600], [0] * 9 + [600]):
+        n = len(offsets) - 1
+        dw, db = torch.full((n, 40, 64), 7.0, device=DEV), torch.full((n, 40), 7.0, device=DEV)
+        grad = apm.make_weight_grad(dy, apm.make_ckpt(*kept, A.I8), dw, db=db, weight=w, bias=w, offsets=torch.tensor(offsets, device=DEV))
+        apm.apm_ckpt_weight_grad(grad, torch.empty(max(16, apm.apm_ckpt_weight_grad_workspace_bytes(grad)), dtype=torch.uint8, device=DEV))
+        assert bool((dw[:-1] == 0).all()) and bool((db[:-1] == 0).all())
+
+
+@pytest.mark.parametrize("fmt", [A.I8, A.F8])
+def test_weight_gradient_reads_every_code_and_scale(fmt):
+    """One token per scale: the product with a dy of one 1 per token and output is the kept value itself."""
+    q = torch.arange(256, device=DEV).to(torch.uint8).repeat(255, 1)
+    bad = [128] if fmt == A.I8 else [127, 255]
+    q[:, bad] = 0
+    s = torch.arange(255, device=DEV).to(torch.uint8)[:, None].repeat(1, 8).contiguous()
+    dy = torch.eye(255, device=DEV).bfloat16()
+    dw = torch.empty(255, 256, device=DEV)
+    apm.apm_ckpt_weight_grad(apm.make_weight_grad(dy, apm.make_ckpt(q, s, fmt), dw), torch.empty(1 << 22, dtype=torch.uint8, device=DEV))
+    want = A.decode(q.cpu().numpy(), s.cpu().numpy(), fmt)
+    lost = (np.abs(want) >= 2.0 ** 128).any(axis=0)     # no bf16 number: infinite, and 0 times it is no number in the other tokens' rows
+    assert np.isnan(f64(dw)[:-8, lost]).all() and lost.any() == (fmt == A.F8)
+    normal = ~lost[None, :] & ((np.abs(want) >= 2.0 ** -126) | (want == 0))
+    assert np.array_equal(f64(dw)[normal], want[normal])
+    assert np.all(np.abs(f64(dw) - want)[:, ~lost] <= 2.0 ** -126)          # subnormals may be taken as zero
+
+
 def test_weight_gradient_of_many_groups():
     check_weight_grad(2000, 64, 96, offsets=sorted(np.random.default_rng(3).integers(0, 2000, 201).tolist()))
 
