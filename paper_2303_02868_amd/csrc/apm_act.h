@@ -34,7 +34,7 @@ template <class T> struct Raw;
 template <> struct Raw<bf16> {
     u32x4 a;
     __device__ __forceinline__ void load(const void* row, int col, int n) {
-        const char* p = (const char*)row + (int64_t)col * 2;
+        const char* p = (const char*)row + (uint32_t)col * 2u;
         a = u32x4{0, 0, 0, 0};
         if (n >= kVec) {
             a = *(const u32x4_any*)p;
@@ -49,7 +49,7 @@ template <> struct Raw<bf16> {
 template <> struct Raw<float> {
     u32x4 a, b;
     __device__ __forceinline__ void load(const void* row, int col, int n) {
-        const char* p = (const char*)row + (int64_t)col * 4;
+        const char* p = (const char*)row + (uint32_t)col * 4u;
         a = b = u32x4{0, 0, 0, 0};
         if (n >= kVec) {
             a = ((const u32x4_any*)p)[0];
@@ -66,7 +66,7 @@ template <> struct Raw<float> {
     __device__ __forceinline__ float operator[](int i) const { return __builtin_bit_cast(float, i < 4 ? a[i & 3] : b[i & 3]); }
 };
 template <class T> __device__ __forceinline__ void store8(void* row, int col, int n, const float (&v)[kVec]) {
-    char* p = (char*)row + (int64_t)col * (int64_t)sizeof(T);
+    char* p = (char*)row + (uint32_t)col * (uint32_t)sizeof(T);
     if constexpr (sizeof(T) == sizeof(float)) {
         if (n >= kVec) {
 #pragma unroll
@@ -108,7 +108,7 @@ struct RawAny {
     __device__ __forceinline__ void load(const void* row, int32_t dtype, int col, int n) {
         const bool wide = dtype == APM_F32;
         a = b = u32x4{0, 0, 0, 0};
-        const char* p = (const char*)row + (int64_t)col * (wide ? 4 : 2);
+        const char* p = (const char*)row + (uint32_t)col * (wide ? 4u : 2u);
         if (n >= kVec) {
             a = ((const u32x4_any*)p)[0];
             if (wide) b = ((const u32x4_any*)p)[1];
@@ -135,6 +135,75 @@ struct RawAny {
         }
     }
 };
+
+// A row's whole vectors as a buffer: what lies beyond them (or all of it, if there is no such row or matrix) reads as zero and is not written,
+// so that every lane loads and stores without a branch, and nothing waits for more than it needs.  What is behind the last whole vector
+// comes and goes one by one.  Non-temporal: these streams are larger than the caches (gradients of a join of 8192 x 5120, fp32 stream: 119 us
+// with the default policy, 115 with non-temporal stores, 108.6 with loads too).
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+constexpr int kNT = 2;
+__device__ __forceinline__ Rsrc row_buffer(const void* data, int64_t byte_offset, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)data + byte_offset), 0, data ? bytes : 0, 0x00027000);
+}
+__device__ __forceinline__ u32x4 load_b128(Rsrc r, uint32_t byte) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)byte, 0, kNT)); }
+__device__ __forceinline__ u32x2 load_b64(Rsrc r, uint32_t byte) { return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)byte, 0, kNT)); }
+
+// A lane's eight columns.  fp32 takes two accesses of 16 bytes.  Each of them covers whole cache lines if the lower half of the wavefront's lanes takes
+// first halves and the upper half second ones, of the lower half's columns and then of the upper half's; the halves then change places in
+// registers.  Rows that end inside a vector go the plain way, so that their last lane has its own elements (the same gradients: 119 us the plain way).
+struct LaneCols {
+    int col, n;           // n of the eight are there; 0 or less: none
+    uint32_t whole;       // columns in whole vectors
+    uint32_t at4, step4;  // fp32: byte of the first access, and from there to the second
+    __device__ __forceinline__ void set(int first, int64_t cols) {
+        const uint32_t lane = threadIdx.x % 64u;
+        col = first;
+        n = (int)min((int64_t)kVec, cols - first);
+        whole = (uint32_t)cols / kVec * kVec;
+        const bool ragged = whole != (uint32_t)cols;
+        at4 = ragged ? (uint32_t)col * 4u : ((uint32_t)col - lane * kVec) * 4u + lane % 32u * 32u + lane / 32u * 16u;
+        step4 = ragged ? 16u : 1024u;
+    }
+    __device__ __forceinline__ bool tail() const { return n > 0 && n < kVec; }
+};
+__device__ __forceinline__ void swap_halves(u32x4& a, u32x4& b) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const auto r = __builtin_amdgcn_permlane32_swap(a[i], b[i], false, false);
+        a[i] = r[0], b[i] = r[1];
+    }
+}
+// Row `row` of a matrix: load_row, and settle before the first look at it.
+__device__ __forceinline__ void load_whole(Raw<bf16>& x, Rsrc r, const LaneCols& l) { x.a = load_b128(r, (uint32_t)l.col * 2u); }
+__device__ __forceinline__ void load_whole(Raw<float>& x, Rsrc r, const LaneCols& l) {
+    x.a = load_b128(r, l.at4);
+    x.b = load_b128(r, l.at4 + l.step4);
+}
+template <class T> __device__ __forceinline__ void load_row(Raw<T>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
+    load_whole(x, row_buffer(m.data, row * m.stride * (int64_t)sizeof(T), there ? l.whole * (uint32_t)sizeof(T) : 0u), l);
+    if (l.whole != (uint32_t)cols && there && m.data && l.tail()) x.load((const char*)m.data + row * m.stride * (int64_t)sizeof(T), l.col, l.n);
+}
+__device__ __forceinline__ void settle(Raw<bf16>&, const LaneCols&, int64_t) {}
+__device__ __forceinline__ void settle(Raw<float>& x, const LaneCols& l, int64_t cols) {
+    if (l.whole == (uint32_t)cols) swap_halves(x.a, x.b);
+}
+template <class T> __device__ __forceinline__ void store_row(const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l, const float (&v)[kVec]) {
+    const Rsrc r = row_buffer(m.data, row * m.stride * (int64_t)sizeof(T), there ? l.whole * (uint32_t)sizeof(T) : 0u);
+    if constexpr (sizeof(T) == sizeof(float)) {
+        u32x4 w[2];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) w[i / 4][i % 4] = __builtin_bit_cast(uint32_t, v[i]);
+        if (l.whole == (uint32_t)cols) swap_halves(w[0], w[1]);
+        __builtin_amdgcn_raw_buffer_store_b128(w[0], r, (int)l.at4, 0, kNT);
+        __builtin_amdgcn_raw_buffer_store_b128(w[1], r, (int)(l.at4 + l.step4), 0, kNT);
+    } else {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = to_bf16x2(v[2 * i], v[2 * i + 1]);
+        __builtin_amdgcn_raw_buffer_store_b128(w, r, (int)((uint32_t)l.col * 2u), 0, kNT);
+    }
+    if (l.whole != (uint32_t)cols && there && m.data && l.tail()) store8<T>((char*)m.data + row * m.stride * (int64_t)sizeof(T), l.col, l.n, v);
+}
 
 // ---- the 8-bit form -----------------------------------------------------------------------------
 // The lanes of a quad (four neighbours from a multiple of four on) hold a block, eight elements each, those beyond the row's end zero.
@@ -205,7 +274,7 @@ __device__ __forceinline__ void decode8(u32x2 w, float m, int32_t format, float 
     }
 }
 __device__ __forceinline__ u32x2 load_q(const void* row, int col, int n) {
-    const char* p = (const char*)row + col;
+    const char* p = (const char*)row + (uint32_t)col;
     u32x2 w = {0u, 0u};
     if (n >= kVec) {
         w = *(const u32x2_any*)p;
@@ -217,7 +286,7 @@ __device__ __forceinline__ u32x2 load_q(const void* row, int col, int n) {
     return w;
 }
 __device__ __forceinline__ void store_q(void* row, int col, int n, u32x2 w) {
-    char* p = (char*)row + col;
+    char* p = (char*)row + (uint32_t)col;
     if (n >= kVec) {
         *(u32x2_any*)p = w;
     } else {
@@ -227,19 +296,43 @@ __device__ __forceinline__ void store_q(void* row, int col, int n, u32x2 w) {
     }
 }
 
+// A lane's eight bytes and its block's scale byte.
+struct Kept {
+    u32x2 q;
+    uint32_t s;
+    __device__ __forceinline__ void load(const apm_ckpt& c, int64_t row, int64_t cols, bool there, const LaneCols& l) {
+        const uint32_t blocks = ((uint32_t)cols + APM_CKPT_BLOCK - 1) / APM_CKPT_BLOCK;
+        q = load_b64(row_buffer(c.q, row * c.q_stride, there ? l.whole : 0u), (uint32_t)l.col);
+        s = __builtin_amdgcn_raw_buffer_load_b8(row_buffer(c.q ? c.scale : nullptr, row * c.scale_stride, there ? blocks : 0u), l.col / APM_CKPT_BLOCK, 0, 0);
+        if (l.whole != (uint32_t)cols && there && c.q && l.tail()) q = load_q((const char*)c.q + row * c.q_stride, l.col, l.n);
+    }
+    __device__ __forceinline__ void get(int32_t format, float (&v)[kVec]) const { decode8(q, scale_of(s, format), format, v); }
+};
+// Encodes and stores a lane's eight columns; quads of lanes hold a block.
+__device__ __forceinline__ void keep(const apm_ckpt& c, int64_t row, int64_t cols, bool there, const LaneCols& l, const float (&v)[kVec]) {
+    uint32_t s;
+    const u32x2 w = encode8(v, c.format, &s);
+    __builtin_amdgcn_raw_buffer_store_b64(w, row_buffer(c.q, row * c.q_stride, there ? l.whole : 0u), l.col, 0, kNT);
+    if (l.whole != (uint32_t)cols && there && l.tail()) store_q((char*)c.q + row * c.q_stride, l.col, l.n, w);
+    if (threadIdx.x % kQuad == 0 && there && l.n > 0) ((uint8_t*)c.scale)[row * c.scale_stride + (uint32_t)l.col / APM_CKPT_BLOCK] = (uint8_t)s;
+}
+
 // ---- sums over a wavefront ----------------------------------------------------------------------
-template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_add(float x) {
-    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
+template <int CTRL> __device__ __forceinline__ float dpp_add(float x) {
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
-__device__ __forceinline__ float wave_sum(float x) {  // the same in every lane
-    x = dpp_add<0x111, 0xf>(x);  // lane - 1, - 2, - 4, - 8 of 16: lane 15 has the row's
-    x = dpp_add<0x112, 0xf>(x);
-    x = dpp_add<0x114, 0xf>(x);
-    x = dpp_add<0x118, 0xf>(x);
-    x = dpp_add<0x142, 0xa>(x);  // rows 0 into 1, 2 into 3
-    x = dpp_add<0x143, 0xc>(x);  // row 1 into 2 and 3
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+__device__ __forceinline__ float row_sum16(float x) {  // of 16 lanes, the same in each: rotated by 8, 4, 2, 1
+    return dpp_add<0x121>(dpp_add<0x122>(dpp_add<0x124>(dpp_add<0x128>(x))));
 }
+// Rows 0 and 1, 2 and 3 of 16 lanes, or the halves, change places between two copies, whose sum then has both.  The copy is made in a
+// statement of its own: given one value twice, the compiler takes the first result for both.
+template <bool HALVES> __device__ __forceinline__ float swap_add(float x) {
+    uint32_t a = __builtin_bit_cast(uint32_t, x), b;
+    asm("v_mov_b32 %0, %1" : "=v"(b) : "v"(a));
+    const auto r = HALVES ? __builtin_amdgcn_permlane32_swap(a, b, false, false) : __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ __forceinline__ float wave_sum(float x) { return swap_add<true>(swap_add<false>(row_sum16(x))); }  // the same in every lane
 
 // ---- argument checks ----------------------------------------------------------------------------
 int check_matrix(const char* name, const apm_matrix& m, int64_t rows, int64_t cols, bool written);

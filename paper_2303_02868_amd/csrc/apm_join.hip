@@ -1,8 +1,9 @@
 // Where one block of a residual network ends and the next begins: y = scale x + gate post(branch), n = pre(y), with both
 // normalised tensors kept in 8 bits, and the gradients out of those.  HBM-bound in both directions (bf16: 10 B/element
 // and the scales, forward x, branch, y, n and two bytes, backward dy, dn, two bytes, dx, dbranch), so a row is read once
-// and stays in registers between its sums: 16 elements a lane, by one wavefront up to 1024 columns, else by as many as it takes.
+// and stays in registers between its sums, held by one wavefront or by as many as it takes.
 #include <algorithm>
+#include <type_traits>
 
 #include "apm_act.h"
 
@@ -10,172 +11,167 @@ namespace apm {
 namespace {
 
 constexpr int kWave = 64, kMaxWaves = 16, kMaxThreads = kWave * kMaxWaves;
-constexpr int kVecs = 2;                          // vectors of a lane
-constexpr int kWaveCols = kWave * kVec * kVecs;   // that one wavefront holds
-static_assert(kWaveCols * kMaxWaves == APM_JOIN_MAX_COLS, "a row fits the largest workgroup");
+constexpr int kFwdVecs = 2;  // vectors of a lane, forward
+static_assert(kMaxThreads * kVec * kFwdVecs == APM_JOIN_MAX_COLS, "a row fits the largest workgroup");
 
 struct JoinArgs {
     apm_norm_join j;
     float scale, eps_pre, eps_post, inv_cols;
 };
 
-// Sums over the lanes that hold a row: a wavefront, or `waves` consecutive ones of the workgroup from `first` on, whose sums go through
-// `slots` (of the whole workgroup's wavefronts, for this sum alone until the next barrier but one).
+// Sums over the lanes that hold a row.  With several wavefronts through `slots`: kMaxWaves floats for each sum, those of wavefronts that the row does
+// not have zero; they may be written again after the next barrier.
 template <bool WAVE, int N>
-__device__ __forceinline__ void row_sums(float (&x)[N], float* slots, int first, int waves) {
+__device__ __forceinline__ void team_sums(float (&x)[N], float* slots, int wave) {
 #pragma unroll
     for (int k = 0; k < N; ++k) x[k] = wave_sum(x[k]);
     if constexpr (!WAVE) {
         if (threadIdx.x % kWave == 0)
 #pragma unroll
-            for (int k = 0; k < N; ++k) slots[k * kMaxWaves + threadIdx.x / kWave] = x[k];
+            for (int k = 0; k < N; ++k) slots[k * kMaxWaves + wave] = x[k];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            float s = 0.0f;
-            for (int w = first; w < first + waves; ++w) s += slots[k * kMaxWaves + w];
-            x[k] = s;
-        }
+        for (int k = 0; k < N; ++k) x[k] = row_sum16(slots[k * kMaxWaves + threadIdx.x % kMaxWaves]);
     }
+}
+
+__device__ __forceinline__ void load_vector(const apm_vector& p, const LaneCols& l, float (&v)[kVec], float none) {
+    if (p.data) {
+        RawAny raw;
+        raw.load(p.data, p.dtype, l.col, l.n);
+        raw.get(p.dtype, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = none;
+    }
+}
+// A column's gate for all rows, or this row's
+__device__ __forceinline__ void load_gate(const apm_norm_join& j, int64_t row, int n, const LaneCols& l, float (&g)[kVec]) {
+    RawAny raw;
+    raw.load((const char*)j.gate.data + (j.gate_kind == APM_GATE_FULL ? row * j.gate.stride * (j.gate.dtype == APM_F32 ? 4 : 2) : 0), j.gate.dtype, l.col, n);
+    raw.get(j.gate.dtype, g);
 }
 
 // z becomes hat(z); elements beyond the row's end are zero before and after.
 template <bool WAVE>
-__device__ __forceinline__ float normalise(float (&z)[kVecs][kVec], const int (&n)[kVecs], int32_t kind, float eps, float inv_cols, float* slots, int waves) {
+__device__ __forceinline__ float normalise(float (&z)[kFwdVecs][kVec], const LaneCols (&l)[kFwdVecs], int32_t kind, float eps, float inv_cols, float* slots) {
     if (kind == APM_NORM_NONE) return 1.0f;
+    const int wave = (int)threadIdx.x / kWave;
     if (kind == APM_NORM_LAYER) {
         float s[1] = {0.0f};
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v)
+        for (int v = 0; v < kFwdVecs; ++v)
 #pragma unroll
             for (int i = 0; i < kVec; ++i) s[0] += z[v][i];
-        row_sums<WAVE>(s, slots, 0, waves);
+        team_sums<WAVE>(s, slots, wave);
         const float mean = s[0] * inv_cols;
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v)
+        for (int v = 0; v < kFwdVecs; ++v)
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) z[v][i] = i < n[v] ? z[v][i] - mean : 0.0f;
+            for (int i = 0; i < kVec; ++i) z[v][i] = i < l[v].n ? z[v][i] - mean : 0.0f;
     }
     float q[1] = {0.0f};
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v)
+    for (int v = 0; v < kFwdVecs; ++v)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) q[0] = fmaf(z[v][i], z[v][i], q[0]);
-    row_sums<WAVE>(q, slots + kMaxWaves, 0, waves);
+    team_sums<WAVE>(q, slots + kMaxWaves, wave);
     const float r = 1.0f / sqrtf(fmaf(q[0], inv_cols, eps));
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v)
+    for (int v = 0; v < kFwdVecs; ++v)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) z[v][i] *= r;
     return r;
 }
 
-__device__ __forceinline__ void keep(const apm_ckpt& c, int64_t row, int col, int n, const float (&z)[kVec]) {
-    uint32_t s;
-    const u32x2 w = encode8(z, c.format, &s);
-    store_q((char*)c.q + row * c.q_stride, col, n, w);
-    if (threadIdx.x % kQuad == 0 && n > 0) ((uint8_t*)c.scale)[row * c.scale_stride + col / APM_CKPT_BLOCK] = (uint8_t)s;
-}
-
-// weight and bias, where they are given
-__device__ __forceinline__ void affine(const apm_norm& norm, int col, int n, const float (&z)[kVec], float (&out)[kVec]) {
-    RawAny w, b;
-    if (norm.weight.data) w.load(norm.weight.data, norm.weight.dtype, col, n);
-    if (norm.bias.data) b.load(norm.bias.data, norm.bias.dtype, col, n);
+__device__ __forceinline__ void affine(const apm_norm& norm, const LaneCols& l, const float (&z)[kVec], float (&out)[kVec]) {
+    float w[kVec], b[kVec];
+    load_vector(norm.weight, l, w, 1.0f);
+    load_vector(norm.bias, l, b, 0.0f);
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) out[i] = z[i];
-    float p[kVec];
-    if (norm.weight.data) {
-        w.get(norm.weight.dtype, p);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) out[i] *= p[i];
-    }
-    if (norm.bias.data) {
-        b.get(norm.bias.dtype, p);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) out[i] += p[i];
-    }
-}
-
-__device__ __forceinline__ const char* row_of(const apm_matrix& m, int64_t row) {
-    return (const char*)m.data + row * m.stride * (m.dtype == APM_F32 ? 4 : 2);
+    for (int i = 0; i < kVec; ++i) out[i] = fmaf(z[i], w[i], b[i]);
 }
 
 constexpr int kRowsPerGroup = 4;  // of one wavefront each
 
+// One row a team: a wavefront up to 1024 columns, else as many as hold it with 16 columns a lane.
 template <class R, class A, bool WAVE>
 __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void apm_join_forward_kernel(JoinArgs a) {
     __shared__ float slots[WAVE ? 1 : 4 * kMaxWaves];
     const apm_norm_join& j = a.j;
-    const int lane = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x, lanes = WAVE ? kWave : (int)blockDim.x, waves = lanes / kWave;
+    const int lane = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x, lanes = WAVE ? kWave : (int)blockDim.x;
     int64_t row = blockIdx.x;
     if constexpr (WAVE) {
         row = row * kRowsPerGroup + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
         if (row >= j.rows) return;
     }
-    int col[kVecs], n[kVecs];
-    Raw<R> x[kVecs];
-    Raw<A> b[kVecs];
+    LaneCols l[kFwdVecs];
+    Raw<R> x[kFwdVecs];
+    Raw<A> b[kFwdVecs];
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v) {
-        col[v] = (v * lanes + lane) * kVec;
-        n[v] = (int)min((int64_t)kVec, j.cols - col[v]);
-        x[v].load((const char*)j.x.data + row * j.x.stride * (int64_t)sizeof(R), col[v], n[v]);
-        if (j.branch.data) b[v].load((const char*)j.branch.data + row * j.branch.stride * (int64_t)sizeof(A), col[v], n[v]);
+    for (int v = 0; v < kFwdVecs; ++v) {
+        l[v].set((v * lanes + lane) * kVec, j.cols);
+        load_row(x[v], j.x, row, j.cols, true, l[v]);
+        load_row(b[v], j.branch, row, j.cols, true, l[v]);
     }
-    float y[kVecs][kVec];
+    if constexpr (!WAVE) {
+        if (threadIdx.x < 4 * kMaxWaves) slots[threadIdx.x] = 0.0f;
+        __syncthreads();
+    }
+    float y[kFwdVecs][kVec];
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v)
+    for (int v = 0; v < kFwdVecs; ++v) {
+        settle(x[v], l[v], j.cols);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) y[v][i] = a.scale * x[v][i];
+    }
     if (j.branch.data) {
-        float z[kVecs][kVec];
+        float z[kFwdVecs][kVec];
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v)
+        for (int v = 0; v < kFwdVecs; ++v) {
+            settle(b[v], l[v], j.cols);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) z[v][i] = b[v][i];
-        const float r = normalise<WAVE>(z, n, j.post.kind, a.eps_post, a.inv_cols, slots, waves);
+        }
+        const float r = normalise<WAVE>(z, l, j.post.kind, a.eps_post, a.inv_cols, slots);
         if (j.post.rstd && lane == 0) j.post.rstd[row] = r;
         const float token = j.gate_kind == APM_GATE_TOKEN ? load1(j.gate.data, j.gate.dtype, row * j.gate.stride) : 1.0f;
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) {
-            if (j.post.ckpt.q) keep(j.post.ckpt, row, col[v], n[v], z[v]);
-            float c[kVec];
-            affine(j.post, col[v], n[v], z[v], c);
+        for (int v = 0; v < kFwdVecs; ++v) {
+            if (j.post.ckpt.q) keep(j.post.ckpt, row, j.cols, true, l[v], z[v]);
+            float c[kVec], g[kVec];
+            affine(j.post, l[v], z[v], c);
             if (j.gate_kind == APM_GATE_CHANNEL || j.gate_kind == APM_GATE_FULL) {
-                RawAny raw;
-                raw.load(j.gate_kind == APM_GATE_FULL ? row_of(j.gate, row) : (const char*)j.gate.data, j.gate.dtype, col[v], n[v]);
-                float g[kVec];
-                raw.get(j.gate.dtype, g);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) y[v][i] = fmaf(g[i], c[i], y[v][i]);
+                load_gate(j, row, l[v].n, l[v], g);
             } else {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) y[v][i] = fmaf(token, c[i], y[v][i]);
+                for (int i = 0; i < kVec; ++i) g[i] = token;
             }
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) y[v][i] = i < l[v].n ? fmaf(g[i], c[i], y[v][i]) : 0.0f;
         }
     }
     if (j.y.data) {
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) store8<R>((char*)j.y.data + row * j.y.stride * (int64_t)sizeof(R), col[v], n[v], y[v]);
+        for (int v = 0; v < kFwdVecs; ++v) store_row<R>(j.y, row, j.cols, true, l[v], y[v]);
     }
     if (!j.n.data && !j.pre.ckpt.q && !j.pre.rstd) return;
-    const float r = normalise<WAVE>(y, n, j.pre.kind, a.eps_pre, a.inv_cols, slots + 2 * kMaxWaves * (WAVE ? 0 : 1), waves);
+    const float r = normalise<WAVE>(y, l, j.pre.kind, a.eps_pre, a.inv_cols, slots + (WAVE ? 0 : 2 * kMaxWaves));
     if (j.pre.rstd && lane == 0) j.pre.rstd[row] = r;
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v) {
-        if (j.pre.ckpt.q) keep(j.pre.ckpt, row, col[v], n[v], y[v]);
+    for (int v = 0; v < kFwdVecs; ++v) {
+        if (j.pre.ckpt.q) keep(j.pre.ckpt, row, j.cols, true, l[v], y[v]);
         if (j.n.data) {
             float o[kVec];
-            affine(j.pre, col[v], n[v], y[v], o);
-            store8<A>((char*)j.n.data + row * j.n.stride * (int64_t)sizeof(A), col[v], n[v], o);
+            affine(j.pre, l[v], y[v], o);
+            store_row<A>(j.n, row, j.cols, true, l[v], o);
         }
     }
 }
 
 // ---- backward -----------------------------------------------------------------------------------
-// Sums over rows: every team of lanes (a wavefront, or the wavefronts that hold a row) adds its rows up in registers, a workgroup's teams are
-// added in LDS, the workgroups' sums in the workspace are added by a second kernel, all in one order.
+// Sums over rows: every thread adds up its columns of its team's rows in LDS, where nobody else touches them, the teams of a workgroup
+// are added at the end, and the workgroups' sums, which lie in the workspace, by a second kernel, all in one order.
 // Per column: dn hat1, dn, and D hat2, D (times the gate, unless it has one value for the column, which then enters at the end).
 enum { kDnHat, kDn, kDHat, kD, kSums };
 
@@ -208,182 +204,237 @@ template <class R, class A, int VECS>
 struct RowRaw {
     Raw<R> dy[VECS];
     Raw<A> dn[VECS];
-    u32x2 q1[VECS], q2[VECS];
-    uint32_t s1[VECS], s2[VECS];
-    float r1, r2, token;
-    __device__ __forceinline__ void load(const BackArgs& a, int64_t row, const int (&col)[VECS], const int (&count)[VECS]) {
+    Kept k1[VECS], k2[VECS];
+    uint32_t r1, r2, token;
+    __device__ __forceinline__ void load(const BackArgs& a, int64_t row, const LaneCols (&l)[VECS]) {
         const bool there = row < a.j.rows;
-        r1 = there && a.j.pre.kind != APM_NORM_NONE ? a.j.pre.rstd[row] : 1.0f;
-        r2 = there && a.j.post.kind != APM_NORM_NONE && a.j.post.rstd ? a.j.post.rstd[row] : 1.0f;
-        token = there && a.j.gate_kind == APM_GATE_TOKEN ? load1(a.j.gate.data, a.j.gate.dtype, row * a.j.gate.stride) : 1.0f;
+        r1 = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(row_buffer(a.j.pre.rstd, row * 4, there ? 4u : 0u), 0, 0, 0);
+        r2 = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(row_buffer(a.j.post.rstd, row * 4, there ? 4u : 0u), 0, 0, 0);
+        token = 0u;
+        if (a.j.gate_kind == APM_GATE_TOKEN && there) token = __builtin_bit_cast(uint32_t, load1(a.j.gate.data, a.j.gate.dtype, row * a.j.gate.stride));
 #pragma unroll
         for (int v = 0; v < VECS; ++v) {
-            const int n = there ? count[v] : 0;
-            dy[v].load((const char*)a.g.dy.data + row * a.g.dy.stride * (int64_t)sizeof(R), col[v], a.g.dy.data ? n : 0);
-            dn[v].load((const char*)a.g.dn.data + row * a.g.dn.stride * (int64_t)sizeof(A), col[v], a.g.dn.data ? n : 0);
-            const bool k1 = a.j.pre.ckpt.q && n > 0, k2 = a.j.post.ckpt.q && n > 0;
-            q1[v] = load_q((const char*)a.j.pre.ckpt.q + row * a.j.pre.ckpt.q_stride, col[v], k1 ? n : 0);
-            q2[v] = load_q((const char*)a.j.post.ckpt.q + row * a.j.post.ckpt.q_stride, col[v], k2 ? n : 0);
-            s1[v] = k1 ? ((const uint8_t*)a.j.pre.ckpt.scale)[row * a.j.pre.ckpt.scale_stride + col[v] / APM_CKPT_BLOCK] : 0u;
-            s2[v] = k2 ? ((const uint8_t*)a.j.post.ckpt.scale)[row * a.j.post.ckpt.scale_stride + col[v] / APM_CKPT_BLOCK] : 0u;
+            load_row(dy[v], a.g.dy, row, a.j.cols, there, l[v]);
+            load_row(dn[v], a.g.dn, row, a.j.cols, there, l[v]);
+            k1[v].load(a.j.pre.ckpt, row, a.j.cols, there, l[v]);
+            k2[v].load(a.j.post.ckpt, row, a.j.cols, there, l[v]);
         }
     }
 };
 
-__device__ __forceinline__ void load_vector(const apm_vector& p, int col, int n, float (&v)[kVec], float none) {
-    if (p.data) {
-        RawAny raw;
-        raw.load(p.data, p.dtype, col, n);
-        raw.get(p.dtype, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = none;
-    }
-}
-
-template <class R, class A, int VECS, bool WAVE, bool BIAS>
+// COLUMN: the gate has one value for a column, or there is none: it then enters with the norm's weight, and at the end.
+// VECS 1: a lane has eight columns, and while a row is worked on the next one's loads are under way, so that the lanes of a CU's 16 wavefronts have two
+// rows' worth of loads out.  VECS 2, for rows that 16 wavefronts do not hold otherwise: no registers for either.
+// 8192 x 5120 with a fp32 stream: 108.6 us = 5.4 TB/s; of that 5 for the second kernel.
+constexpr int kSlotSums = 5;  // two for the first norm, three for the second and the gate
+template <class R, class A, int VECS, bool WAVE, bool BIAS, bool COLUMN>
 __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs a) {
-    extern __shared__ float lds[];  // 2 x 5 sums of every wavefront while rows are walked, then the teams' sums
+    // The teams' slots, twice; then the sums, four at a time of a thread's.
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    constexpr bool kAhead = VECS == 1;
+    constexpr int kAccs = BIAS ? 4 : 2, kInLds = VECS == 1 ? kAccs : 2;
     const apm_norm_join& j = a.j;
+    const int threads = (int)blockDim.x, slots_size = WAVE ? 0 : 2 * a.teams * kSlotSums * kMaxWaves;
+    f32x4* const sums = (f32x4*)(lds + slots_size) + threadIdx.x;  // [sum][vector][half][thread]
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const int waves = WAVE ? 1 : a.waves, team = wave / waves, first = team * waves;
-    const int lanes = waves * kWave, lane = (int)threadIdx.x - first * kWave;
-    int col[VECS], n[VECS];
+    const int waves = WAVE ? 1 : a.waves, team = WAVE ? wave : wave / waves, in_team = wave - team * waves;
+    const int lanes = waves * kWave, lane = in_team * kWave + (int)threadIdx.x % kWave;
+    LaneCols l[VECS];
 #pragma unroll
-    for (int v = 0; v < VECS; ++v) {
-        col[v] = (v * lanes + lane) * kVec;
-        n[v] = (int)min((int64_t)kVec, j.cols - col[v]);
+    for (int v = 0; v < VECS; ++v) l[v].set((v * lanes + lane) * kVec, j.cols);
+    auto first_weight = [&](int v, float (&w)[kVec]) { load_vector(j.pre.weight, l[v], w, 1.0f); };
+    auto second_weight = [&](int v, float (&w)[kVec]) {
+        load_vector(j.post.weight, l[v], w, 1.0f);
+        if (COLUMN && j.gate_kind == APM_GATE_CHANNEL) {
+            float g[kVec];
+            load_gate(j, 0, l[v].n, l[v], g);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) w[i] *= g[i];
+        }
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) w[i] = i < l[v].n ? w[i] : 0.0f;  // what is no column adds nothing to the second norm's sums
+    };
+    float w1[VECS][kVec], w2[VECS][kVec];
+    if constexpr (kAhead) first_weight(0, w1[0]), second_weight(0, w2[0]);
+    if constexpr (!WAVE) {
+        for (int i = (int)threadIdx.x; i < slots_size; i += threads) lds[i] = 0.0f;
+        __syncthreads();
     }
-    float acc[BIAS ? 4 : 2][VECS][kVec];
 #pragma unroll
-    for (int k = 0; k < (BIAS ? 4 : 2); ++k)
+    for (int k = 0; k < kInLds * VECS * 2; ++k) sums[k * threads] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float more[kAccs > kInLds ? kAccs - kInLds : 1][VECS][kVec] = {};  // where LDS does not hold all
+    auto add = [&](int k, int v, const float (&x)[kVec], const float (&y)[kVec]) {  // sum k += x y
+        if (k < kInLds) {
 #pragma unroll
-        for (int v = 0; v < VECS; ++v)
+            for (int h = 0; h < 2; ++h) {
+                f32x4 s = sums[((k * VECS + v) * 2 + h) * threads];
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) acc[k][v][i] = 0.0f;
-    const bool pre = a.g.dn.data != nullptr;
+                for (int i = 0; i < 4; ++i) s[i] = fmaf(x[4 * h + i], y[4 * h + i], s[i]);
+                sums[((k * VECS + v) * 2 + h) * threads] = s;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) more[k < kInLds ? 0 : k - kInLds][v][i] = fmaf(x[i], y[i], more[k < kInLds ? 0 : k - kInLds][v][i]);
+        }
+    };
+    float ones[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) ones[i] = 1.0f;
+    const bool through1 = j.pre.kind != APM_NORM_NONE, through2 = a.g.dbranch.data && j.post.kind != APM_NORM_NONE;
+    const bool mean1 = j.pre.kind == APM_NORM_LAYER, mean2 = through2 && j.post.kind == APM_NORM_LAYER;
     const int64_t step = (int64_t)gridDim.x * a.teams;
-    int64_t row = (int64_t)blockIdx.x * a.teams + team;
     const int64_t begin = (int64_t)blockIdx.x * a.teams;  // the workgroup's first row: all its wavefronts walk as often
+    int64_t row = begin + team;
     RowRaw<R, A, VECS> next;
-    next.load(a, row, col, n);
+    if constexpr (kAhead) next.load(a, row, l);
     int turn = 0;
     for (int64_t at = begin; at < j.rows; at += step, row += step, turn ^= 1) {
-        const RowRaw<R, A, VECS> cur = next;
+        if constexpr (!kAhead) next.load(a, row, l);
+        RowRaw<R, A, VECS> cur = next;
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) settle(cur.dy[v], l[v], j.cols), settle(cur.dn[v], l[v], j.cols);
         const bool there = row < j.rows;
-        if (at + step < j.rows) next.load(a, row + step, col, n);
-        float* slots = lds + turn * 5 * kMaxWaves;
+        const float r1 = through1 ? __builtin_bit_cast(float, cur.r1) : 1.0f, r2 = through2 ? __builtin_bit_cast(float, cur.r2) : 1.0f;
+        const float token = j.gate_kind == APM_GATE_TOKEN ? __builtin_bit_cast(float, cur.token) : 1.0f;
+        if constexpr (kAhead) next.load(a, row + step, l);
+        float* slots = lds + (turn * a.teams + team) * kSlotSums * kMaxWaves;
         float D[VECS][kVec];
         {
-            float z[VECS][kVec], t[VECS][kVec], s[2] = {0.0f, 0.0f};
+            float z[VECS][kVec], s[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int v = 0; v < VECS; ++v) {
-                decode8(cur.q1[v], scale_of(cur.s1[v], j.pre.ckpt.format), j.pre.ckpt.format, z[v]);
-                float w[kVec];
-                load_vector(j.pre.weight, col[v], n[v], w, 1.0f);
+                cur.k1[v].get(j.pre.ckpt.format, z[v]);
+                if constexpr (!kAhead) first_weight(v, w1[v]);
+                float dn[kVec];
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
-                    const float dn = cur.dn[v][i];
-                    t[v][i] = dn * w[i];
-                    s[0] = fmaf(t[v][i], z[v][i], s[0]);
-                    s[1] += t[v][i];
-                    acc[0][v][i] = fmaf(dn, z[v][i], acc[0][v][i]);
-                    if constexpr (BIAS) acc[2][v][i] += dn;
+                    dn[i] = cur.dn[v][i];
+                    D[v][i] = dn[i] * w1[v][i];
+                    s[0] = fmaf(D[v][i], z[v][i], s[0]);
                 }
+                add(0, v, dn, z[v]);
+                if constexpr (BIAS) add(2, v, dn, ones);
             }
-            if (pre && j.pre.kind != APM_NORM_NONE) {
-                row_sums<WAVE>(s, slots, first, waves);
-                const float k = s[0] * a.inv_cols, m = j.pre.kind == APM_NORM_LAYER ? s[1] * a.inv_cols : 0.0f;
+            if (through1) {
+                if (mean1) {
+#pragma unroll
+                    for (int v = 0; v < VECS; ++v)
+#pragma unroll
+                        for (int i = 0; i < kVec; ++i) s[1] += D[v][i];
+                    team_sums<WAVE>(s, slots, in_team);
+                } else {
+                    float one[1] = {s[0]};
+                    team_sums<WAVE>(one, slots, in_team);
+                    s[0] = one[0];
+                }
+                const float k = s[0] * a.inv_cols, m = s[1] * a.inv_cols;
 #pragma unroll
                 for (int v = 0; v < VECS; ++v)
 #pragma unroll
-                    for (int i = 0; i < kVec; ++i) t[v][i] = cur.r1 * (t[v][i] - fmaf(z[v][i], k, m));
+                    for (int i = 0; i < kVec; ++i) D[v][i] = r1 * (D[v][i] - fmaf(z[v][i], k, m));
             }
+        }
 #pragma unroll
-            for (int v = 0; v < VECS; ++v) {
-                const int count = there ? n[v] : 0;
-                float o[kVec];
+        for (int v = 0; v < VECS; ++v) {
+            float o[kVec];
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    D[v][i] = i < count ? cur.dy[v][i] + t[v][i] : 0.0f;
-                    o[i] = a.scale * D[v][i];
-                }
-                if (a.g.dx.data) store8<R>((char*)a.g.dx.data + row * a.g.dx.stride * (int64_t)sizeof(R), col[v], count, o);
+            for (int i = 0; i < kVec; ++i) {
+                D[v][i] += cur.dy[v][i];
+                o[i] = a.scale * D[v][i];
             }
+            store_row<R>(a.g.dx, row, j.cols, there, l[v], o);
         }
         {
             float z[VECS][kVec], s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int v = 0; v < VECS; ++v) {
-                const int count = there ? n[v] : 0;
-                decode8(cur.q2[v], scale_of(cur.s2[v], j.post.ckpt.format), j.post.ckpt.format, z[v]);
-                float w[kVec], g[kVec];
-                load_vector(j.post.weight, col[v], n[v], w, 1.0f);
-                if (j.gate_kind == APM_GATE_TOKEN || (j.gate_kind == APM_GATE_FULL && a.g.dgate.data)) {
-                    float b[kVec], o[kVec];
-                    load_vector(j.post.bias, col[v], n[v], b, 0.0f);
+                cur.k2[v].get(j.post.ckpt.format, z[v]);
+                if constexpr (!kAhead) second_weight(v, w2[v]);
+                if constexpr (!COLUMN) {
+                    const int count = there ? l[v].n : 0;
+                    if (a.g.dgate.data) {
+                        float b[kVec], o[kVec];
+                        load_vector(j.post.bias, l[v], b, 0.0f);
 #pragma unroll
-                    for (int i = 0; i < kVec; ++i) {
-                        o[i] = D[v][i] * fmaf(z[v][i], w[i], b[i]);
-                        s[2] += i < count ? o[i] : 0.0f;
+                        for (int i = 0; i < kVec; ++i) {
+                            o[i] = D[v][i] * fmaf(z[v][i], w2[v][i], i < count ? b[i] : 0.0f);
+                            s[2] += o[i];
+                        }
+                        if (j.gate_kind == APM_GATE_FULL) {
+                            char* p = (char*)a.g.dgate.data + row * a.g.dgate.stride * (a.g.dgate.dtype == APM_F32 ? 4 : 2);
+                            if (a.g.dgate.dtype == APM_F32) store8<float>(p, l[v].col, count, o);
+                            else store8<bf16>(p, l[v].col, count, o);
+                        }
                     }
+                    float g[kVec];
                     if (j.gate_kind == APM_GATE_FULL) {
-                        char* p = (char*)a.g.dgate.data + row * a.g.dgate.stride * (a.g.dgate.dtype == APM_F32 ? 4 : 2);
-                        if (a.g.dgate.dtype == APM_F32) store8<float>(p, col[v], count, o);
-                        else store8<bf16>(p, col[v], count, o);
-                    }
-                }
+                        load_gate(j, row, count, l[v], g);
+                    } else {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) g[i] = cur.token;
-                if (j.gate_kind == APM_GATE_CHANNEL || j.gate_kind == APM_GATE_FULL) {
-                    RawAny raw;
-                    raw.load(j.gate_kind == APM_GATE_FULL ? row_of(j.gate, row) : (const char*)j.gate.data, j.gate.dtype, col[v], count);
-                    raw.get(j.gate.dtype, g);
+                        for (int i = 0; i < kVec; ++i) g[i] = token;
+                    }
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) D[v][i] *= g[i];
                 }
+                add(1, v, D[v], z[v]);
+                if constexpr (BIAS) add(3, v, D[v], ones);
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
-                    const float dc = D[v][i] * g[i], summed = j.gate_kind == APM_GATE_CHANNEL ? D[v][i] : dc;
-                    acc[1][v][i] = fmaf(summed, z[v][i], acc[1][v][i]);
-                    if constexpr (BIAS) acc[3][v][i] += summed;
-                    D[v][i] = dc * w[i];
+                    D[v][i] *= w2[v][i];
                     s[0] = fmaf(D[v][i], z[v][i], s[0]);
-                    s[1] += D[v][i];
+                }
+                if (mean2) {
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) s[1] += D[v][i];
                 }
             }
-            const bool through = a.g.dbranch.data && j.post.kind != APM_NORM_NONE;
-            if (through || j.gate_kind == APM_GATE_TOKEN) {
-                row_sums<WAVE>(s, slots + 2 * kMaxWaves, first, waves);
-                if (j.gate_kind == APM_GATE_TOKEN && a.g.dgate.data && lane == 0 && there) store1(a.g.dgate.data, a.g.dgate.dtype, row * a.g.dgate.stride, s[2]);
+            if (!COLUMN || mean2) {
+                team_sums<WAVE>(s, slots + 2 * kMaxWaves, in_team);
+                if (!COLUMN && j.gate_kind == APM_GATE_TOKEN && a.g.dgate.data && lane == 0 && there)
+                    store1(a.g.dgate.data, a.g.dgate.dtype, row * a.g.dgate.stride, s[2]);
+            } else if (through2) {
+                float one[1] = {s[0]};
+                team_sums<WAVE>(one, slots + 2 * kMaxWaves, in_team);
+                s[0] = one[0];
             }
-            if (a.g.dbranch.data) {
-                const float k = s[0] * a.inv_cols, m = j.post.kind == APM_NORM_LAYER ? s[1] * a.inv_cols : 0.0f;
+            // without a norm r2 = 1, and k = m = 0
+            const float k = through2 ? s[0] * a.inv_cols : 0.0f, m = mean2 ? s[1] * a.inv_cols : 0.0f;
 #pragma unroll
-                for (int v = 0; v < VECS; ++v) {
-                    float o[kVec];
+            for (int v = 0; v < VECS; ++v) {
+                float o[kVec];
 #pragma unroll
-                    for (int i = 0; i < kVec; ++i) o[i] = through ? cur.r2 * (D[v][i] - fmaf(z[v][i], k, m)) : D[v][i];
-                    store8<A>((char*)a.g.dbranch.data + row * a.g.dbranch.stride * (int64_t)sizeof(A), col[v], there ? n[v] : 0, o);
-                }
+                for (int i = 0; i < kVec; ++i) o[i] = r2 * (D[v][i] - fmaf(z[v][i], k, m));
+                store_row<A>(a.g.dbranch, row, j.cols, there, l[v], o);
             }
         }
     }
-    // The teams' sums.  The lane's 16 columns lie in LDS as in a row.
-    const int64_t cap = (int64_t)lanes * kVec * VECS;
+    // The teams' sums of a column, which is element c mod 8 of vector c / 8 of the row.
     float* mine = a.part + (int64_t)blockIdx.x * kSums * j.cols;
-#pragma unroll
-    for (int k = 0; k < (BIAS ? 4 : 2); ++k) {
-        __syncthreads();
-#pragma unroll
-        for (int v = 0; v < VECS; ++v)
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) lds[team * cap + col[v] + i] = acc[k][v][i];
-        __syncthreads();
+    auto store_sums = [&](int k, int at) {
         const int sum = k == 0 ? kDnHat : k == 1 ? kDHat : k == 2 ? kDn : kD;
-        for (int64_t c = threadIdx.x; c < j.cols; c += blockDim.x) {
+        for (int c = (int)threadIdx.x; c < (int)j.cols; c += threads) {
+            const int vec = c / kVec, v = VECS == 1 ? 0 : vec / lanes, i = c % kVec;
+            const float* p = lds + slots_size + ((((at * VECS + v) * 2 + i / 4) * threads) + vec - v * lanes) * 4 + i % 4;
             float s = 0.0f;
-            for (int m = 0; m < a.teams; ++m) s += lds[m * cap + c];
+            for (int m = 0; m < a.teams; ++m) s += p[m * lanes * 4];
             mine[sum * j.cols + c] = s;
         }
+    };
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kInLds; ++k) store_sums(k, k);
+    if constexpr (kAccs > kInLds) {
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kAccs - kInLds; ++k)
+#pragma unroll
+            for (int v = 0; v < VECS; ++v)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) sums[((k * VECS + v) * 2 + h) * threads] = f32x4{more[k][v][4 * h], more[k][v][4 * h + 1], more[k][v][4 * h + 2], more[k][v][4 * h + 3]};
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kAccs - kInLds; ++k) store_sums(kInLds + k, k);
     }
     if (gridDim.x == 1) {
         for (int64_t c = threadIdx.x; c < j.cols; c += blockDim.x) {  // what this thread itself wrote
@@ -394,22 +445,34 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
     }
 }
 
-// The workgroups' sums of 32 columns: 32 lanes side by side, as many parts at a time.
+// The workgroups' sums of 32 columns: 32 lanes side by side, 32 parts at a time, eight of them under way.
 constexpr int kSide = 32;
 template <bool BIAS>
 __global__ __launch_bounds__(kSide * kSide) void apm_join_sums_kernel(apm_norm_join j, apm_norm_join_grads g, const float* part, int32_t parts) {
     __shared__ float lds[kSide][kSide + 1];
     const int x = (int)threadIdx.x % kSide, y = (int)threadIdx.x / kSide;
     const int64_t c = (int64_t)blockIdx.x * kSide + x;
-    float s[kSums] = {};
+    float t[kSums] = {}, s[kSums] = {};
+    if (c < j.cols) {
+        for (int32_t p = y; p < parts; p += 8 * kSide) {
+            float v[kSums][8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int k = 0; k < kSums; ++k)
+                    if (BIAS || k == kDnHat || k == kDHat) v[k][i] = p + i * kSide < parts ? part[((int64_t)(p + i * kSide) * kSums + k) * j.cols + c] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int k = 0; k < kSums; ++k)
+                    if (BIAS || k == kDnHat || k == kDHat) t[k] += v[k][i];
+        }
+    }
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
         if (!BIAS && (k == kDn || k == kD)) continue;
-        float t = 0.0f;
-        if (c < j.cols)
-            for (int32_t p = y; p < parts; p += kSide) t += part[((int64_t)p * kSums + k) * j.cols + c];
         __syncthreads();
-        lds[y][x] = t;
+        lds[y][x] = t[k];
         __syncthreads();
         if (y == 0)
             for (int i = 0; i < kSide; ++i) s[k] += lds[i][x];
@@ -446,7 +509,7 @@ int check_types(const apm_matrix& res, const apm_matrix& act) {
     return APM_OK;
 }
 
-int waves_of(int64_t cols) { return (int)div_up(cols, kWaveCols); }
+int waves_of(int64_t cols) { return (int)div_up(cols, kWave * kVec * kFwdVecs); }
 
 // Calls go(R(), A()) with the element types.
 template <class F>
@@ -491,8 +554,9 @@ int forward(const apm_norm_join* jp, void* stream) {
     return APM_OK;
 }
 
-// How many workgroups walk the rows, and with how many teams: one workgroup a CU.
-constexpr int64_t kGroups = 256;
+// How many workgroups walk the rows, and with how many teams: one workgroup a CU, of as many teams as 16 wavefronts make, so that there are few
+// sums of workgroups to add (16384 x 768, us: 50 with 16 wavefronts, 55 with workgroups of 4, of which four share a CU).
+constexpr int64_t kCus = 256;
 struct BackShape {
     int vecs, waves, teams;
     int64_t groups;
@@ -502,7 +566,8 @@ BackShape back_shape(int64_t rows, int64_t cols) {
     b.vecs = cols <= (int64_t)kMaxThreads * kVec ? 1 : 2;
     b.waves = (int)div_up(cols, kWave * kVec * b.vecs);
     b.teams = kMaxWaves / b.waves;
-    b.groups = std::max<int64_t>(1, std::min(kGroups, div_up(rows, b.teams)));
+    // Few rows: one workgroup, and no second kernel.
+    b.groups = rows <= 2 * b.teams ? 1 : std::min(kCus, div_up(rows, b.teams));
     return b;
 }
 
@@ -550,14 +615,21 @@ int backward(const apm_norm_join* jp, const apm_norm_join_grads* gp, void* works
     const bool sums = bias || g.dpre_weight.data || g.dpost_weight.data || (g.dgate.data && j.gate_kind == APM_GATE_CHANNEL);
     const hipStream_t s = (hipStream_t)stream;
     const dim3 grid((unsigned)b.groups), block((unsigned)(b.teams * b.waves * kWave));
-    const size_t shared = std::max<size_t>((size_t)block.x * kVec * b.vecs, 2 * 5 * kMaxWaves) * sizeof(float);
+    const size_t shared = ((size_t)block.x * kVec * b.vecs * (b.vecs == 1 && bias ? 4 : 2) + (b.waves > 1 ? (size_t)2 * b.teams * kSlotSums * kMaxWaves : 0)) * sizeof(float);
     with_types(res.data ? res.dtype : act.data ? act.dtype : APM_BF16, act.data ? act.dtype : APM_BF16, [&](auto r, auto t) {
         using R = decltype(r);
         using A = decltype(t);
         auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, shared, s, a); };
-        if (b.waves == 1) bias ? start(apm_join_backward_kernel<R, A, 1, true, true>) : start(apm_join_backward_kernel<R, A, 1, true, false>);
-        else if (b.vecs == 1) bias ? start(apm_join_backward_kernel<R, A, 1, false, true>) : start(apm_join_backward_kernel<R, A, 1, false, false>);
-        else bias ? start(apm_join_backward_kernel<R, A, 2, false, true>) : start(apm_join_backward_kernel<R, A, 2, false, false>);
+        const bool column = j.gate_kind == APM_GATE_NONE || j.gate_kind == APM_GATE_CHANNEL;
+        auto with = [&](auto vecs, auto wave) {
+            constexpr int V = decltype(vecs)::value;
+            constexpr bool W = decltype(wave)::value;
+            if (column) bias ? start(apm_join_backward_kernel<R, A, V, W, true, true>) : start(apm_join_backward_kernel<R, A, V, W, false, true>);
+            else bias ? start(apm_join_backward_kernel<R, A, V, W, true, false>) : start(apm_join_backward_kernel<R, A, V, W, false, false>);
+        };
+        if (b.waves == 1) with(std::integral_constant<int, 1>(), std::true_type());
+        else if (b.vecs == 1) with(std::integral_constant<int, 1>(), std::false_type());
+        else with(std::integral_constant<int, 2>(), std::false_type());
     });
     APM_HIP(hipGetLastError());
     if (b.groups > 1 && sums) {
