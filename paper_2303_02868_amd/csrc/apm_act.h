@@ -12,6 +12,15 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 __attribute__((aligned(1))) u32x4_any;
 typedef u32x2 __attribute__((aligned(1))) u32x2_any;
 
+template <bool NT, class V> __device__ __forceinline__ V load_at(const V* p) {
+    if constexpr (NT) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool NT, class V> __device__ __forceinline__ void store_at(V v, V* p) {
+    if constexpr (NT) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
 constexpr int kVec = 8;                          // elements a lane takes at a time: 16 bytes of bf16
 constexpr int kQuad = APM_CKPT_BLOCK / kVec;     // neighbouring lanes that hold a block of the 8-bit form
 static_assert(kQuad == 4, "a block is a quad of lanes");
@@ -33,11 +42,11 @@ __device__ __forceinline__ uint16_t to_bf16(float a) { return __builtin_bit_cast
 template <class T> struct Raw;
 template <> struct Raw<bf16> {
     u32x4 a;
-    __device__ __forceinline__ void load(const void* row, int col, int n) {
+    template <bool NT = false> __device__ __forceinline__ void load(const void* row, int col, int n) {
         const char* p = (const char*)row + (uint32_t)col * 2u;
         a = u32x4{0, 0, 0, 0};
         if (n >= kVec) {
-            a = *(const u32x4_any*)p;
+            a = load_at<NT>((const u32x4_any*)p);
         } else {
 #pragma unroll
             for (int i = 0; i < kVec; ++i)
@@ -48,12 +57,12 @@ template <> struct Raw<bf16> {
 };
 template <> struct Raw<float> {
     u32x4 a, b;
-    __device__ __forceinline__ void load(const void* row, int col, int n) {
+    template <bool NT = false> __device__ __forceinline__ void load(const void* row, int col, int n) {
         const char* p = (const char*)row + (uint32_t)col * 4u;
         a = b = u32x4{0, 0, 0, 0};
         if (n >= kVec) {
-            a = ((const u32x4_any*)p)[0];
-            b = ((const u32x4_any*)p)[1];
+            a = load_at<NT>((const u32x4_any*)p);
+            b = load_at<NT>((const u32x4_any*)p + 1);
         } else {
 #pragma unroll
             for (int i = 0; i < kVec; ++i)
@@ -65,7 +74,7 @@ template <> struct Raw<float> {
     }
     __device__ __forceinline__ float operator[](int i) const { return __builtin_bit_cast(float, i < 4 ? a[i & 3] : b[i & 3]); }
 };
-template <class T> __device__ __forceinline__ void store8(void* row, int col, int n, const float (&v)[kVec]) {
+template <class T, bool NT = false> __device__ __forceinline__ void store8(void* row, int col, int n, const float (&v)[kVec]) {
     char* p = (char*)row + (uint32_t)col * (uint32_t)sizeof(T);
     if constexpr (sizeof(T) == sizeof(float)) {
         if (n >= kVec) {
@@ -74,7 +83,7 @@ template <class T> __device__ __forceinline__ void store8(void* row, int col, in
                 u32x4 w;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, v[4 * h + i]);
-                ((u32x4_any*)p)[h] = w;
+                store_at<NT, u32x4_any>(w, (u32x4_any*)p + h);
             }
         } else {
 #pragma unroll
@@ -86,7 +95,7 @@ template <class T> __device__ __forceinline__ void store8(void* row, int col, in
             u32x4 w;
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = to_bf16x2(v[2 * i], v[2 * i + 1]);
-            *(u32x4_any*)p = w;
+            store_at<NT, u32x4_any>(w, (u32x4_any*)p);
         } else {
 #pragma unroll
             for (int i = 0; i < kVec; ++i)
@@ -273,11 +282,11 @@ __device__ __forceinline__ void decode8(u32x2 w, float m, int32_t format, float 
         }
     }
 }
-__device__ __forceinline__ u32x2 load_q(const void* row, int col, int n) {
+template <bool NT = false> __device__ __forceinline__ u32x2 load_q(const void* row, int col, int n) {
     const char* p = (const char*)row + (uint32_t)col;
     u32x2 w = {0u, 0u};
     if (n >= kVec) {
-        w = *(const u32x2_any*)p;
+        w = load_at<NT>((const u32x2_any*)p);
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
@@ -285,10 +294,10 @@ __device__ __forceinline__ u32x2 load_q(const void* row, int col, int n) {
     }
     return w;
 }
-__device__ __forceinline__ void store_q(void* row, int col, int n, u32x2 w) {
+template <bool NT = false> __device__ __forceinline__ void store_q(void* row, int col, int n, u32x2 w) {
     char* p = (char*)row + (uint32_t)col;
     if (n >= kVec) {
-        *(u32x2_any*)p = w;
+        store_at<NT, u32x2_any>(w, (u32x2_any*)p);
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)

@@ -11,8 +11,7 @@ namespace apm {
 namespace {
 
 constexpr int kWave = 64, kMaxWaves = 16, kMaxThreads = kWave * kMaxWaves;
-constexpr int kFwdVecs = 2;  // vectors of a lane, forward
-static_assert(kMaxThreads * kVec * kFwdVecs == APM_JOIN_MAX_COLS, "a row fits the largest workgroup");
+static_assert(kMaxThreads * kVec * 2 == APM_JOIN_MAX_COLS, "a row fits the largest workgroup with two vectors a lane");
 
 struct JoinArgs {
     apm_norm_join j;
@@ -53,32 +52,32 @@ __device__ __forceinline__ void load_gate(const apm_norm_join& j, int64_t row, i
 }
 
 // z becomes hat(z); elements beyond the row's end are zero before and after.
-template <bool WAVE>
-__device__ __forceinline__ float normalise(float (&z)[kFwdVecs][kVec], const LaneCols (&l)[kFwdVecs], int32_t kind, float eps, float inv_cols, float* slots) {
+template <bool WAVE, int VECS>
+__device__ __forceinline__ float normalise(float (&z)[VECS][kVec], const LaneCols (&l)[VECS], int32_t kind, float eps, float inv_cols, float* slots) {
     if (kind == APM_NORM_NONE) return 1.0f;
     const int wave = (int)threadIdx.x / kWave;
     if (kind == APM_NORM_LAYER) {
         float s[1] = {0.0f};
 #pragma unroll
-        for (int v = 0; v < kFwdVecs; ++v)
+        for (int v = 0; v < VECS; ++v)
 #pragma unroll
             for (int i = 0; i < kVec; ++i) s[0] += z[v][i];
         team_sums<WAVE>(s, slots, wave);
         const float mean = s[0] * inv_cols;
 #pragma unroll
-        for (int v = 0; v < kFwdVecs; ++v)
+        for (int v = 0; v < VECS; ++v)
 #pragma unroll
             for (int i = 0; i < kVec; ++i) z[v][i] = i < l[v].n ? z[v][i] - mean : 0.0f;
     }
     float q[1] = {0.0f};
 #pragma unroll
-    for (int v = 0; v < kFwdVecs; ++v)
+    for (int v = 0; v < VECS; ++v)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) q[0] = fmaf(z[v][i], z[v][i], q[0]);
     team_sums<WAVE>(q, slots + kMaxWaves, wave);
     const float r = 1.0f / sqrtf(fmaf(q[0], inv_cols, eps));
 #pragma unroll
-    for (int v = 0; v < kFwdVecs; ++v)
+    for (int v = 0; v < VECS; ++v)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) z[v][i] *= r;
     return r;
@@ -94,8 +93,9 @@ __device__ __forceinline__ void affine(const apm_norm& norm, const LaneCols& l, 
 
 constexpr int kRowsPerGroup = 4;  // of one wavefront each
 
-// One row a team: a wavefront up to 1024 columns, else as many as hold it with 16 columns a lane.
-template <class R, class A, bool WAVE>
+// One row a team: a wavefront up to 512 columns, else as many as hold it with eight columns a lane, or from 8192 columns on with 16 (16 all along, us: 8192 x
+// 5120 with a fp32 stream 131, with eight 111; 8192 x 2048 37 and 34; 8 x 768 6.9 and 4.7).  5.3 TB/s at 8192 x 5120, 5.0 at 8192 x 2048.
+template <class R, class A, int VECS, bool WAVE>
 __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void apm_join_forward_kernel(JoinArgs a) {
     __shared__ float slots[WAVE ? 1 : 4 * kMaxWaves];
     const apm_norm_join& j = a.j;
@@ -105,11 +105,11 @@ __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void ap
         row = row * kRowsPerGroup + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
         if (row >= j.rows) return;
     }
-    LaneCols l[kFwdVecs];
-    Raw<R> x[kFwdVecs];
-    Raw<A> b[kFwdVecs];
+    LaneCols l[VECS];
+    Raw<R> x[VECS];
+    Raw<A> b[VECS];
 #pragma unroll
-    for (int v = 0; v < kFwdVecs; ++v) {
+    for (int v = 0; v < VECS; ++v) {
         l[v].set((v * lanes + lane) * kVec, j.cols);
         load_row(x[v], j.x, row, j.cols, true, l[v]);
         load_row(b[v], j.branch, row, j.cols, true, l[v]);
@@ -118,17 +118,17 @@ __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void ap
         if (threadIdx.x < 4 * kMaxWaves) slots[threadIdx.x] = 0.0f;
         __syncthreads();
     }
-    float y[kFwdVecs][kVec];
+    float y[VECS][kVec];
 #pragma unroll
-    for (int v = 0; v < kFwdVecs; ++v) {
+    for (int v = 0; v < VECS; ++v) {
         settle(x[v], l[v], j.cols);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) y[v][i] = a.scale * x[v][i];
     }
     if (j.branch.data) {
-        float z[kFwdVecs][kVec];
+        float z[VECS][kVec];
 #pragma unroll
-        for (int v = 0; v < kFwdVecs; ++v) {
+        for (int v = 0; v < VECS; ++v) {
             settle(b[v], l[v], j.cols);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) z[v][i] = b[v][i];
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void ap
         if (j.post.rstd && lane == 0) j.post.rstd[row] = r;
         const float token = j.gate_kind == APM_GATE_TOKEN ? load1(j.gate.data, j.gate.dtype, row * j.gate.stride) : 1.0f;
 #pragma unroll
-        for (int v = 0; v < kFwdVecs; ++v) {
+        for (int v = 0; v < VECS; ++v) {
             if (j.post.ckpt.q) keep(j.post.ckpt, row, j.cols, true, l[v], z[v]);
             float c[kVec], g[kVec];
             affine(j.post, l[v], z[v], c);
@@ -153,13 +153,13 @@ __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void ap
     }
     if (j.y.data) {
 #pragma unroll
-        for (int v = 0; v < kFwdVecs; ++v) store_row<R>(j.y, row, j.cols, true, l[v], y[v]);
+        for (int v = 0; v < VECS; ++v) store_row<R>(j.y, row, j.cols, true, l[v], y[v]);
     }
     if (!j.n.data && !j.pre.ckpt.q && !j.pre.rstd) return;
     const float r = normalise<WAVE>(y, l, j.pre.kind, a.eps_pre, a.inv_cols, slots + (WAVE ? 0 : 2 * kMaxWaves));
     if (j.pre.rstd && lane == 0) j.pre.rstd[row] = r;
 #pragma unroll
-    for (int v = 0; v < kFwdVecs; ++v) {
+    for (int v = 0; v < VECS; ++v) {
         if (j.pre.ckpt.q) keep(j.pre.ckpt, row, j.cols, true, l[v], y[v]);
         if (j.n.data) {
             float o[kVec];
@@ -509,8 +509,6 @@ int check_types(const apm_matrix& res, const apm_matrix& act) {
     return APM_OK;
 }
 
-int waves_of(int64_t cols) { return (int)div_up(cols, kWave * kVec * kFwdVecs); }
-
 // Calls go(R(), A()) with the element types.
 template <class F>
 auto with_types(int32_t res, int32_t act, F&& go) {
@@ -540,15 +538,14 @@ int forward(const apm_norm_join* jp, void* stream) {
     if (rc != APM_OK || j.rows == 0) return rc;
     if (j.rows > (int64_t)1 << 31) return fail(APM_EINVAL, "too many rows");
     JoinArgs a{j, (float)j.residual_scale, (float)j.pre.eps, (float)j.post.eps, (float)(1.0 / (double)j.cols)};
-    const int waves = waves_of(j.cols);
     with_types(j.x.dtype, act.data ? act.dtype : APM_BF16, [&](auto r, auto t) {
         using R = decltype(r);
         using A = decltype(t);
         const hipStream_t s = (hipStream_t)stream;
-        if (waves == 1)
-            hipLaunchKernelGGL((apm_join_forward_kernel<R, A, true>), dim3((unsigned)div_up(j.rows, kRowsPerGroup)), dim3(kWave * kRowsPerGroup), 0, s, a);
-        else
-            hipLaunchKernelGGL((apm_join_forward_kernel<R, A, false>), dim3((unsigned)j.rows), dim3((unsigned)(waves * kWave)), 0, s, a);
+        auto start = [&](auto kernel, int64_t groups, int64_t threads) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), 0, s, a); };
+        if (j.cols <= kWave * kVec) start(apm_join_forward_kernel<R, A, 1, true>, div_up(j.rows, kRowsPerGroup), kWave * kRowsPerGroup);
+        else if (j.cols <= kMaxThreads * kVec) start(apm_join_forward_kernel<R, A, 1, false>, j.rows, div_up(j.cols, kWave * kVec) * kWave);
+        else start(apm_join_forward_kernel<R, A, 2, false>, j.rows, div_up(j.cols, kWave * kVec * 2) * kWave);
     });
     APM_HIP(hipGetLastError());
     return APM_OK;
