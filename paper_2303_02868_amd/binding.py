@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -623,9 +624,17 @@ def apm_pool_read_timing(pool: Pool):
 
 
 # ---- activations --------------------------------------------------------------------------------
-# Tensors in, raw structures out: these look at shapes, strides and types, which the structures do not all carry.
+# Tensors in, raw structures out: these look at shapes, strides, types and memory, which the structures do not all carry.  The large
+# structures are packed in one go: field by field they cost more than the smallest calls' kernels (a join of eight tokens, us of
+# host time: 33 field by field, 19 packed).
 
 _DTYPES: dict = {}
+_NO_MATRIX, _NO_VECTOR, _NO_CKPT = (0, 0, 0, 0), (0, 0, 0), (0, 0, 0, 0, 0, 0)
+_MATRIX, _VECTOR, _CKPT = "Qqii", "Qii", "QQqqii"
+_NORM = "iid" + _VECTOR * 2 + _CKPT + "Q"
+_pack_join = struct.Struct("<qqd" + _MATRIX * 5 + "ii" + _NORM * 2).pack
+_pack_grads = struct.Struct("<" + _MATRIX * 5 + _VECTOR * 4).pack
+_pack_weight_grad = struct.Struct("<qqqqQ" + _MATRIX + _CKPT + _VECTOR * 2 + _MATRIX + "q" + _VECTOR + "ii").pack
 
 
 def _dtype(t) -> int:
@@ -638,86 +647,111 @@ def _dtype(t) -> int:
     return code
 
 
-def _on_gpu(name, t):
+def _on_gpu(name, t) -> int:
     if not t.is_cuda and not t.is_pinned():
         raise ValueError(f"{name} is in memory that the GPU cannot address")
-    return t.data_ptr() or None
+    return t.data_ptr()
+
+
+def _matrix(name, t, rows, cols):
+    if t is None:
+        return _NO_MATRIX
+    stride, code = t.stride(), _DTYPES.get(t.dtype)
+    if t.shape != (rows, cols) or (stride[1] != 1 and cols > 1):
+        raise ValueError(f"{name}: {tuple(t.shape)} with strides {stride}, {rows} rows of {cols} contiguous elements are needed")
+    return t.data_ptr() if t.is_cuda else _on_gpu(name, t), stride[0], _dtype(t) if code is None else code, 0
+
+
+def _vector(name, t, n):
+    if t is None:
+        return _NO_VECTOR
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()}, {n} contiguous elements are needed")
+    code = _DTYPES.get(t.dtype)
+    return t.data_ptr() if t.is_cuda else _on_gpu(name, t), _dtype(t) if code is None else code, 0
 
 
 def make_matrix(name: str, t, rows: int, cols: int) -> apm_matrix:
     """The apm_matrix of a two-dimensional tensor (None: not given) that has to be rows x cols."""
-    if t is None:
-        return apm_matrix()
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()}, {rows} rows of {cols} contiguous elements are needed")
-    return apm_matrix(_on_gpu(name, t), t.stride(0), _dtype(t), 0)
+    return apm_matrix(*_matrix(name, t, rows, cols))
 
 
 def make_vector(name: str, t, n: int) -> apm_vector:
-    if t is None:
-        return apm_vector()
-    if t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()}, {n} contiguous elements are needed")
-    return apm_vector(_on_gpu(name, t), _dtype(t), 0)
+    return apm_vector(*_vector(name, t, n))
 
 
-def make_ckpt(q, scale, format: int) -> apm_ckpt:
+class Ckpt:
+    """An 8-bit matrix: the tensors, and the words of its apm_ckpt."""
+    __slots__ = ("shape", "words", "tensors")
+
+
+def make_ckpt(q, scale, format: int) -> Ckpt:
     """q: rows x cols of one byte each (any type), scale: rows x ceil(cols / 32) likewise."""
-    rows, cols = q.shape
+    c = Ckpt()
+    rows, cols = c.shape = q.shape
     nb = -(-cols // APM_CKPT_BLOCK)
-    if q.element_size() != 1 or scale.element_size() != 1 or scale.dim() != 2 or scale.shape[0] != rows or scale.shape[1] != nb \
-            or (cols > 1 and q.stride(1) != 1) or (nb > 1 and scale.stride(1) != 1):
+    q_stride, s_stride = q.stride(), scale.stride()
+    if q.element_size() != 1 or scale.element_size() != 1 or scale.shape != (rows, nb) or (q_stride[1] != 1 and cols > 1) or (s_stride[1] != 1 and nb > 1):
         raise ValueError(f"an 8-bit matrix of {tuple(q.shape)} needs bytes, and scales of {(rows, nb)}: got {tuple(scale.shape)}")
-    c = apm_ckpt(_on_gpu("q", q), _on_gpu("scale", scale), q.stride(0), scale.stride(0), format, 0)
-    c.shape, c.tensors = (rows, cols), (q, scale)
+    c.words = (q.data_ptr() if q.is_cuda else _on_gpu("q", q), scale.data_ptr() if scale.is_cuda else _on_gpu("scale", scale),
+               q_stride[0], s_stride[0], format, 0)
+    c.tensors = q, scale
     return c
 
 
-def _ckpt_of(name, c, rows, cols) -> apm_ckpt:
+def _ckpt_words(name, c, rows, cols):
     if c is None:
-        return apm_ckpt()
+        return _NO_CKPT
     if c.shape != (rows, cols):
-        raise ValueError(f"{name}: {c.shape}, {(rows, cols)} is needed")
-    return c
+        raise ValueError(f"{name}: {tuple(c.shape)}, {(rows, cols)} is needed")
+    return c.words
 
 
-def apm_ckpt_write(x, ckpt: apm_ckpt, stream=None) -> None:
+def apm_ckpt_write(x, ckpt: Ckpt, stream=None) -> None:
     rows, cols = ckpt.shape
-    _check(lib().apm_ckpt_write(rows, cols, make_matrix("x", x, rows, cols), ckpt, _stream(stream)))
+    _check(lib().apm_ckpt_write(rows, cols, apm_matrix(*_matrix("x", x, rows, cols)), apm_ckpt(*ckpt.words), _stream(stream)))
 
 
-def apm_ckpt_read(ckpt: apm_ckpt, x, stream=None) -> None:
+def apm_ckpt_read(ckpt: Ckpt, x, stream=None) -> None:
     rows, cols = ckpt.shape
-    _check(lib().apm_ckpt_read(rows, cols, ckpt, make_matrix("x", x, rows, cols), _stream(stream)))
+    _check(lib().apm_ckpt_read(rows, cols, apm_ckpt(*ckpt.words), apm_matrix(*_matrix("x", x, rows, cols)), _stream(stream)))
+
+
+def _gate_shape(kind, rows, cols):
+    return (1, cols) if kind == APM_GATE_CHANNEL else (rows, 1) if kind == APM_GATE_TOKEN else (rows, cols)
+
+
+def _rstd(name, t, rows):
+    data, dtype, _ = _vector(name, t, rows)
+    if t is not None and dtype != APM_F32:
+        raise ValueError(f"{name} must be float32")
+    return data
 
 
 def make_norm_join(rows: int, cols: int, *, x=None, branch=None, y=None, n=None, residual_scale=1.0, gate_kind=APM_GATE_NONE, gate=None,
                    pre_norm=APM_NORM_NONE, pre_eps=0.0, pre_weight=None, pre_bias=None, pre_ckpt=None, pre_rstd=None,
                    post_norm=APM_NORM_NONE, post_eps=0.0, post_weight=None, post_bias=None, post_ckpt=None, post_rstd=None) -> apm_norm_join:
     """What apm_norm_join_forward and _backward work on.  The tensors are kept alive by it."""
-    def norm(name, kind, eps, weight, bias, ckpt, rstd):
-        if rstd is not None and _dtype(rstd) != APM_F32:
-            raise ValueError(f"{name}_rstd must be float32")
-        return apm_norm(kind, 0, eps, make_vector(name + "_weight", weight, cols), make_vector(name + "_bias", bias, cols),
-                        _ckpt_of(name + "_ckpt", ckpt, rows, cols), make_vector(name + "_rstd", rstd, rows).data)
-
-    gate_rows, gate_cols = {APM_GATE_CHANNEL: (1, cols), APM_GATE_TOKEN: (rows, 1)}.get(gate_kind, (rows, cols))
-    j = apm_norm_join(rows, cols, residual_scale, make_matrix("x", x, rows, cols), make_matrix("branch", branch, rows, cols),
-                      make_matrix("y", y, rows, cols), make_matrix("n", n, rows, cols), make_matrix("gate", gate, gate_rows, gate_cols),
-                      gate_kind, 0, norm("pre", pre_norm, pre_eps, pre_weight, pre_bias, pre_ckpt, pre_rstd),
-                      norm("post", post_norm, post_eps, post_weight, post_bias, post_ckpt, post_rstd))
+    j = apm_norm_join.from_buffer_copy(_pack_join(
+        rows, cols, residual_scale, *_matrix("x", x, rows, cols), *_matrix("branch", branch, rows, cols), *_matrix("y", y, rows, cols),
+        *_matrix("n", n, rows, cols), *_matrix("gate", gate, *_gate_shape(gate_kind, rows, cols)), gate_kind, 0,
+        pre_norm, 0, pre_eps, *_vector("pre_weight", pre_weight, cols), *_vector("pre_bias", pre_bias, cols),
+        *_ckpt_words("pre_ckpt", pre_ckpt, rows, cols), _rstd("pre_rstd", pre_rstd, rows),
+        post_norm, 0, post_eps, *_vector("post_weight", post_weight, cols), *_vector("post_bias", post_bias, cols),
+        *_ckpt_words("post_ckpt", post_ckpt, rows, cols), _rstd("post_rstd", post_rstd, rows)))
+    j.shape, j.kind = (rows, cols), gate_kind
     j.tensors = (x, branch, y, n, gate, pre_weight, pre_bias, pre_ckpt, pre_rstd, post_weight, post_bias, post_ckpt, post_rstd)
     return j
 
 
 def make_norm_join_grads(join: apm_norm_join, *, dn=None, dy=None, dx=None, dbranch=None, dgate=None, dpre_weight=None, dpre_bias=None,
                          dpost_weight=None, dpost_bias=None) -> apm_norm_join_grads:
-    rows, cols = join.rows, join.cols
-    gate_rows, gate_cols = {APM_GATE_CHANNEL: (1, cols), APM_GATE_TOKEN: (rows, 1)}.get(join.gate_kind, (rows, cols))
-    g = apm_norm_join_grads(make_matrix("dn", dn, rows, cols), make_matrix("dy", dy, rows, cols), make_matrix("dx", dx, rows, cols),
-                            make_matrix("dbranch", dbranch, rows, cols), make_matrix("dgate", dgate, gate_rows, gate_cols),
-                            make_vector("dpre_weight", dpre_weight, cols), make_vector("dpre_bias", dpre_bias, cols),
-                            make_vector("dpost_weight", dpost_weight, cols), make_vector("dpost_bias", dpost_bias, cols))
+    """dgate has the gate's shape."""
+    rows, cols = join.shape
+    g = apm_norm_join_grads.from_buffer_copy(_pack_grads(
+        *_matrix("dn", dn, rows, cols), *_matrix("dy", dy, rows, cols), *_matrix("dx", dx, rows, cols), *_matrix("dbranch", dbranch, rows, cols),
+        *_matrix("dgate", dgate, *_gate_shape(join.kind, rows, cols)), *_vector("dpre_weight", dpre_weight, cols), *_vector("dpre_bias", dpre_bias, cols),
+        *_vector("dpost_weight", dpost_weight, cols), *_vector("dpost_bias", dpost_bias, cols)))
     g.tensors = (dn, dy, dx, dbranch, dgate, dpre_weight, dpre_bias, dpost_weight, dpost_bias)
     return g
 
@@ -738,17 +772,17 @@ def apm_norm_join_backward(join: apm_norm_join, grads: apm_norm_join_grads, work
     _check(lib().apm_norm_join_backward(join, grads, *_room(workspace), _stream(stream)))
 
 
-def make_weight_grad(dy, kept: apm_ckpt, dw, *, db=None, weight=None, bias=None, offsets=None, accumulate=False) -> apm_weight_grad:
+def make_weight_grad(dy, kept: Ckpt, dw, *, db=None, weight=None, bias=None, offsets=None, accumulate=False) -> apm_weight_grad:
     """dw: [out, in], or with offsets (int64, groups + 1) [groups, out, in]; db: [out] or [groups, out]."""
     tokens, k = kept.shape
-    out, groups = dy.shape[1], 0
+    out, groups, at = dy.shape[1], 0, 0
     if offsets is not None:
-        groups = offsets.numel() - 1
+        groups, at = offsets.numel() - 1, _on_gpu("offsets", offsets)
         if str(offsets.dtype) != "torch.int64" or not offsets.is_contiguous() or groups < 1 or dw.dim() != 3 or dw.shape[0] != groups:
             raise ValueError(f"offsets {offsets.dtype} of {tuple(offsets.shape)} for gradients of {tuple(dw.shape)}")
-    w = apm_weight_grad(tokens, out, k, groups, None if offsets is None else _on_gpu("offsets", offsets), make_matrix("dy", dy, tokens, out), kept,
-                        make_vector("weight", weight, k), make_vector("bias", bias, k), make_matrix("dw", dw[0] if groups else dw, out, k),
-                        dw.stride(0) if groups else 0, make_vector("db", db, max(1, groups) * out), int(accumulate), 0)
+    w = apm_weight_grad.from_buffer_copy(_pack_weight_grad(
+        tokens, out, k, groups, at, *_matrix("dy", dy, tokens, out), *kept.words, *_vector("weight", weight, k), *_vector("bias", bias, k),
+        *_matrix("dw", dw[0] if groups else dw, out, k), dw.stride(0) if groups else 0, *_vector("db", db, max(1, groups) * out), int(accumulate), 0))
     w.tensors = (dy, kept, dw, db, weight, bias, offsets)
     return w
 
