@@ -1,0 +1,149 @@
+"""A small residual network trained with the library end to end on one GPU: activations kept in 8 bits, gradients out of them, parameters
+in pages.
+
+    python examples/train_blocks.py [--steps 40] [--tokens 2048] [--width 512] [--hidden 1024] [--blocks 3] [--format f8]
+
+A block is u = n W1^T, a = max(u, 0)^2, branch = a W2^T between two joins.  Join i adds the block before it to the residual stream, with a norm
+and a gate, and normalises the stream for the block behind it:
+    y_i = y_(i-1) + gate_i post_i(branch_i),    n_i = pre_i(y_i)
+The backward pass finds everything in 8 bits: the joins their normalised tensors, the activation function u, and the two weight gradients
+of a block the a and the normalised stream that its products were fed.  Matrix products that are no operator of the library
+(forward, and gradients of activations) are torch's.  The task: another random network's output.
+"""
+import argparse
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+import paper_2303_02868_amd as apm  # noqa: E402
+
+DEV = "cuda:0"
+BF16 = torch.bfloat16
+EPS = 1e-5
+
+
+def kept_like(rows, cols, form):
+    return apm.make_ckpt(torch.empty(rows, cols, dtype=torch.uint8, device=DEV),
+                         torch.empty(rows, -(-cols // apm.APM_CKPT_BLOCK), dtype=torch.uint8, device=DEV), form)
+
+
+class Parameters:
+    """bf16 parameters and gradients as tensors; fp32 masters and moments in the pages of a pool."""
+
+    def __init__(self, shapes, generator, page_elems=1 << 16):
+        self.names = list(shapes)
+        self.numels = [int(torch.Size(s).numel()) for s in shapes.values()]
+        masters = []
+        for name, s in shapes.items():
+            start = {"pre": 1.0, "post": 1.0, "gate": 0.3}.get(name.split(".")[-1])
+            masters.append(torch.full(s, start, device=DEV) if start is not None else torch.randn(s, device=DEV, generator=generator) * s[1] ** -0.5)
+        self.value = {n: m.to(BF16) for n, m in zip(self.names, masters)}
+        self.grad = {n: torch.zeros_like(v) for n, v in self.value.items()}
+        plan = apm.apm_pack_plan(page_elems, self.numels)
+        self.pool, self.pages = apm.apm_pool_create(apm.APM_DEV_GPU, page_elems, plan.n_pages), plan.n_pages
+        apm.apm_pack_tensors(self.pool, apm.APM_P32, apm.make_tensors(self.numels, apm.APM_F32, masters), len(masters))
+        torch.cuda.synchronize()
+        self.steps = 0
+
+    def step(self, lr):
+        self.steps += 1
+        lists = [apm.make_tensors(self.numels, apm.APM_BF16, [d[n] for n in self.names]) for d in (self.grad, self.value)]
+        apm.apm_page_adamw_step_fused(self.pool, None, self.pages, self.steps, apm.make_hyper(lr=lr, weight_decay=0.0, max_grad_norm=1.0), *lists,
+                                      len(self.names))
+
+
+class Network:
+    def __init__(self, tokens, width, hidden, blocks, form=apm.APM_CKPT_I8, seed=0):
+        self.tokens, self.width, self.hidden, self.blocks, self.form = tokens, width, hidden, blocks, form
+        shapes = {"0.pre": (width,)}
+        for i in range(1, blocks + 1):
+            shapes |= {f"{i}.w1": (hidden, width), f"{i}.w2": (width, hidden), f"{i}.post": (width,), f"{i}.gate": (1, width), f"{i}.pre": (width,)}
+        self.p = Parameters(shapes, torch.Generator(device=DEV).manual_seed(seed))
+
+        def make(cols, dtype=BF16):
+            return torch.empty(tokens, cols, dtype=dtype, device=DEV)
+
+        v, g = self.p.value, self.p.grad
+        self.y = [make(width, torch.float32) for _ in range(blocks + 1)]     # the residual stream
+        self.n = [make(width) for _ in range(blocks + 1)]
+        self.u_kept = [kept_like(tokens, hidden, form) for _ in range(blocks)]
+        self.a_kept = [kept_like(tokens, hidden, form) for _ in range(blocks)]
+        self.hats = [(kept_like(tokens, width, form), kept_like(tokens, width, form)) for _ in range(blocks + 1)]
+        self.rstd = [(torch.empty(tokens, device=DEV), torch.empty(tokens, device=DEV)) for _ in range(blocks + 1)]
+        self.branch, self.u_back = make(width), make(hidden)
+        self.dy, self.dn, self.dbranch = make(width, torch.float32), make(width), make(width)
+        # All buffers stay where they are, so what the calls are told is made once.
+        self.joins, self.grads = [], []
+        for i in range(blocks + 1):
+            more = {}
+            if i > 0:
+                more = dict(branch=self.branch, gate_kind=apm.APM_GATE_CHANNEL, gate=v[f"{i}.gate"], post_norm=apm.APM_NORM_RMS, post_eps=EPS,
+                            post_weight=v[f"{i}.post"], post_ckpt=self.hats[i][1], post_rstd=self.rstd[i][1])
+            join = apm.make_norm_join(tokens, width, x=self.y[max(0, i - 1)], y=self.y[i] if i > 0 else None, n=self.n[i], pre_norm=apm.APM_NORM_RMS,
+                                      pre_eps=EPS, pre_weight=v[f"{i}.pre"], pre_ckpt=self.hats[i][0], pre_rstd=self.rstd[i][0], **more)
+            more = dict(dbranch=self.dbranch, dgate=g[f"{i}.gate"], dpost_weight=g[f"{i}.post"]) if i > 0 else {}
+            self.joins.append(join)
+            self.grads.append(apm.make_norm_join_grads(join, dn=self.dn, dy=self.dy if i < blocks else None, dx=self.dy, dpre_weight=g[f"{i}.pre"], **more))
+        self.room = torch.empty(apm.apm_norm_join_workspace_bytes(tokens, width), dtype=torch.uint8, device=DEV)
+
+    def forward(self, x):
+        self.y[0].copy_(x)
+        for i, join in enumerate(self.joins):
+            if i > 0:
+                u = self.n[i - 1] @ self.p.value[f"{i}.w1"].T
+                a = u.relu().square()
+                apm.apm_ckpt_write(u, self.u_kept[i - 1])
+                apm.apm_ckpt_write(a, self.a_kept[i - 1])
+                torch.matmul(a, self.p.value[f"{i}.w2"].T, out=self.branch)
+            apm.apm_norm_join_forward(join)
+        return self.n[-1]
+
+    def weight_gradient(self, dy, kept, name, weight=None):
+        grad = apm.make_weight_grad(dy, kept, self.p.grad[name], weight=weight)
+        size = apm.apm_ckpt_weight_grad_workspace_bytes(grad)
+        apm.apm_ckpt_weight_grad(grad, torch.empty(size, dtype=torch.uint8, device=DEV) if size else None)
+
+    def backward(self, dn):
+        self.dn.copy_(dn)
+        for i in range(self.blocks, -1, -1):
+            apm.apm_norm_join_backward(self.joins[i], self.grads[i], self.room)
+            if i > 0:
+                self.weight_gradient(self.dbranch, self.a_kept[i - 1], f"{i}.w2")
+                apm.apm_ckpt_read(self.u_kept[i - 1], self.u_back)
+                du = (self.dbranch @ self.p.value[f"{i}.w2"]) * (2 * self.u_back.relu())
+                self.weight_gradient(du, self.hats[i - 1][0], f"{i}.w1", weight=self.p.value[f"{i - 1}.pre"])
+                torch.matmul(du, self.p.value[f"{i}.w1"], out=self.dn)
+
+    def kept_bytes(self):
+        pairs = [p for h in self.hats for p in h] + self.u_kept + self.a_kept
+        return sum(t.numel() for c in pairs for t in c.tensors)
+
+
+def train(steps=40, tokens=2048, width=512, hidden=1024, blocks=3, form=apm.APM_CKPT_I8, lr=2e-3, seed=0, say=print):
+    net, teacher = Network(tokens, width, hidden, blocks, form, seed), Network(tokens, width, hidden, blocks, form, seed + 1)
+    g = torch.Generator(device=DEV).manual_seed(seed + 2)
+    elems = sum(c.tensors[0].numel() for c in [h for pair in net.hats for h in pair] + net.u_kept + net.a_kept)
+    say(f"{sum(net.p.numels)} parameters in {net.p.pages} pages; kept for the backward pass: {net.kept_bytes() / 1e6:.1f} MB, in bf16 it were {2 * elems / 1e6:.1f}")
+    losses = []
+    for step in range(steps):
+        x = torch.randn(tokens, width, device=DEV, generator=g)
+        target = teacher.forward(x).clone()
+        error = net.forward(x).float() - target.float()
+        losses.append(error.square().mean())
+        net.backward(error * (2.0 / tokens))
+        net.p.step(lr)
+        if step % 10 == 0 or step == steps - 1:
+            say(f"step {step}: loss {float(losses[-1]):.4f}")
+    return [float(v) for v in losses]
+
+
+if __name__ == "__main__":
+    parser = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    for name, default in (("steps", 40), ("tokens", 2048), ("width", 512), ("hidden", 1024), ("blocks", 3)):
+        parser.add_argument("--" + name, type=int, default=default)
+    parser.add_argument("--format", choices=["i8", "f8"], default="i8")
+    args = vars(parser.parse_args())
+    form = {"i8": apm.APM_CKPT_I8, "f8": apm.APM_CKPT_F8}[args.pop("format")]
+    train(form=form, **args)
