@@ -33,6 +33,8 @@ struct Tile {
 // with one set, 181 with two).
 typedef Tile<4, 2, 2, 4, 1> Large;
 typedef Tile<4, 2, 1, 2, 2> Small;
+// 64 x 64, of which four share a CU: the shortest way from the first load to the last store (1000 tokens x 768 x 768 12.4 us, by 128 x 128 in two parts 17.8).
+typedef Tile<2, 2, 1, 1, 1> Tiny;
 
 struct WgradArgs {
     const char* dy;
@@ -51,16 +53,17 @@ struct WgradArgs {
     int32_t dw_type, accumulate;
 };
 
-// LDS: the 64-byte chunks of a tile's row t are exchanged by t mod 4, so that the four rows that a transposing load
-// takes a chunk of lie in different banks.
-template <int ROW> __device__ __forceinline__ int lds_at(int t, int byte) { return t * ROW + ((((byte >> 6) ^ (t & 3)) << 6) | (byte & 63)); }
+// LDS: the 64-byte chunks of a tile's row t are exchanged by t mod 4 (or, where a row is two of them and two rows fill the banks, by half of that), so that
+// the four rows that a transposing load takes a chunk of lie in different banks.
+template <int ROW> __device__ __forceinline__ int exchange(int t) { return ROW >= 256 ? t & 3 : (t >> 1) & 1; }
+template <int ROW> __device__ __forceinline__ int lds_at(int t, int byte) { return t * ROW + ((((byte >> 6) ^ exchange<ROW>(t)) << 6) | (byte & 63)); }
 
 // A fragment of one operand: lane l gets column l mod 32, eight tokens from 8 (l / 32) on.  A transposing load gives each of 16 lanes a column of
 // four rows that they bring together, eight bytes each.
 template <int ROW> __device__ __forceinline__ bf16x8 read_fragment(const char* tile, int frag, int t0, int lane) {
     typedef __attribute__((address_space(3))) s16x4* lds_ptr;
     const int row = t0 + 8 * (lane / 32) + (lane % 16) / 4;
-    const char* p = tile + row * ROW + ((frag ^ (row & 3)) << 6) + ((lane / 16) & 1) * 32 + (lane & 3) * 8;
+    const char* p = tile + row * ROW + ((frag ^ exchange<ROW>(row)) << 6) + ((lane / 16) & 1) * 32 + (lane & 3) * 8;
     union {
         s16x4 h[2];
         bf16x8 v;
@@ -406,52 +409,57 @@ __global__ __launch_bounds__(kJoinThreads) void apm_wgrad_join_kernel(WgradArgs 
     tokens_of(a, group, &begin, &end);
     Columns cols;
     cols.load(a, k, begin < end ? n : 0, SUMS);
-    float v[kVec] = {};
+    float v[kVec] = {}, sum = 0.0f;
     for (int s = 0; s < a.splits; s += 4) {
         Raw<float> part[4];
+        float of_row[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[i].load(a.part + ((s + i) * rows + row) * a.in, k, s + i < a.splits ? n : 0);
+        for (int i = 0; i < 4; ++i) {
+            part[i].load(a.part + ((s + i) * rows + row) * a.in, k, s + i < a.splits ? n : 0);
+            if constexpr (SUMS) of_row[i] = s + i < a.splits ? a.sums[(s + i) * rows + row] : 0.0f;
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (SUMS) sum += of_row[i];
 #pragma unroll
             for (int e = 0; e < kVec; ++e) v[e] += part[i][e];
+        }
     }
-    float sum = 0.0f;
-    if constexpr (SUMS) {
-        for (int s = 0; s < a.splits; ++s) sum += a.sums[s * rows + row];
-        if (k == 0 && a.db.data) finish_sum(a, group, o, sum);
-    }
+    if (SUMS && k == 0 && a.db.data) finish_sum(a, group, o, sum);
     finish(a, cols, group, o, k, n, v, sum);
 }
 
 // Which tile, and into how many parts the tokens are split, so that few tiles fill the chip.  Estimated in us, from calls that were timed: a round of
-// workgroups, one a CU, costs `start` and `tile` for each 64 tokens (256 x 256: 515 us for 256 of them, 140 for 64, 18.7 for one; 128 x 128: 181 for 256, 18.9 for
-// 16); parts are written and read at 4 TB/s, by one kernel more.  With one part and the better split (tokens x out x in): 1000 x 768 x 768 18.9 / 17.8,
-// 8192 x 768 x 768 94.6 / 30.3, 8192 x 2048 x 2048 by 256 x 256 209 / 91, by 128 x 128 102 / 112.
+// workgroups costs `start`, and `turn` for each 64 tokens, or `busy` times the workgroups that share a CU where that is more (256 x 256 alone on a CU: 515 us
+// for 256 turns, 140 for 64, 18.7 for one; 128 x 128 alone: 181 for 256, 18.4 for 16; 64 x 64 with up to four: 156 for 256, 12.4 for 16, 45 for 32 with four).
+// Parts are written and read at 4 TB/s, by one kernel more.  With one part and the better split (tokens x out x in): 8192 x 768 x 768 97 / 30.5, 16384 x 256 x 256 by
+// 64 x 64 156 / 23, by 128 x 128 181 / 29; 8192 x 2048 x 2048 by 256 x 256 209 / 91, by 128 x 128 102 / 112.
 constexpr int64_t kCus = 256, kMostSplits = 64;
+enum { kLarge, kSmall, kTiny };
 struct WgradShape {
-    bool large;
+    int which;
     int64_t tiles_out, tiles_in, groups;
     int32_t splits;
+    double cost;
 };
 template <class T>
-double best_split(const apm_weight_grad& w, double start, double tile, WgradShape* s) {
-    s->tiles_out = div_up(w.out, T::kOut), s->tiles_in = div_up(w.in, T::kIn), s->groups = std::max<int64_t>(1, w.n_groups);
-    const int64_t tiles = s->tiles_out * s->tiles_in * s->groups, each = div_up(w.tokens, s->groups);
-    double best = 0.0;
-    s->splits = 1;
+void best_split(const apm_weight_grad& w, int which, int64_t per_cu, double start, double turn, double busy, WgradShape* best) {
+    WgradShape s{which, div_up(w.out, T::kOut), div_up(w.in, T::kIn), std::max<int64_t>(1, w.n_groups), 1, 0.0};
+    const int64_t tiles = s.tiles_out * s.tiles_in * s.groups, each = div_up(w.tokens, s.groups);
     for (int64_t n = 1; n <= kMostSplits && (n == 1 || (tiles * n <= 2 * kCus && n <= div_up(each, 2 * T::kTokens))); ++n) {
-        const double rounds = (double)div_up(tiles * n, kCus), turns = (double)div_up(div_up(each, n), T::kTokens);
-        const double parts = n > 1 ? 4.0 + 8.0 * (double)n * (double)s->groups * (double)w.out * (double)w.in / 4e6 : 0.0;
-        const double cost = rounds * (start + turns * tile) + parts;
-        if (n == 1 || cost < best) best = cost, s->splits = (int32_t)n;
+        const double rounds = (double)div_up(tiles * n, kCus * per_cu), turns = (double)div_up(div_up(each, n), T::kTokens);
+        const double parts = n > 1 ? 4.0 + 8.0 * (double)n * (double)s.groups * (double)w.out * (double)w.in / 4e6 : 0.0;
+        s.splits = (int32_t)n;
+        s.cost = rounds * start + turns * std::max(rounds * turn, busy * (double)(tiles * n) / (double)kCus) + parts;
+        if (best->cost < 0.0 || s.cost < best->cost) *best = s;
     }
-    return best;
 }
 WgradShape wgrad_shape(const apm_weight_grad& w) {
-    WgradShape large, small;
-    large.large = true, small.large = false;
-    return best_split<Large>(w, 14.0, 1.95, &large) < best_split<Small>(w, 8.0, 0.7, &small) ? large : small;
+    WgradShape s{kLarge, 0, 0, 0, 1, -1.0};
+    best_split<Large>(w, kLarge, 1, 14.0, 1.95, 0.0, &s);
+    best_split<Small>(w, kSmall, 1, 8.0, 0.7, 0.0, &s);
+    best_split<Tiny>(w, kTiny, 4, 5.0, 0.55, 0.33, &s);
+    return s;
 }
 size_t workspace_of(const apm_weight_grad& w, const WgradShape& s) {
     return s.splits > 1 ? (size_t)s.splits * s.groups * w.out * (w.in + 1) * sizeof(float) : 0;
@@ -500,7 +508,7 @@ int weight_grad(const apm_weight_grad* wp, void* workspace, size_t workspace_byt
     a.groups = (int32_t)s.groups, a.splits = s.splits, a.tiles_in = (int32_t)s.tiles_in;
     a.near_rows = std::max({w.dy.stride, w.kept.q_stride, w.kept.scale_stride}) < (1 << 24);
     a.dw_type = w.dw.dtype, a.accumulate = w.accumulate;
-    const int64_t tiles = s.tiles_out * s.tiles_in, most = max_workgroups(std::max(Large::kThreads, Small::kThreads));
+    const int64_t tiles = s.tiles_out * s.tiles_in, most = max_workgroups(std::max({Large::kThreads, Small::kThreads, Tiny::kThreads}));
     if (tiles > most / s.splits) return fail(APM_EINVAL, "dw is too large for one product");
     a.tiles = (int32_t)tiles;
     const bool sums = w.bias.data || w.db.data;
@@ -509,7 +517,9 @@ int weight_grad(const apm_weight_grad* wp, void* workspace, size_t workspace_byt
     for (int64_t g = 0; g < s.groups; g += groups_per_launch) {
         a.first_group = (int32_t)g;
         const unsigned n = (unsigned)(tiles * s.splits * std::min(groups_per_launch, s.groups - g));
-        APM_HIP(s.large ? launch_wgrad<Large>(a, w.kept.format, sums, n, st) : launch_wgrad<Small>(a, w.kept.format, sums, n, st));
+        APM_HIP(s.which == kLarge   ? launch_wgrad<Large>(a, w.kept.format, sums, n, st)
+                : s.which == kSmall ? launch_wgrad<Small>(a, w.kept.format, sums, n, st)
+                                    : launch_wgrad<Tiny>(a, w.kept.format, sums, n, st));
     }
     if (s.splits > 1) {  // so that there are few tiles: under 2^32 vectors
         const dim3 grid((unsigned)div_up(div_up(w.in, kVec) * s.groups * w.out, kJoinThreads));
