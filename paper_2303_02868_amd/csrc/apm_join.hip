@@ -255,8 +255,12 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
 #pragma unroll
         for (int i = 0; i < kVec; ++i) w[i] = i < l[v].n ? w[i] : 0.0f;  // what is no column adds nothing to the second norm's sums
     };
-    float w1[VECS][kVec], w2[VECS][kVec];
-    if constexpr (kAhead) first_weight(0, w1[0]), second_weight(0, w2[0]);
+    auto second_bias = [&](int v, float (&b)[kVec]) { load_vector(j.post.bias, l[v], b, 0.0f); };
+    float w1[VECS][kVec], w2[VECS][kVec], b2[VECS][kVec];
+    if constexpr (kAhead) {
+        first_weight(0, w1[0]), second_weight(0, w2[0]);
+        if constexpr (!COLUMN) second_bias(0, b2[0]);
+    }
     if constexpr (!WAVE) {
         for (int i = (int)threadIdx.x; i < slots_size; i += threads) lds[i] = 0.0f;
         __syncthreads();
@@ -354,11 +358,11 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
                 if constexpr (!COLUMN) {
                     const int count = there ? l[v].n : 0;
                     if (a.g.dgate.data) {
-                        float b[kVec], o[kVec];
-                        load_vector(j.post.bias, l[v], b, 0.0f);
+                        float o[kVec];
+                        if constexpr (!kAhead) second_bias(v, b2[v]);
 #pragma unroll
                         for (int i = 0; i < kVec; ++i) {
-                            o[i] = D[v][i] * fmaf(z[v][i], w2[v][i], i < count ? b[i] : 0.0f);
+                            o[i] = D[v][i] * fmaf(z[v][i], w2[v][i], b2[v][i]);
                             s[2] += o[i];
                         }
                         if (j.gate_kind == APM_GATE_FULL) {
