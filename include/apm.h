@@ -7,6 +7,7 @@
  * parameters run page by page (Alg. 2; Sec. 4.3, last paragraph), pages move between pinned host
  * memory and HBM asynchronously (Sec. 5 "Allocator") overlapped with the update (Sec. 4.2), and a
  * one-step-stale variant decouples gradient production from the update (Sec. 4.3, Alg. 2).
+ * Calls that need no pool keep a step's activations in 8 bits and make the gradients that the update reads out of them.
  *
  * Conventions
  *   - Every function returns an apm_status (0 = ok, negative = error) unless stated; nothing
