@@ -693,7 +693,8 @@ enum apm_ckpt_format {
  * floats are).  A block that holds an infinity or a NaN has s = 255 and stands for NaN throughout.  Elements are rounded
  * to nearest, ties to even: I8 elements are off by at most 1/255 to 1/127 of the block's largest (by where that lies between two
  * powers of two), F8 elements by 2^-4 of their own size, or less than 2^-17 of the block's largest.  The values are bf16 numbers.
- * q: rows of cols bytes, q_stride >= cols apart.  scale: rows of ceil(cols / 32) bytes, scale_stride apart.
+ * q: rows of cols bytes, q_stride >= cols apart.  scale: rows of ceil(cols / 32) bytes, scale_stride apart.  Each lies in one allocation, as
+ * an apm_matrix does.
  */
 typedef struct {
     void* q;
@@ -787,7 +788,8 @@ int apm_norm_join_backward(const apm_norm_join* j, const apm_norm_join_grads* g,
  * starts as empty).  dw is then [n_groups][out, in], dw_group_stride elements apart, db [n_groups][out] contiguous.  A group without tokens gets zeros.
  * accumulate: added to what dw and db hold, with one rounding.
  * Products are exact (kept values are bf16 numbers), sums fp32; weight and bias enter after the sum.  A second call gives the same bits.
- * workspace: apm_ckpt_weight_grad_workspace_bytes(w) bytes (may be 0), 16-byte aligned, in use until the call's work is done.
+ * workspace: apm_ckpt_weight_grad_workspace_bytes(w) bytes (may be 0, as it is where the call would refuse w), 16-byte aligned, in use until
+ * the call's work is done.
  */
 typedef struct {
     int64_t tokens, out, in;

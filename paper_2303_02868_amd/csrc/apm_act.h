@@ -12,11 +12,14 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 __attribute__((aligned(1))) u32x4_any;
 typedef u32x2 __attribute__((aligned(1))) u32x2_any;
 
-template <bool NT, class V> __device__ __forceinline__ V load_at(const V* p) {
-    if constexpr (NT) return __builtin_nontemporal_load(p);
-    else return *p;
+// (Functions of their own for each type: as an argument of a template it would lose its alignment.)
+template <bool NT> __device__ __forceinline__ u32x4 load_at(const u32x4_any* p) { return NT ? __builtin_nontemporal_load(p) : *p; }
+template <bool NT> __device__ __forceinline__ u32x2 load_at(const u32x2_any* p) { return NT ? __builtin_nontemporal_load(p) : *p; }
+template <bool NT> __device__ __forceinline__ void store_at(u32x4 v, u32x4_any* p) {
+    if constexpr (NT) __builtin_nontemporal_store(v, p);
+    else *p = v;
 }
-template <bool NT, class V> __device__ __forceinline__ void store_at(V v, V* p) {
+template <bool NT> __device__ __forceinline__ void store_at(u32x2 v, u32x2_any* p) {
     if constexpr (NT) __builtin_nontemporal_store(v, p);
     else *p = v;
 }
@@ -83,7 +86,7 @@ template <class T, bool NT = false> __device__ __forceinline__ void store8(void*
                 u32x4 w;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, v[4 * h + i]);
-                store_at<NT, u32x4_any>(w, (u32x4_any*)p + h);
+                store_at<NT>(w, (u32x4_any*)p + h);
             }
         } else {
 #pragma unroll
@@ -95,7 +98,7 @@ template <class T, bool NT = false> __device__ __forceinline__ void store8(void*
             u32x4 w;
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = to_bf16x2(v[2 * i], v[2 * i + 1]);
-            store_at<NT, u32x4_any>(w, (u32x4_any*)p);
+            store_at<NT>(w, (u32x4_any*)p);
         } else {
 #pragma unroll
             for (int i = 0; i < kVec; ++i)
@@ -297,7 +300,7 @@ template <bool NT = false> __device__ __forceinline__ u32x2 load_q(const void* r
 template <bool NT = false> __device__ __forceinline__ void store_q(void* row, int col, int n, u32x2 w) {
     char* p = (char*)row + (uint32_t)col;
     if (n >= kVec) {
-        store_at<NT, u32x2_any>(w, (u32x2_any*)p);
+        store_at<NT>(w, (u32x2_any*)p);
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)

@@ -5,12 +5,15 @@
 
 namespace apm {
 
+// Rows times the distance between them stays in an address.
+static bool far_rows(int64_t rows, int64_t stride) { return rows > 1 && stride > ((int64_t)1 << 56) / rows; }
+
 int check_matrix(const char* name, const apm_matrix& m, int64_t rows, int64_t cols, bool written) {
     if (rows == 0) return APM_OK;
     if (!m.data) return fail(APM_EINVAL, "%s is missing", name);
     if (m.dtype != APM_F32 && m.dtype != APM_BF16) return fail(APM_EINVAL, "%s: bad dtype %d", name, m.dtype);
     if ((uintptr_t)m.data % (m.dtype == APM_F32 ? 4 : 2) != 0) return fail(APM_EINVAL, "%s is not aligned to its elements", name);
-    if (m.stride < 0 || (written && rows > 1 && m.stride < cols))
+    if (m.stride < 0 || far_rows(rows, m.stride) || (written && rows > 1 && m.stride < cols))
         return fail(APM_EINVAL, "%s: a row stride of %lld for %lld columns", name, (long long)m.stride, (long long)cols);
     return APM_OK;
 }
@@ -27,7 +30,7 @@ int check_ckpt(const char* name, const apm_ckpt& c, int64_t rows, int64_t cols, 
     if (!c.q || !c.scale) return fail(APM_EINVAL, "%s is missing", name);
     if (c.format != APM_CKPT_I8 && c.format != APM_CKPT_F8) return fail(APM_EINVAL, "%s: bad format %d", name, c.format);
     const int64_t nb = div_up(cols, APM_CKPT_BLOCK);
-    if (c.q_stride < 0 || c.scale_stride < 0 || (written && rows > 1 && (c.q_stride < cols || c.scale_stride < nb)))
+    if (c.q_stride < 0 || c.scale_stride < 0 || far_rows(rows, c.q_stride) || far_rows(rows, c.scale_stride) || (written && rows > 1 && (c.q_stride < cols || c.scale_stride < nb)))
         return fail(APM_EINVAL, "%s: row strides of %lld and %lld for %lld columns", name, (long long)c.q_stride, (long long)c.scale_stride,
                     (long long)cols);
     return APM_OK;

@@ -16,6 +16,7 @@ static_assert(kMaxThreads * kVec * 2 == APM_JOIN_MAX_COLS, "a row fits the large
 struct JoinArgs {
     apm_norm_join j;
     float scale, eps_pre, eps_post, inv_cols;
+    int64_t first_row;  // of the launch
 };
 
 // Sums over the lanes that hold a row.  With several wavefronts through `slots`: kMaxWaves floats for each sum, those of wavefronts that the row does
@@ -100,9 +101,9 @@ __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void ap
     __shared__ float slots[WAVE ? 1 : 4 * kMaxWaves];
     const apm_norm_join& j = a.j;
     const int lane = WAVE ? (int)threadIdx.x % kWave : (int)threadIdx.x, lanes = WAVE ? kWave : (int)blockDim.x;
-    int64_t row = blockIdx.x;
+    int64_t row = a.first_row + blockIdx.x;
     if constexpr (WAVE) {
-        row = row * kRowsPerGroup + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+        row = a.first_row + (int64_t)blockIdx.x * kRowsPerGroup + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
         if (row >= j.rows) return;
     }
     LaneCols l[VECS];
@@ -540,18 +541,26 @@ int forward(const apm_norm_join* jp, void* stream) {
     const apm_matrix& act = j.branch.data ? j.branch : j.n;
     rc = check_types(j.x, act);
     if (rc != APM_OK || j.rows == 0) return rc;
-    if (j.rows > (int64_t)1 << 31) return fail(APM_EINVAL, "too many rows");
-    JoinArgs a{j, (float)j.residual_scale, (float)j.pre.eps, (float)j.post.eps, (float)(1.0 / (double)j.cols)};
-    with_types(j.x.dtype, act.data ? act.dtype : APM_BF16, [&](auto r, auto t) {
+    JoinArgs a{j, (float)j.residual_scale, (float)j.pre.eps, (float)j.post.eps, (float)(1.0 / (double)j.cols), 0};
+    const hipError_t e = with_types(j.x.dtype, act.data ? act.dtype : APM_BF16, [&](auto r, auto t) {
         using R = decltype(r);
         using A = decltype(t);
         const hipStream_t s = (hipStream_t)stream;
-        auto start = [&](auto kernel, int64_t groups, int64_t threads) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), 0, s, a); };
-        if (j.cols <= kWave * kVec) start(apm_join_forward_kernel<R, A, 1, true>, div_up(j.rows, kRowsPerGroup), kWave * kRowsPerGroup);
-        else if (j.cols <= kMaxThreads * kVec) start(apm_join_forward_kernel<R, A, 1, false>, j.rows, div_up(j.cols, kWave * kVec) * kWave);
-        else start(apm_join_forward_kernel<R, A, 2, false>, j.rows, div_up(j.cols, kWave * kVec * 2) * kWave);
+        auto start = [&](auto kernel, int64_t rows_per_group, int64_t threads) {
+            const int64_t most = max_workgroups((int)threads) * rows_per_group;  // rows of a launch
+            for (a.first_row = 0; a.first_row < j.rows; a.first_row += most) {
+                const int64_t rows = std::min(most, j.rows - a.first_row);
+                hipLaunchKernelGGL(kernel, dim3((unsigned)div_up(rows, rows_per_group)), dim3((unsigned)threads), 0, s, a);
+                const hipError_t e = hipGetLastError();
+                if (e != hipSuccess) return e;
+            }
+            return hipSuccess;
+        };
+        if (j.cols <= kWave * kVec) return start(apm_join_forward_kernel<R, A, 1, true>, kRowsPerGroup, kWave * kRowsPerGroup);
+        if (j.cols <= kMaxThreads * kVec) return start(apm_join_forward_kernel<R, A, 1, false>, 1, div_up(j.cols, kWave * kVec) * kWave);
+        return start(apm_join_forward_kernel<R, A, 2, false>, 1, div_up(j.cols, kWave * kVec * 2) * kWave);
     });
-    APM_HIP(hipGetLastError());
+    APM_HIP(e);
     return APM_OK;
 }
 

@@ -138,6 +138,12 @@ __device__ __forceinline__ void finish(const WgradArgs& a, const Columns& c, int
     else store8<bf16, true>(row, (int)k, n, v);
 }
 
+// What lanes of a wavefront hand each other through LDS: its accesses are carried out in order, so it is the compiler's order that counts.
+__device__ __forceinline__ void among_lanes() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 constexpr int kXcds = 8;
 constexpr int kStrip = 4;  // rows of tiles that are walked together
 
@@ -378,12 +384,12 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
     for (int m = 0; m < FO; ++m)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // registers 8 h .. 8 h + 7: rows 16 h .. 16 h + 15
-            __builtin_amdgcn_wave_barrier();
+            among_lanes();
 #pragma unroll
             for (int r = 0; r < 8; ++r)
 #pragma unroll
                 for (int n = 0; n < FK; ++n) mine[(8 * (r / 4) + 4 * (lane / 32) + r % 4) * kRow + n * kFrag + lane % 32] = acc[m][n][8 * h + r];
-            __builtin_amdgcn_wave_barrier();
+            among_lanes();
 #pragma unroll
             for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
                 const int row = i * kRowsAtOnce + lane / kPer, in_tile = (wm + m) * kFrag + 16 * h + row;
@@ -485,6 +491,7 @@ int check_grad(const apm_weight_grad& w) {
     if (rc == APM_OK) rc = check_vector("bias", w.bias);
     if (rc == APM_OK) rc = check_vector("db", w.db);
     if (rc == APM_OK) rc = check_matrix("dw", w.dw, w.out, w.in, true);
+    if (rc == APM_OK && w.n_groups > 1 && w.dw_group_stride > ((int64_t)1 << 56) / w.n_groups) rc = fail(APM_EINVAL, "dw's groups are too far apart");
     if (rc == APM_OK && w.n_groups > 1 && w.dw_group_stride < (w.out - 1) * w.dw.stride + w.in) rc = fail(APM_EINVAL, "dw's groups overlap");
     return rc;
 }

@@ -157,6 +157,17 @@ def test_weight_gradient():
     assert apm.apm_ckpt_weight_grad_workspace_bytes(grad(out=0)) == 0
 
 
+def test_rows_too_far_apart_for_an_address():
+    far = 1 << 55
+    refused(apm.lib().apm_ckpt_write(4, 64, matrix(stride=far), ckpt(), None), apm.APM_EINVAL, "stride")
+    refused(apm.lib().apm_ckpt_read(4, 64, ckpt(q_stride=far), matrix(), None), apm.APM_EINVAL, "stride")
+    refused(apm.lib().apm_norm_join_forward(join(x=matrix(stride=far)), None), apm.APM_EINVAL, "stride")
+    g = apm.apm_weight_grad(100, 64, 64, 0, None, matrix(), ckpt(), apm.apm_vector(), apm.apm_vector(), matrix(stride=far))
+    refused(apm.lib().apm_ckpt_weight_grad(g, None, 0, None), apm.APM_EINVAL, "stride")
+    g = apm.apm_weight_grad(100, 64, 64, 9, PTR, matrix(), ckpt(), apm.apm_vector(), apm.apm_vector(), matrix(), 1 << 55)
+    refused(apm.lib().apm_ckpt_weight_grad(g, None, 0, None), apm.APM_EINVAL, "apart")
+
+
 def test_the_binding_looks_at_shapes_types_and_memory():
     torch = pytest.importorskip("torch")
     cpu = torch.zeros(4, 64, dtype=torch.bfloat16)
