@@ -247,18 +247,22 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
             for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.0f;
     }
     const int wm = wave / T::WK * FO, wn = wave % T::WK * FK;  // the wavefront's first fragments
-    bf16x8 fa[2][FO], fb[2][FK];
-    auto read = [&](int buf, int step) {
+    // Fragments of dy for two steps; of what was kept for two where registers are left.
+    constexpr int kSetsB = FO * FK == 8 ? 1 : 2;
+    bf16x8 fa[2][FO], fb[kSetsB][FK];
+    auto read_a = [&](int buf, int step) {
 #pragma unroll
         for (int m = 0; m < FO; ++m) fa[step & 1][m] = read_fragment<kRowA>(tile_a(buf), wm + m, step * kStep, lane);
+    };
+    auto read_b = [&](int buf, int step) {
 #pragma unroll
-        for (int n = 0; n < FK; ++n) fb[step & 1][n] = read_fragment<kRowB>(tile_b(buf), wn + n, step * kStep, lane);
+        for (int n = 0; n < FK; ++n) fb[step % kSetsB][n] = read_fragment<kRowB>(tile_b(buf), wn + n, step * kStep, lane);
     };
     auto multiply = [&](int step) {
 #pragma unroll
         for (int m = 0; m < FO; ++m) {
 #pragma unroll
-            for (int n = 0; n < FK; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[step & 1][m], fb[step & 1][n], acc[m][n], 0, 0, 0);
+            for (int n = 0; n < FK; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[step & 1][m], fb[step % kSetsB][n], acc[m][n], 0, 0, 0);
             if constexpr (SUMS) {
                 const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
@@ -275,8 +279,11 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
                 __syncthreads();
                 fetch();
             }
-            read(s == kSteps - 1 ? buf ^ 1 : buf, (s + 1) % kSteps);
+            const int from = s == kSteps - 1 ? buf ^ 1 : buf, ahead = (s + 1) % kSteps;
+            read_a(from, ahead);
+            if constexpr (kSetsB == 2) read_b(from, ahead);
             multiply(s);
+            if constexpr (kSetsB == 1) read_b(from, ahead);
             if (s > 0 && s < kSteps - 1) {
 #pragma unroll
                 for (int i = s - 1; i < T::kA; i += kSteps - 2) put_a(buf ^ 1, set, i);
@@ -319,7 +326,8 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
 #pragma unroll
         for (int i = 1; i <= D; ++i) fetch(i % D, i);
         __syncthreads();
-        read(0, 0);
+        read_a(0, 0);
+        read_b(0, 0);
         int64_t i = 0;
         if constexpr (D == 1) {
             int buf = 0;
