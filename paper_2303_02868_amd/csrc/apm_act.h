@@ -148,9 +148,9 @@ struct RawAny {
     }
 };
 
-// A row's whole vectors as a buffer: what lies beyond them (or all of it, if there is no such row or matrix) reads as zero and is not written,
-// so that every lane loads and stores without a branch, and nothing waits for more than it needs.  What is behind the last whole vector
-// comes and goes one by one.  Non-temporal: these streams are larger than the caches (gradients of a join of 8192 x 5120, fp32 stream: 119 us
+// A row as a buffer: what lies beyond it (or all of it, if there is no such row or matrix) reads as zero and is not written, so that every lane
+// loads and stores without a branch, and nothing waits for more than it needs.  The bound is checked for each 32-bit word of an access by itself: an
+// fp32 row may end anywhere.  Non-temporal: these streams are larger than the caches (gradients of a join of 8192 x 5120, fp32 stream: 119 us
 // with the default policy, 115 with non-temporal stores, 108.6 with loads too).
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 constexpr int kNT = 2;
@@ -162,19 +162,18 @@ __device__ __forceinline__ u32x2 load_b64(Rsrc r, uint32_t byte) { return __buil
 
 // A lane's eight columns.  fp32 takes two accesses of 16 bytes.  Each of them covers whole cache lines if the lower half of the wavefront's lanes takes
 // first halves and the upper half second ones, of the lower half's columns and then of the upper half's; the halves then change places in
-// registers.  Rows that end inside a vector go the plain way, so that their last lane has its own elements (the same gradients: 119 us the plain way).
+// registers (the same gradients: 119 us with each lane's own 32 bytes).
 struct LaneCols {
-    int col, n;           // n of the eight are there; 0 or less: none
-    uint32_t whole;       // columns in whole vectors
-    uint32_t at4, step4;  // fp32: byte of the first access, and from there to the second
+    int col, n;      // n of the eight are there; 0 or less: none
+    uint32_t whole;  // columns in whole vectors
+    uint32_t at4;    // fp32: byte of the first access, the second is kStep4 behind it
+    static constexpr uint32_t kStep4 = 1024;
     __device__ __forceinline__ void set(int first, int64_t cols) {
         const uint32_t lane = threadIdx.x % 64u;
         col = first;
         n = (int)min((int64_t)kVec, cols - first);
         whole = (uint32_t)cols / kVec * kVec;
-        const bool ragged = whole != (uint32_t)cols;
-        at4 = ragged ? (uint32_t)col * 4u : ((uint32_t)col - lane * kVec) * 4u + lane % 32u * 32u + lane / 32u * 16u;
-        step4 = ragged ? 16u : 1024u;
+        at4 = ((uint32_t)col - lane * kVec) * 4u + lane % 32u * 32u + lane / 32u * 16u;
     }
     __device__ __forceinline__ bool tail() const { return n > 0 && n < kVec; }
 };
@@ -185,36 +184,55 @@ __device__ __forceinline__ void swap_halves(u32x4& a, u32x4& b) {
         a[i] = r[0], b[i] = r[1];
     }
 }
-// Row `row` of a matrix: load_row, and settle before the first look at it.
-__device__ __forceinline__ void load_whole(Raw<bf16>& x, Rsrc r, const LaneCols& l) { x.a = load_b128(r, (uint32_t)l.col * 2u); }
-__device__ __forceinline__ void load_whole(Raw<float>& x, Rsrc r, const LaneCols& l) {
+// A row's last eight elements, n of which are wanted, moved down to the first places, zeros behind them
+__device__ __forceinline__ void move_down(u32x4& w, int n) {
+    const int by = kVec - n;
+    uint64_t lo = (uint64_t)w[1] << 32 | w[0], hi = (uint64_t)w[3] << 32 | w[2];
+    if (by & 4) lo = hi, hi = 0;
+    const int s = (by & 3) * 16;
+    lo = lo >> s | (hi << 1) << (63 - s);
+    hi >>= s;
+    w = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+__device__ __forceinline__ void move_down(u32x2& w, int n) {
+    const uint64_t v = ((uint64_t)w[1] << 32 | w[0]) >> (8 * (kVec - n));
+    w = u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
+}
+
+// Row `row` of a matrix: load_row, and settle before the first look at it.  A bf16 row's last elements, fewer than eight, come as the end of the eight
+// that end with the row, where it has eight, and not one by one: a branch and a trip to memory for each took gradients of 8000 x 1501 71 us and not 42.
+__device__ __forceinline__ void load_row(Raw<bf16>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
+    const bool eight = cols >= kVec;
+    const int from = l.tail() && eight ? (int)cols - kVec : l.col;
+    x.a = load_b128(row_buffer(m.data, row * m.stride * 2, there && eight ? (uint32_t)cols * 2u : 0u), (uint32_t)from * 2u);
+    if (!eight && there && m.data && l.tail()) x.load((const char*)m.data + row * m.stride * 2, l.col, l.n);
+}
+__device__ __forceinline__ void load_row(Raw<float>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
+    const Rsrc r = row_buffer(m.data, row * m.stride * 4, there ? (uint32_t)cols * 4u : 0u);
     x.a = load_b128(r, l.at4);
-    x.b = load_b128(r, l.at4 + l.step4);
+    x.b = load_b128(r, l.at4 + LaneCols::kStep4);
 }
-template <class T> __device__ __forceinline__ void load_row(Raw<T>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
-    load_whole(x, row_buffer(m.data, row * m.stride * (int64_t)sizeof(T), there ? l.whole * (uint32_t)sizeof(T) : 0u), l);
-    if (l.whole != (uint32_t)cols && there && m.data && l.tail()) x.load((const char*)m.data + row * m.stride * (int64_t)sizeof(T), l.col, l.n);
+__device__ __forceinline__ void settle(Raw<bf16>& x, const LaneCols& l, int64_t cols) {
+    if (l.whole != (uint32_t)cols && cols >= kVec && l.tail()) move_down(x.a, l.n);
 }
-__device__ __forceinline__ void settle(Raw<bf16>&, const LaneCols&, int64_t) {}
-__device__ __forceinline__ void settle(Raw<float>& x, const LaneCols& l, int64_t cols) {
-    if (l.whole == (uint32_t)cols) swap_halves(x.a, x.b);
-}
+__device__ __forceinline__ void settle(Raw<float>& x, const LaneCols&, int64_t) { swap_halves(x.a, x.b); }
 template <class T> __device__ __forceinline__ void store_row(const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l, const float (&v)[kVec]) {
-    const Rsrc r = row_buffer(m.data, row * m.stride * (int64_t)sizeof(T), there ? l.whole * (uint32_t)sizeof(T) : 0u);
     if constexpr (sizeof(T) == sizeof(float)) {
+        const Rsrc r = row_buffer(m.data, row * m.stride * 4, there ? (uint32_t)cols * 4u : 0u);
         u32x4 w[2];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) w[i / 4][i % 4] = __builtin_bit_cast(uint32_t, v[i]);
-        if (l.whole == (uint32_t)cols) swap_halves(w[0], w[1]);
+        swap_halves(w[0], w[1]);
         __builtin_amdgcn_raw_buffer_store_b128(w[0], r, (int)l.at4, 0, kNT);
-        __builtin_amdgcn_raw_buffer_store_b128(w[1], r, (int)(l.at4 + l.step4), 0, kNT);
+        __builtin_amdgcn_raw_buffer_store_b128(w[1], r, (int)(l.at4 + LaneCols::kStep4), 0, kNT);
     } else {
+        const Rsrc r = row_buffer(m.data, row * m.stride * 2, there ? l.whole * 2u : 0u);
         u32x4 w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = to_bf16x2(v[2 * i], v[2 * i + 1]);
         __builtin_amdgcn_raw_buffer_store_b128(w, r, (int)((uint32_t)l.col * 2u), 0, kNT);
+        if (l.whole != (uint32_t)cols && there && m.data && l.tail()) store8<T>((char*)m.data + row * m.stride * 2, l.col, l.n, v);
     }
-    if (l.whole != (uint32_t)cols && there && m.data && l.tail()) store8<T>((char*)m.data + row * m.stride * (int64_t)sizeof(T), l.col, l.n, v);
 }
 
 // ---- the 8-bit form -----------------------------------------------------------------------------
@@ -314,9 +332,14 @@ struct Kept {
     uint32_t s;
     __device__ __forceinline__ void load(const apm_ckpt& c, int64_t row, int64_t cols, bool there, const LaneCols& l) {
         const uint32_t blocks = ((uint32_t)cols + APM_CKPT_BLOCK - 1) / APM_CKPT_BLOCK;
-        q = load_b64(row_buffer(c.q, row * c.q_stride, there ? l.whole : 0u), (uint32_t)l.col);
+        const bool eight = cols >= kVec;
+        const int from = l.tail() && eight ? (int)cols - kVec : l.col;
+        q = load_b64(row_buffer(c.q, row * c.q_stride, there && eight ? (uint32_t)cols : 0u), (uint32_t)from);
         s = __builtin_amdgcn_raw_buffer_load_b8(row_buffer(c.q ? c.scale : nullptr, row * c.scale_stride, there ? blocks : 0u), l.col / APM_CKPT_BLOCK, 0, 0);
-        if (l.whole != (uint32_t)cols && there && c.q && l.tail()) q = load_q((const char*)c.q + row * c.q_stride, l.col, l.n);
+        if (!eight && there && c.q && l.tail()) q = load_q((const char*)c.q + row * c.q_stride, l.col, l.n);
+    }
+    __device__ __forceinline__ void settle(const LaneCols& l, int64_t cols) {
+        if (l.whole != (uint32_t)cols && cols >= kVec && l.tail()) move_down(q, l.n);
     }
     __device__ __forceinline__ void get(int32_t format, float (&v)[kVec]) const { decode8(q, scale_of(s, format), format, v); }
 };

@@ -298,7 +298,12 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
         if constexpr (!kAhead) next.load(a, row, l);
         RowRaw<R, A, VECS> cur = next;
 #pragma unroll
-        for (int v = 0; v < VECS; ++v) settle(cur.dy[v], l[v], j.cols), settle(cur.dn[v], l[v], j.cols);
+        for (int v = 0; v < VECS; ++v) {
+            settle(cur.dy[v], l[v], j.cols);
+            settle(cur.dn[v], l[v], j.cols);
+            cur.k1[v].settle(l[v], j.cols);
+            cur.k2[v].settle(l[v], j.cols);
+        }
         const bool there = row < j.rows;
         const float r1 = through1 ? __builtin_bit_cast(float, cur.r1) : 1.0f, r2 = through2 ? __builtin_bit_cast(float, cur.r2) : 1.0f;
         const float token = j.gate_kind == APM_GATE_TOKEN ? __builtin_bit_cast(float, cur.token) : 1.0f;

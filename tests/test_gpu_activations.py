@@ -359,6 +359,15 @@ def test_join_rows_at_any_alignment(cols):
         assert untouched(flat, m, 7.0)
 
 
+@pytest.mark.parametrize("cols", list(range(1, 16)) + list(range(505, 513)) + list(range(1025, 1033)))
+@pytest.mark.parametrize("res,act", [(BF16, BF16), (F32, BF16), (F32, F32)])
+def test_join_rows_that_end_at_any_column(cols, res, act):
+    J = Join(5 + 1300 // cols, cols, res, act, pre=A.LAYER, post=A.LAYER, gate=A.TOKEN, pad=3, shift=1)
+    run_both(J)
+    for flat, m in ((J.flat_y, J.y), (J.flat_n, J.n), (J.flat_dx, J.dx), (J.flat_db, J.dbranch)):
+        assert untouched(flat, m, 7.0)
+
+
 def test_join_without_a_branch_is_the_norm_of_the_stream():
     run_both(Join(20, 100, branch=False, gate=A.NO_GATE, post=A.NONE, pre=A.LAYER))
 
