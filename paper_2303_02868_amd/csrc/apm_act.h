@@ -157,7 +157,9 @@ constexpr int kNT = 2;
 __device__ __forceinline__ Rsrc row_buffer(const void* data, int64_t byte_offset, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)data + byte_offset), 0, data ? bytes : 0, 0x00027000);
 }
-__device__ __forceinline__ u32x4 load_b128(Rsrc r, uint32_t byte) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)byte, 0, kNT)); }
+template <int CACHE = kNT> __device__ __forceinline__ u32x4 load_b128(Rsrc r, uint32_t byte) {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)byte, 0, CACHE));
+}
 __device__ __forceinline__ u32x2 load_b64(Rsrc r, uint32_t byte) { return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)byte, 0, kNT)); }
 
 // A lane's eight columns.  fp32 takes two accesses of 16 bytes.  Each of them covers whole cache lines if the lower half of the wavefront's lanes takes
@@ -199,23 +201,82 @@ __device__ __forceinline__ void move_down(u32x2& w, int n) {
     w = u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
 }
 
+// The rest goes element by element, in loops and not unrolled: a call of few rows runs through a kernel's code once, and waits for that code.
+__device__ __forceinline__ u32x4 load_short(const uint16_t* p, int n) {
+    uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+    for (int i = n - 1; i >= 0; --i) {
+        hi = hi << 16 | lo >> 48;
+        lo = lo << 16 | p[i];
+    }
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+__device__ __forceinline__ u32x2 load_short(const uint8_t* p, int n) {
+    uint64_t w = 0;
+#pragma unroll 1
+    for (int i = n - 1; i >= 0; --i) w = w << 8 | p[i];
+    return u32x2{(uint32_t)w, (uint32_t)(w >> 32)};
+}
+__device__ __forceinline__ void store_short(uint16_t* p, int n, u32x4 w) {
+    uint64_t lo = (uint64_t)w[1] << 32 | w[0], hi = (uint64_t)w[3] << 32 | w[2];
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        p[i] = (uint16_t)lo;
+        lo = lo >> 16 | hi << 48;
+        hi >>= 16;
+    }
+}
+__device__ __forceinline__ void store_short(uint8_t* p, int n, u32x2 w) {
+    uint64_t v = (uint64_t)w[1] << 32 | w[0];
+#pragma unroll 1
+    for (int i = 0; i < n; ++i, v >>= 8) p[i] = (uint8_t)v;
+}
+
 // Row `row` of a matrix: load_row, and settle before the first look at it.  A bf16 row's last elements, fewer than eight, come as the end of the eight
 // that end with the row, where it has eight, and not one by one: a branch and a trip to memory for each took gradients of 8000 x 1501 71 us and not 42.
-__device__ __forceinline__ void load_row(Raw<bf16>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
+template <int CACHE = kNT> __device__ __forceinline__ u32x4 load_bf16(const void* data, int64_t byte_offset, int64_t cols, bool there, const LaneCols& l) {
     const bool eight = cols >= kVec;
     const int from = l.tail() && eight ? (int)cols - kVec : l.col;
-    x.a = load_b128(row_buffer(m.data, row * m.stride * 2, there && eight ? (uint32_t)cols * 2u : 0u), (uint32_t)from * 2u);
-    if (!eight && there && m.data && l.tail()) x.load((const char*)m.data + row * m.stride * 2, l.col, l.n);
+    u32x4 a = load_b128<CACHE>(row_buffer(data, byte_offset, there && eight ? (uint32_t)cols * 2u : 0u), (uint32_t)from * 2u);
+    if (!eight && there && data && l.tail()) a = load_short((const uint16_t*)((const char*)data + byte_offset), l.n);
+    return a;
+}
+__device__ __forceinline__ void settle_bf16(u32x4& a, const LaneCols& l, int64_t cols) {
+    if (l.whole != (uint32_t)cols && cols >= kVec && l.tail()) move_down(a, l.n);
+}
+__device__ __forceinline__ void load_row(Raw<bf16>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
+    x.a = load_bf16(m.data, row * m.stride * 2, cols, there, l);
 }
 __device__ __forceinline__ void load_row(Raw<float>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
     const Rsrc r = row_buffer(m.data, row * m.stride * 4, there ? (uint32_t)cols * 4u : 0u);
     x.a = load_b128(r, l.at4);
     x.b = load_b128(r, l.at4 + LaneCols::kStep4);
 }
-__device__ __forceinline__ void settle(Raw<bf16>& x, const LaneCols& l, int64_t cols) {
-    if (l.whole != (uint32_t)cols && cols >= kVec && l.tail()) move_down(x.a, l.n);
-}
+__device__ __forceinline__ void settle(Raw<bf16>& x, const LaneCols& l, int64_t cols) { settle_bf16(x.a, l, cols); }
 __device__ __forceinline__ void settle(Raw<float>& x, const LaneCols&, int64_t) { swap_halves(x.a, x.b); }
+// The same for eight columns of a vector of parameters, or of a gate, whose type is known at run time
+struct RowAny {
+    u32x4 a, b;
+    __device__ __forceinline__ void load(const void* data, int64_t offset, int32_t dtype, int64_t cols, bool there, const LaneCols& l) {
+        if (dtype == APM_F32) {
+            const Rsrc r = row_buffer(data, offset * 4, there ? (uint32_t)cols * 4u : 0u);
+            a = load_b128<0>(r, (uint32_t)l.col * 4u);
+            b = load_b128<0>(r, (uint32_t)l.col * 4u + 16u);
+        } else {
+            a = load_bf16<0>(data, offset * 2, cols, there, l);
+        }
+    }
+    __device__ __forceinline__ void get(int32_t dtype, int64_t cols, const LaneCols& l, float (&v)[kVec]) {
+        if (dtype == APM_F32) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v[i] = __builtin_bit_cast(float, i < 4 ? a[i & 3] : b[i & 3]);
+        } else {
+            settle_bf16(a, l, cols);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v[i] = (i & 1) ? bf16_hi(a[i / 2]) : bf16_lo(a[i / 2]);
+        }
+    }
+};
 template <class T> __device__ __forceinline__ void store_row(const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l, const float (&v)[kVec]) {
     if constexpr (sizeof(T) == sizeof(float)) {
         const Rsrc r = row_buffer(m.data, row * m.stride * 4, there ? (uint32_t)cols * 4u : 0u);
@@ -231,7 +292,7 @@ template <class T> __device__ __forceinline__ void store_row(const apm_matrix& m
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = to_bf16x2(v[2 * i], v[2 * i + 1]);
         __builtin_amdgcn_raw_buffer_store_b128(w, r, (int)((uint32_t)l.col * 2u), 0, kNT);
-        if (l.whole != (uint32_t)cols && there && m.data && l.tail()) store8<T>((char*)m.data + row * m.stride * 2, l.col, l.n, v);
+        if (l.whole != (uint32_t)cols && there && m.data && l.tail()) store_short((uint16_t*)((char*)m.data + row * m.stride * 2) + l.col, l.n, w);
     }
 }
 
@@ -336,7 +397,7 @@ struct Kept {
         const int from = l.tail() && eight ? (int)cols - kVec : l.col;
         q = load_b64(row_buffer(c.q, row * c.q_stride, there && eight ? (uint32_t)cols : 0u), (uint32_t)from);
         s = __builtin_amdgcn_raw_buffer_load_b8(row_buffer(c.q ? c.scale : nullptr, row * c.scale_stride, there ? blocks : 0u), l.col / APM_CKPT_BLOCK, 0, 0);
-        if (!eight && there && c.q && l.tail()) q = load_q((const char*)c.q + row * c.q_stride, l.col, l.n);
+        if (!eight && there && c.q && l.tail()) q = load_short((const uint8_t*)c.q + row * c.q_stride, l.n);
     }
     __device__ __forceinline__ void settle(const LaneCols& l, int64_t cols) {
         if (l.whole != (uint32_t)cols && cols >= kVec && l.tail()) move_down(q, l.n);
@@ -348,7 +409,7 @@ __device__ __forceinline__ void keep(const apm_ckpt& c, int64_t row, int64_t col
     uint32_t s;
     const u32x2 w = encode8(v, c.format, &s);
     __builtin_amdgcn_raw_buffer_store_b64(w, row_buffer(c.q, row * c.q_stride, there ? l.whole : 0u), l.col, 0, kNT);
-    if (l.whole != (uint32_t)cols && there && l.tail()) store_q((char*)c.q + row * c.q_stride, l.col, l.n, w);
+    if (l.whole != (uint32_t)cols && there && l.tail()) store_short((uint8_t*)c.q + row * c.q_stride + l.col, l.n, w);
     if (threadIdx.x % kQuad == 0 && there && l.n > 0) ((uint8_t*)c.scale)[row * c.scale_stride + (uint32_t)l.col / APM_CKPT_BLOCK] = (uint8_t)s;
 }
 

@@ -35,22 +35,37 @@ __device__ __forceinline__ void team_sums(float (&x)[N], float* slots, int wave)
     }
 }
 
-__device__ __forceinline__ void load_vector(const apm_vector& p, const LaneCols& l, float (&v)[kVec], float none) {
-    if (p.data) {
-        RawAny raw;
-        raw.load(p.data, p.dtype, l.col, l.n);
-        raw.get(p.dtype, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = none;
+// Eight columns of a vector of parameters (`none` where it is absent), or of the gate: loaded, and looked at later, so that several are under way.
+struct Param {
+    RowAny raw;
+    __device__ __forceinline__ void load(const apm_vector& p, int64_t cols, const LaneCols& l) {
+        if (p.data) raw.load(p.data, 0, p.dtype, cols, true, l);
     }
-}
-// A column's gate for all rows, or this row's
-__device__ __forceinline__ void load_gate(const apm_norm_join& j, int64_t row, int n, const LaneCols& l, float (&g)[kVec]) {
-    RawAny raw;
-    raw.load((const char*)j.gate.data + (j.gate_kind == APM_GATE_FULL ? row * j.gate.stride * (j.gate.dtype == APM_F32 ? 4 : 2) : 0), j.gate.dtype, l.col, n);
-    raw.get(j.gate.dtype, g);
-}
+    __device__ __forceinline__ void get(const apm_vector& p, int64_t cols, const LaneCols& l, float (&v)[kVec], float none) {
+        if (p.data) {
+            raw.get(p.dtype, cols, l, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v[i] = none;
+        }
+    }
+    // A column's gate for all rows, or this row's
+    __device__ __forceinline__ void load_gate(const apm_norm_join& j, int64_t row, bool there, const LaneCols& l) {
+        raw.load(j.gate.data, j.gate_kind == APM_GATE_FULL ? row * j.gate.stride : 0, j.gate.dtype, j.cols, there, l);
+    }
+    __device__ __forceinline__ void get_gate(const apm_norm_join& j, const LaneCols& l, float (&g)[kVec]) { raw.get(j.gate.dtype, j.cols, l, g); }
+};
+// A gate that is one value of a row, likewise
+struct Token {
+    uint32_t raw;
+    __device__ __forceinline__ void load(const apm_norm_join& j, int64_t row, bool there) {
+        raw = 0u;
+        if (j.gate_kind == APM_GATE_TOKEN && there) raw = j.gate.dtype == APM_F32 ? ((const uint32_t*)j.gate.data)[row * j.gate.stride] : ((const uint16_t*)j.gate.data)[row * j.gate.stride];
+    }
+    __device__ __forceinline__ float get(const apm_norm_join& j) const {
+        return j.gate_kind != APM_GATE_TOKEN ? 1.0f : __builtin_bit_cast(float, j.gate.dtype == APM_F32 ? raw : raw << 16);
+    }
+};
 
 // z becomes hat(z); elements beyond the row's end are zero before and after.
 template <bool WAVE, int VECS>
@@ -84,10 +99,15 @@ __device__ __forceinline__ float normalise(float (&z)[VECS][kVec], const LaneCol
     return r;
 }
 
-__device__ __forceinline__ void affine(const apm_norm& norm, const LaneCols& l, const float (&z)[kVec], float (&out)[kVec]) {
+// The forward kernel has other wavefronts to run while one waits: it loads these one after the other, in few registers (8192 x 2048: 34.8 us, with
+// a norm's weight, bias and gate under way together 38).
+__device__ __forceinline__ void affine(const apm_norm& norm, int64_t cols, const LaneCols& l, const float (&z)[kVec], float (&out)[kVec]) {
+    Param p;
     float w[kVec], b[kVec];
-    load_vector(norm.weight, l, w, 1.0f);
-    load_vector(norm.bias, l, b, 0.0f);
+    p.load(norm.weight, cols, l);
+    p.get(norm.weight, cols, l, w, 1.0f);
+    p.load(norm.bias, cols, l);
+    p.get(norm.bias, cols, l, b, 0.0f);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) out[i] = fmaf(z[i], w[i], b[i]);
 }
@@ -115,6 +135,8 @@ __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void ap
         load_row(x[v], j.x, row, j.cols, true, l[v]);
         load_row(b[v], j.branch, row, j.cols, true, l[v]);
     }
+    Token token;
+    token.load(j, row, true);
     if constexpr (!WAVE) {
         if (threadIdx.x < 4 * kMaxWaves) slots[threadIdx.x] = 0.0f;
         __syncthreads();
@@ -136,17 +158,18 @@ __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void ap
         }
         const float r = normalise<WAVE>(z, l, j.post.kind, a.eps_post, a.inv_cols, slots);
         if (j.post.rstd && lane == 0) j.post.rstd[row] = r;
-        const float token = j.gate_kind == APM_GATE_TOKEN ? load1(j.gate.data, j.gate.dtype, row * j.gate.stride) : 1.0f;
 #pragma unroll
         for (int v = 0; v < VECS; ++v) {
             if (j.post.ckpt.q) keep(j.post.ckpt, row, j.cols, true, l[v], z[v]);
             float c[kVec], g[kVec];
-            affine(j.post, l[v], z[v], c);
+            affine(j.post, j.cols, l[v], z[v], c);
             if (j.gate_kind == APM_GATE_CHANNEL || j.gate_kind == APM_GATE_FULL) {
-                load_gate(j, row, l[v].n, l[v], g);
+                Param gate;
+                gate.load_gate(j, row, true, l[v]);
+                gate.get_gate(j, l[v], g);
             } else {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) g[i] = token;
+                for (int i = 0; i < kVec; ++i) g[i] = token.get(j);
             }
 #pragma unroll
             for (int i = 0; i < kVec; ++i) y[v][i] = i < l[v].n ? fmaf(g[i], c[i], y[v][i]) : 0.0f;
@@ -164,7 +187,7 @@ __global__ __launch_bounds__(WAVE ? kWave * kRowsPerGroup : kMaxThreads) void ap
         if (j.pre.ckpt.q) keep(j.pre.ckpt, row, j.cols, true, l[v], y[v]);
         if (j.n.data) {
             float o[kVec];
-            affine(j.pre, l[v], y[v], o);
+            affine(j.pre, j.cols, l[v], y[v], o);
             store_row<A>(j.n, row, j.cols, true, l[v], o);
         }
     }
@@ -206,13 +229,13 @@ struct RowRaw {
     Raw<R> dy[VECS];
     Raw<A> dn[VECS];
     Kept k1[VECS], k2[VECS];
-    uint32_t r1, r2, token;
+    uint32_t r1, r2;
+    Token token;
     __device__ __forceinline__ void load(const BackArgs& a, int64_t row, const LaneCols (&l)[VECS]) {
         const bool there = row < a.j.rows;
         r1 = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(row_buffer(a.j.pre.rstd, row * 4, there ? 4u : 0u), 0, 0, 0);
         r2 = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(row_buffer(a.j.post.rstd, row * 4, there ? 4u : 0u), 0, 0, 0);
-        token = 0u;
-        if (a.j.gate_kind == APM_GATE_TOKEN && there) token = __builtin_bit_cast(uint32_t, load1(a.j.gate.data, a.j.gate.dtype, row * a.j.gate.stride));
+        token.load(a.j, row, there);
 #pragma unroll
         for (int v = 0; v < VECS; ++v) {
             load_row(dy[v], a.g.dy, row, a.j.cols, there, l[v]);
@@ -226,7 +249,8 @@ struct RowRaw {
 // COLUMN: the gate has one value for a column, or there is none: it then enters with the norm's weight, and at the end.
 // VECS 1: a lane has eight columns, and while a row is worked on the next one's loads are under way, so that the lanes of a CU's 16 wavefronts have two
 // rows' worth of loads out.  VECS 2, for rows that 16 wavefronts do not hold otherwise: no registers for either.
-// 8192 x 5120 with a fp32 stream: 108.6 us = 5.4 TB/s; of that 5 for the second kernel.
+// The first row is on its way before the weights are asked for, and they all before one of them is looked at (127 x 10215 in fp32: 54 us, so 44).
+// 8192 x 5120 with a fp32 stream: 107.4 us = 5.5 TB/s; of that 5 for the second kernel.
 constexpr int kSlotSums = 5;  // two for the first norm, three for the second and the gate
 template <class R, class A, int VECS, bool WAVE, bool BIAS, bool COLUMN>
 __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs a) {
@@ -244,24 +268,37 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
     LaneCols l[VECS];
 #pragma unroll
     for (int v = 0; v < VECS; ++v) l[v].set((v * lanes + lane) * kVec, j.cols);
-    auto first_weight = [&](int v, float (&w)[kVec]) { load_vector(j.pre.weight, l[v], w, 1.0f); };
-    auto second_weight = [&](int v, float (&w)[kVec]) {
-        load_vector(j.post.weight, l[v], w, 1.0f);
-        if (COLUMN && j.gate_kind == APM_GATE_CHANNEL) {
-            float g[kVec];
-            load_gate(j, 0, l[v].n, l[v], g);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) w[i] *= g[i];
-        }
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) w[i] = i < l[v].n ? w[i] : 0.0f;  // what is no column adds nothing to the second norm's sums
-    };
-    auto second_bias = [&](int v, float (&b)[kVec]) { load_vector(j.post.bias, l[v], b, 0.0f); };
+    const int64_t step = (int64_t)gridDim.x * a.teams;
+    const int64_t begin = (int64_t)blockIdx.x * a.teams;  // the workgroup's first row: all its wavefronts walk as often
+    int64_t row = begin + team;
+    RowRaw<R, A, VECS> next;
+    if constexpr (kAhead) next.load(a, row, l);
+    const bool by_column = COLUMN && j.gate_kind == APM_GATE_CHANNEL;
     float w1[VECS][kVec], w2[VECS][kVec], b2[VECS][kVec];
-    if constexpr (kAhead) {
-        first_weight(0, w1[0]), second_weight(0, w2[0]);
-        if constexpr (!COLUMN) second_bias(0, b2[0]);
-    }
+    // w1 the first norm's weight, w2 the second's times a column's gate, b2 the second's bias
+    auto weights = [&](int v, bool first, bool second) {
+        Param weight1, weight2, gate, bias2;
+        if (first) weight1.load(j.pre.weight, j.cols, l[v]);
+        if (second) {
+            weight2.load(j.post.weight, j.cols, l[v]);
+            if (by_column) gate.load_gate(j, 0, true, l[v]);
+            if (!COLUMN) bias2.load(j.post.bias, j.cols, l[v]);
+        }
+        if (first) weight1.get(j.pre.weight, j.cols, l[v], w1[v], 1.0f);
+        if (second) {
+            weight2.get(j.post.weight, j.cols, l[v], w2[v], 1.0f);
+            if (by_column) {
+                float g[kVec];
+                gate.get_gate(j, l[v], g);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) w2[v][i] *= g[i];
+            }
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) w2[v][i] = i < l[v].n ? w2[v][i] : 0.0f;  // what is no column adds nothing to the second norm's sums
+            if (!COLUMN) bias2.get(j.post.bias, j.cols, l[v], b2[v], 0.0f);
+        }
+    };
+    if constexpr (kAhead) weights(0, true, true);
     if constexpr (!WAVE) {
         for (int i = (int)threadIdx.x; i < slots_size; i += threads) lds[i] = 0.0f;
         __syncthreads();
@@ -288,11 +325,6 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
     for (int i = 0; i < kVec; ++i) ones[i] = 1.0f;
     const bool through1 = j.pre.kind != APM_NORM_NONE, through2 = a.g.dbranch.data && j.post.kind != APM_NORM_NONE;
     const bool mean1 = j.pre.kind == APM_NORM_LAYER, mean2 = through2 && j.post.kind == APM_NORM_LAYER;
-    const int64_t step = (int64_t)gridDim.x * a.teams;
-    const int64_t begin = (int64_t)blockIdx.x * a.teams;  // the workgroup's first row: all its wavefronts walk as often
-    int64_t row = begin + team;
-    RowRaw<R, A, VECS> next;
-    if constexpr (kAhead) next.load(a, row, l);
     int turn = 0;
     for (int64_t at = begin; at < j.rows; at += step, row += step, turn ^= 1) {
         if constexpr (!kAhead) next.load(a, row, l);
@@ -306,7 +338,7 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
         }
         const bool there = row < j.rows;
         const float r1 = through1 ? __builtin_bit_cast(float, cur.r1) : 1.0f, r2 = through2 ? __builtin_bit_cast(float, cur.r2) : 1.0f;
-        const float token = j.gate_kind == APM_GATE_TOKEN ? __builtin_bit_cast(float, cur.token) : 1.0f;
+        const float token = cur.token.get(j);
         if constexpr (kAhead) next.load(a, row + step, l);
         float* slots = lds + (turn * a.teams + team) * kSlotSums * kMaxWaves;
         float D[VECS][kVec];
@@ -315,7 +347,7 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
 #pragma unroll
             for (int v = 0; v < VECS; ++v) {
                 cur.k1[v].get(j.pre.ckpt.format, z[v]);
-                if constexpr (!kAhead) first_weight(v, w1[v]);
+                if constexpr (!kAhead) weights(v, true, false);
                 float dn[kVec];
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
@@ -360,26 +392,25 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
 #pragma unroll
             for (int v = 0; v < VECS; ++v) {
                 cur.k2[v].get(j.post.ckpt.format, z[v]);
-                if constexpr (!kAhead) second_weight(v, w2[v]);
+                if constexpr (!kAhead) weights(v, false, true);
                 if constexpr (!COLUMN) {
-                    const int count = there ? l[v].n : 0;
                     if (a.g.dgate.data) {
                         float o[kVec];
-                        if constexpr (!kAhead) second_bias(v, b2[v]);
 #pragma unroll
                         for (int i = 0; i < kVec; ++i) {
                             o[i] = D[v][i] * fmaf(z[v][i], w2[v][i], b2[v][i]);
                             s[2] += o[i];
                         }
                         if (j.gate_kind == APM_GATE_FULL) {
-                            char* p = (char*)a.g.dgate.data + row * a.g.dgate.stride * (a.g.dgate.dtype == APM_F32 ? 4 : 2);
-                            if (a.g.dgate.dtype == APM_F32) store8<float>(p, l[v].col, count, o);
-                            else store8<bf16>(p, l[v].col, count, o);
+                            if (a.g.dgate.dtype == APM_F32) store_row<float>(a.g.dgate, row, j.cols, there, l[v], o);
+                            else store_row<bf16>(a.g.dgate, row, j.cols, there, l[v], o);
                         }
                     }
                     float g[kVec];
                     if (j.gate_kind == APM_GATE_FULL) {
-                        load_gate(j, row, count, l[v], g);
+                        Param gate;
+                        gate.load_gate(j, row, there, l[v]);
+                        gate.get_gate(j, l[v], g);
                     } else {
 #pragma unroll
                         for (int i = 0; i < kVec; ++i) g[i] = token;
@@ -419,21 +450,45 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
             }
         }
     }
-    // The teams' sums of a column, which is element c mod 8 of vector c / 8 of the row.
-    float* mine = a.part + (int64_t)blockIdx.x * kSums * j.cols;
-    auto store_sums = [&](int k, int at) {
-        const int sum = k == 0 ? kDnHat : k == 1 ? kDHat : k == 2 ? kDn : kD;
-        for (int c = (int)threadIdx.x; c < (int)j.cols; c += threads) {
-            const int vec = c / kVec, v = VECS == 1 ? 0 : vec / lanes, i = c % kVec;
-            const float* p = lds + slots_size + ((((at * VECS + v) * 2 + i / 4) * threads) + vec - v * lanes) * 4 + i % 4;
-            float s = 0.0f;
-            for (int m = 0; m < a.teams; ++m) s += p[m * lanes * 4];
-            mine[sum * j.cols + c] = s;
+    // The teams' sums of four columns, the `half`-th four of vector `vec` of the row
+    constexpr int kIndex[4] = {kDnHat, kDHat, kDn, kD};
+    auto four = [&](int at, int half, int vec) {
+        const int v = VECS == 1 ? 0 : vec / lanes;
+        const f32x4* p = (const f32x4*)(lds + slots_size) + ((at * VECS + v) * 2 + half) * threads + vec - v * lanes;
+        f32x4 s = p[0];
+        for (int m = 1; m < a.teams; ++m) s += p[m * lanes];
+        return s;
+    };
+    const int vectors = ((int)j.cols + kVec - 1) / kVec, fours = 2 * vectors;
+    // Four columns a thread, which are next to its neighbours'
+    auto store_sums = [&](int first, int count) {
+        float* mine = a.part + (int64_t)blockIdx.x * kSums * j.cols;
+        for (int at = 0; at < count; ++at) {
+            float* to = mine + (int64_t)kIndex[first + at] * j.cols;
+            for (int i = (int)threadIdx.x; i < fours; i += threads) {
+                const f32x4 s = four(at, i % 2, i / 2);
+                const int c = i * 4;
+                if (c + 4 <= (int)j.cols) {
+                    store_at<false>(__builtin_bit_cast(u32x4, s), (u32x4_any*)(to + c));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (c + e < (int)j.cols) to[c + e] = s[e];
+                }
+            }
         }
     };
     __syncthreads();
+    if (kAccs == kInLds && gridDim.x == 1) {
+        for (int c = (int)threadIdx.x; c < (int)j.cols; c += threads) {
+            float s[kSums] = {};
 #pragma unroll
-    for (int k = 0; k < kInLds; ++k) store_sums(k, k);
+            for (int k = 0; k < kInLds; ++k) s[kIndex[k]] = four(k, c % kVec / 4, c / kVec)[c % 4];
+            finish_column(j, a.g, c, s);
+        }
+        return;
+    }
+    store_sums(0, kInLds);
     if constexpr (kAccs > kInLds) {
         __syncthreads();
 #pragma unroll
@@ -443,14 +498,14 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
 #pragma unroll
                 for (int h = 0; h < 2; ++h) sums[((k * VECS + v) * 2 + h) * threads] = f32x4{more[k][v][4 * h], more[k][v][4 * h + 1], more[k][v][4 * h + 2], more[k][v][4 * h + 3]};
         __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kAccs - kInLds; ++k) store_sums(kInLds + k, k);
-    }
-    if (gridDim.x == 1) {
-        for (int64_t c = threadIdx.x; c < j.cols; c += blockDim.x) {  // what this thread itself wrote
-            float s[kSums] = {mine[kDnHat * j.cols + c], 0.0f, mine[kDHat * j.cols + c], 0.0f};
-            if constexpr (BIAS) s[kDn] = mine[kDn * j.cols + c], s[kD] = mine[kD * j.cols + c];
-            finish_column(j, a.g, c, s);
+        store_sums(kInLds, kAccs - kInLds);
+        if (gridDim.x == 1) {
+            __syncthreads();
+            const float* mine = a.part;
+            for (int64_t c = threadIdx.x; c < j.cols; c += blockDim.x) {
+                float s[kSums] = {mine[kDnHat * j.cols + c], mine[kDn * j.cols + c], mine[kDHat * j.cols + c], mine[kD * j.cols + c]};
+                finish_column(j, a.g, c, s);
+            }
         }
     }
 }
@@ -459,10 +514,10 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
 constexpr int kSide = 32;
 template <bool BIAS>
 __global__ __launch_bounds__(kSide * kSide) void apm_join_sums_kernel(apm_norm_join j, apm_norm_join_grads g, const float* part, int32_t parts) {
-    __shared__ float lds[kSide][kSide + 1];
+    __shared__ float lds[kSums][kSide][kSide + 1], all[kSums][kSide];
     const int x = (int)threadIdx.x % kSide, y = (int)threadIdx.x / kSide;
     const int64_t c = (int64_t)blockIdx.x * kSide + x;
-    float t[kSums] = {}, s[kSums] = {};
+    float t[kSums] = {};
     if (c < j.cols) {
         for (int32_t p = y; p < parts; p += 8 * kSide) {
             float v[kSums][8];
@@ -479,15 +534,21 @@ __global__ __launch_bounds__(kSide * kSide) void apm_join_sums_kernel(apm_norm_j
         }
     }
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) {
-        if (!BIAS && (k == kDn || k == kD)) continue;
-        __syncthreads();
-        lds[y][x] = t[k];
-        __syncthreads();
-        if (y == 0)
-            for (int i = 0; i < kSide; ++i) s[k] += lds[i][x];
+    for (int k = 0; k < kSums; ++k) lds[k][y][x] = t[k];
+    __syncthreads();
+    if (y < kSums) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kSide; ++i) s += lds[y][i][x];
+        all[y][x] = s;
     }
-    if (y == 0 && c < j.cols) finish_column(j, g, c, s);
+    __syncthreads();
+    if (y == 0 && c < j.cols) {
+        float s[kSums];
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) s[k] = all[k][x];
+        finish_column(j, g, c, s);
+    }
 }
 
 // ---- entry points -------------------------------------------------------------------------------
