@@ -249,8 +249,8 @@ struct RowRaw {
 // COLUMN: the gate has one value for a column, or there is none: it then enters with the norm's weight, and at the end.
 // VECS 1: a lane has eight columns, and while a row is worked on the next one's loads are under way, so that the lanes of a CU's 16 wavefronts have two
 // rows' worth of loads out.  VECS 2, for rows that 16 wavefronts do not hold otherwise: no registers for either.
-// The first row is on its way before the weights are asked for, and they all before one of them is looked at (127 x 10215 in fp32: 54 us, so 44).
-// 8192 x 5120 with a fp32 stream: 107.4 us = 5.5 TB/s; of that 5 for the second kernel.
+// The first row is on its way before the weights are asked for, and they all before one of them is looked at (127 x 10215 in fp32: 54 us, so 42).
+// 8192 x 5120 with a fp32 stream: 106 us = 5.6 TB/s; of that 5 for the second kernel.
 constexpr int kSlotSums = 5;  // two for the first norm, three for the second and the gate
 template <class R, class A, int VECS, bool WAVE, bool BIAS, bool COLUMN>
 __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs a) {
@@ -479,15 +479,6 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
         }
     };
     __syncthreads();
-    if (kAccs == kInLds && gridDim.x == 1) {
-        for (int c = (int)threadIdx.x; c < (int)j.cols; c += threads) {
-            float s[kSums] = {};
-#pragma unroll
-            for (int k = 0; k < kInLds; ++k) s[kIndex[k]] = four(k, c % kVec / 4, c / kVec)[c % 4];
-            finish_column(j, a.g, c, s);
-        }
-        return;
-    }
     store_sums(0, kInLds);
     if constexpr (kAccs > kInLds) {
         __syncthreads();
@@ -499,14 +490,6 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
                 for (int h = 0; h < 2; ++h) sums[((k * VECS + v) * 2 + h) * threads] = f32x4{more[k][v][4 * h], more[k][v][4 * h + 1], more[k][v][4 * h + 2], more[k][v][4 * h + 3]};
         __syncthreads();
         store_sums(kInLds, kAccs - kInLds);
-        if (gridDim.x == 1) {
-            __syncthreads();
-            const float* mine = a.part;
-            for (int64_t c = threadIdx.x; c < j.cols; c += blockDim.x) {
-                float s[kSums] = {mine[kDnHat * j.cols + c], mine[kDn * j.cols + c], mine[kDHat * j.cols + c], mine[kD * j.cols + c]};
-                finish_column(j, a.g, c, s);
-            }
-        }
     }
 }
 
@@ -631,7 +614,8 @@ int forward(const apm_norm_join* jp, void* stream) {
 }
 
 // How many workgroups walk the rows, and with how many teams: one workgroup a CU, of as many teams as 16 wavefronts make, so that there are few
-// sums of workgroups to add (16384 x 768, us: 50 with 16 wavefronts, 55 with workgroups of 4, of which four share a CU).
+// sums of workgroups to add (16384 x 768, us: 50 with 16 wavefronts, 55 with workgroups of 4, of which four share a CU), but no more than all CUs
+// have rows for (256 x 768: 14.1 us with as many as there are, 10.5 with one; 8 rows in one workgroup, without the second kernel, 10.5, and 9.1).
 constexpr int64_t kCus = 256;
 struct BackShape {
     int vecs, waves, teams;
@@ -641,9 +625,8 @@ BackShape back_shape(int64_t rows, int64_t cols) {
     BackShape b;
     b.vecs = cols <= (int64_t)kMaxThreads * kVec ? 1 : 2;
     b.waves = (int)div_up(cols, kWave * kVec * b.vecs);
-    b.teams = kMaxWaves / b.waves;
-    // Few rows: one workgroup, and no second kernel.
-    b.groups = rows <= 2 * b.teams ? 1 : std::min(kCus, div_up(rows, b.teams));
+    b.teams = (int)std::clamp<int64_t>(div_up(rows, kCus), 1, kMaxWaves / b.waves);
+    b.groups = std::clamp<int64_t>(div_up(rows, b.teams), 1, kCus);
     return b;
 }
 
@@ -708,7 +691,7 @@ int backward(const apm_norm_join* jp, const apm_norm_join_grads* gp, void* works
         else with(std::integral_constant<int, 2>(), std::false_type());
     });
     APM_HIP(hipGetLastError());
-    if (b.groups > 1 && sums) {
+    if (sums) {
         const dim3 parts((unsigned)div_up(j.cols, kSide)), all(kSide * kSide);
         if (bias) hipLaunchKernelGGL(apm_join_sums_kernel<true>, parts, all, 0, s, j, g, a.part, (int32_t)b.groups);
         else hipLaunchKernelGGL(apm_join_sums_kernel<false>, parts, all, 0, s, j, g, a.part, (int32_t)b.groups);
