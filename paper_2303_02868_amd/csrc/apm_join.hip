@@ -246,13 +246,14 @@ struct RowRaw {
     }
 };
 
+// ONE: one workgroup, which also does the second kernel's work (in a variant of its own, as it costs the others up to 0.8 us to have the code).
 // COLUMN: the gate has one value for a column, or there is none: it then enters with the norm's weight, and at the end.
 // VECS 1: a lane has eight columns, and while a row is worked on the next one's loads are under way, so that the lanes of a CU's 16 wavefronts have two
 // rows' worth of loads out.  VECS 2, for rows that 16 wavefronts do not hold otherwise: no registers for either.
 // The first row is on its way before the weights are asked for, and they all before one of them is looked at (127 x 10215 in fp32: 54 us, so 42).
 // 8192 x 5120 with a fp32 stream: 106 us = 5.6 TB/s; of that 5 for the second kernel.
 constexpr int kSlotSums = 5;  // two for the first norm, three for the second and the gate
-template <class R, class A, int VECS, bool WAVE, bool BIAS, bool COLUMN>
+template <class R, class A, int VECS, bool WAVE, bool BIAS, bool COLUMN, bool ONE>
 __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs a) {
     // The teams' slots, twice; then the sums, four at a time of a thread's.
     extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -479,6 +480,17 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
         }
     };
     __syncthreads();
+    if constexpr (ONE) {
+        for (int c = (int)threadIdx.x; c < (int)j.cols; c += threads) {
+            const float* p = lds + slots_size + (c % kVec / 4 * threads + c / kVec) * 4 + c % 4;
+            float s[kSums] = {};
+            for (int m = 0; m < a.teams; ++m, p += lanes * 4)
+#pragma unroll
+                for (int k = 0; k < kInLds; ++k) s[kIndex[k]] += p[k * 8 * threads];
+            finish_column(j, a.g, c, s);
+        }
+        return;
+    }
     store_sums(0, kInLds);
     if constexpr (kAccs > kInLds) {
         __syncthreads();
@@ -615,18 +627,24 @@ int forward(const apm_norm_join* jp, void* stream) {
 
 // How many workgroups walk the rows, and with how many teams: one workgroup a CU, of as many teams as 16 wavefronts make, so that there are few
 // sums of workgroups to add (16384 x 768, us: 50 with 16 wavefronts, 55 with workgroups of 4, of which four share a CU), but no more than all CUs
-// have rows for (256 x 768: 14.1 us with as many as there are, 10.5 with one; 8 rows in one workgroup, without the second kernel, 10.5, and 9.1).
+// have rows for (256 x 768: 14.1 us with as many as there are, 10.5 with one).
 constexpr int64_t kCus = 256;
 struct BackShape {
     int vecs, waves, teams;
     int64_t groups;
+    bool one;  // workgroup, and no second kernel: few rows, whose time is the host's (8 x 768: 16 us, with a second launch 19)
 };
 BackShape back_shape(int64_t rows, int64_t cols) {
     BackShape b;
     b.vecs = cols <= (int64_t)kMaxThreads * kVec ? 1 : 2;
     b.waves = (int)div_up(cols, kWave * kVec * b.vecs);
-    b.teams = (int)std::clamp<int64_t>(div_up(rows, kCus), 1, kMaxWaves / b.waves);
-    b.groups = std::clamp<int64_t>(div_up(rows, b.teams), 1, kCus);
+    b.teams = kMaxWaves / b.waves;
+    b.groups = 1;
+    b.one = b.vecs == 1 && rows <= b.teams;
+    if (!b.one) {
+        b.teams = (int)std::clamp<int64_t>(div_up(rows, kCus), 1, b.teams);
+        b.groups = std::clamp<int64_t>(div_up(rows, b.teams), 1, kCus);
+    }
     return b;
 }
 
@@ -683,15 +701,22 @@ int backward(const apm_norm_join* jp, const apm_norm_join_grads* gp, void* works
         auto with = [&](auto vecs, auto wave) {
             constexpr int V = decltype(vecs)::value;
             constexpr bool W = decltype(wave)::value;
-            if (column) bias ? start(apm_join_backward_kernel<R, A, V, W, true, true>) : start(apm_join_backward_kernel<R, A, V, W, false, true>);
-            else bias ? start(apm_join_backward_kernel<R, A, V, W, true, false>) : start(apm_join_backward_kernel<R, A, V, W, false, false>);
+            auto go = [&](auto alone) {
+                constexpr bool O = decltype(alone)::value;
+                if (column) bias ? start(apm_join_backward_kernel<R, A, V, W, true, true, O>) : start(apm_join_backward_kernel<R, A, V, W, false, true, O>);
+                else bias ? start(apm_join_backward_kernel<R, A, V, W, true, false, O>) : start(apm_join_backward_kernel<R, A, V, W, false, false, O>);
+            };
+            if constexpr (V == 1) {
+                if (b.one) return go(std::true_type());
+            }
+            go(std::false_type());
         };
         if (b.waves == 1) with(std::integral_constant<int, 1>(), std::true_type());
         else if (b.vecs == 1) with(std::integral_constant<int, 1>(), std::false_type());
         else with(std::integral_constant<int, 2>(), std::false_type());
     });
     APM_HIP(hipGetLastError());
-    if (sums) {
+    if (sums && !b.one) {
         const dim3 parts((unsigned)div_up(j.cols, kSide)), all(kSide * kSide);
         if (bias) hipLaunchKernelGGL(apm_join_sums_kernel<true>, parts, all, 0, s, j, g, a.part, (int32_t)b.groups);
         else hipLaunchKernelGGL(apm_join_sums_kernel<false>, parts, all, 0, s, j, g, a.part, (int32_t)b.groups);
