@@ -33,8 +33,9 @@ struct Tile {
 // with one set, 181 with two).
 typedef Tile<4, 2, 2, 4, 1> Large;
 typedef Tile<4, 2, 1, 2, 2> Small;
-// 64 x 64, of which four share a CU: the shortest way from the first load to the last store (1000 tokens x 768 x 768 12.4 us, by 128 x 128 in two parts 17.8).
-typedef Tile<2, 2, 1, 1, 1> Tiny;
+// 64 x 64, of which four share a CU: the shortest way from the first load to the last store (1000 tokens x 768 x 768 11.3 us, by 128 x 128 in two parts 17.8).
+// With one set of registers for later tiles 11.6 us there, and 2048 x 768 x 2304 (F8) 21.2 instead of 19.5; 64 tokens take 0.3 us more with two.
+typedef Tile<2, 2, 1, 1, 2> Tiny;
 
 struct WgradArgs {
     const char* dy;
@@ -247,12 +248,14 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
             for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.0f;
     }
     const int wm = wave / T::WK * FO, wn = wave % T::WK * FK;  // the wavefront's first fragments
-    // Fragments of dy for two steps; of what was kept for two where registers are left.
-    constexpr int kSetsB = FO * FK == 8 ? 1 : 2;
-    bf16x8 fa[2][FO], fb[kSetsB][FK];
+    // Fragments of dy for two steps; of what was kept for two where registers are left; of both for all steps where a wavefront has one of each, which
+    // then waits for LDS once a tile and not at each step (2048 tokens x 1024 x 1024 in F8: 16.6 us, so 16.0; without sums 13.7 and 13.2).
+    constexpr bool kWhole = FO * FK == 1;
+    constexpr int kSetsA = kWhole ? kSteps : 2, kSetsB = kWhole ? kSteps : FO * FK == 8 ? 1 : 2;
+    bf16x8 fa[kSetsA][FO], fb[kSetsB][FK];
     auto read_a = [&](int buf, int step) {
 #pragma unroll
-        for (int m = 0; m < FO; ++m) fa[step & 1][m] = read_fragment<kRowA>(tile_a(buf), wm + m, step * kStep, lane);
+        for (int m = 0; m < FO; ++m) fa[step % kSetsA][m] = read_fragment<kRowA>(tile_a(buf), wm + m, step * kStep, lane);
     };
     auto read_b = [&](int buf, int step) {
 #pragma unroll
@@ -262,17 +265,30 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
 #pragma unroll
         for (int m = 0; m < FO; ++m) {
 #pragma unroll
-            for (int n = 0; n < FK; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[step & 1][m], fb[step % kSetsB][n], acc[m][n], 0, 0, 0);
+            for (int n = 0; n < FK; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[step % kSetsA][m], fb[step % kSetsB][n], acc[m][n], 0, 0, 0);
             if constexpr (SUMS) {
                 const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-                for (int i = 0; i < kVec; i += 2) sum[m] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{fa[step & 1][m][i], fa[step & 1][m][i + 1]}, one, sum[m], false);
+                for (int i = 0; i < kVec; i += 2) sum[m] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{fa[step % kSetsA][m][i], fa[step % kSetsA][m][i + 1]}, one, sum[m], false);
             }
         }
     };
     // A tile of tokens, in steps.  Fragments are read a step ahead.  In the middle steps what a set of registers holds of the next tile goes into the
     // other buffer; before the last one everybody has read this buffer, so that the set is filled anew and the next tile's first fragments are read.
     auto turn = [&](int buf, int set, auto&& fetch) {
+        if constexpr (kWhole) {  // the next tile is put down while this one's fragments are on their way
+#pragma unroll
+            for (int i = 0; i < T::kA; ++i) put_a(buf ^ 1, set, i);
+#pragma unroll
+            for (int i = 0; i < T::kB; ++i) put_b(buf ^ 1, set, i);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) multiply(s);
+            __syncthreads();
+            fetch();
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) read_a(buf ^ 1, s), read_b(buf ^ 1, s);
+            return;
+        }
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             if (s == kSteps - 1) {
@@ -328,6 +344,10 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
         __syncthreads();
         read_a(0, 0);
         read_b(0, 0);
+        if constexpr (kWhole) {
+#pragma unroll
+            for (int s = 1; s < kSteps; ++s) read_a(0, s), read_b(0, s);
+        }
         int64_t i = 0;
         if constexpr (D == 1) {
             int buf = 0;
