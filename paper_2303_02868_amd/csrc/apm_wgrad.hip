@@ -123,7 +123,9 @@ struct Columns {
         }
     }
 };
-__device__ __forceinline__ void finish(const WgradArgs& a, const Columns& c, int64_t group, int64_t o, int64_t k, int n, float (&v)[kVec], float sum) {
+// HOP > 0: the lanes' upper half has the rows HOP below those of the lower half, and if `whole` all 64 have eight columns of a row.
+template <int HOP>
+__device__ __forceinline__ void finish(const WgradArgs& a, const Columns& c, int64_t group, int64_t o, int64_t k, int n, bool whole, float (&v)[kVec], float sum) {
     char* row = a.dw + (group * a.group_stride + o * a.dw_stride) * (a.dw_type == APM_F32 ? 4 : 2);
 #pragma unroll
     for (int e = 0; e < kVec; ++e) v[e] = fmaf(v[e], c.w[e], c.b[e] * sum);
@@ -134,6 +136,20 @@ __device__ __forceinline__ void finish(const WgradArgs& a, const Columns& c, int
         old.get(a.dw_type, f);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) v[e] += f[e];
+    }
+    // fp32 in whole cache lines at a time, the lower half of the lanes' rows, then the upper half's (64 groups of 704 x 2560, a token each: 152 us with a
+    // lane's own 32 bytes, so 107).
+    if (HOP > 0 && whole && a.dw_type == APM_F32) {
+        u32x4 w[2];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) w[e / 4][e % 4] = __builtin_bit_cast(uint32_t, v[e]);
+        swap_halves(w[0], w[1]);
+        const int64_t hop = HOP * a.dw_stride * 4;
+        const bool upper = threadIdx.x % kWave >= kWave / 2;
+        char* at = row + k * 4 + (upper ? 16 : 0);
+        store_at<true>(w[0], (u32x4_any*)(at - (upper ? hop : 0)));
+        store_at<true>(w[1], (u32x4_any*)(at + (upper ? 0 : hop)));
+        return;
     }
     if (a.dw_type == APM_F32) store8<float, true>(row, (int)k, n, v);
     else store8<bf16, true>(row, (int)k, n, v);
@@ -171,18 +187,25 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
     int64_t begin, end;
     tokens_of(a, group, &begin, &end);
     // No sum at all: not even weight times it.  Stored non-temporally, as the results are: rows of other groups stay in L2 (64 groups of 4096 x 1024, an
-    // eighth of them with tokens: 181 us, with non-temporal stores 141; zeros alone 97).
+    // eighth of them with tokens: 181 us, with non-temporal stores 131; zeros alone 97).  In fp32 with eight elements a lane, which halves of lines take,
+    // 64 empty groups of 704 x 2560 took 194 us, so 91.
     if (begin == end && a.splits == 1) {
         if (a.accumulate) return;
-        const float none[kVec] = {};
-        const int size = a.dw_type == APM_F32 ? 4 : 2;
+        const bool wide = a.dw_type == APM_F32;
+        const int size = wide ? 4 : 2, per = 16 / size, in_row = T::kIn / per;  // 16 bytes a lane, next to its neighbours' in both types
 #pragma unroll 4
-        for (int i = tid; i < T::kOut * T::kIn / kVec; i += T::kThreads) {
-            const int64_t o = o0 + i / (T::kIn / kVec), k = k0 + i % (T::kIn / kVec) * kVec;
-            char* row = a.dw + (group * a.group_stride + o * a.dw_stride) * size;
-            const int n = o < a.out ? (int)max((int64_t)0, min((int64_t)kVec, a.in - k)) : 0;
-            if (a.dw_type == APM_F32) store8<float, true>(row, (int)k, n, none);
-            else store8<bf16, true>(row, (int)k, n, none);
+        for (int i = tid; i < T::kOut * in_row; i += T::kThreads) {
+            const int64_t o = o0 + i / in_row, k = k0 + i % in_row * per;
+            char* to = a.dw + (group * a.group_stride + o * a.dw_stride + k) * size;
+            if (o >= a.out) continue;
+            if (k + per <= a.in) {
+                store_at<true>(u32x4{0u, 0u, 0u, 0u}, (u32x4_any*)to);
+            } else {
+                for (int64_t e = k; e < a.in; ++e, to += size) {
+                    if (wide) *(uint32_t*)to = 0u;
+                    else *(uint16_t*)to = 0;
+                }
+            }
         }
         if (SUMS && a.db.data && k0 == 0 && tid < T::kOut && o0 + tid < a.out) finish_sum(a, group, o0 + tid, 0.0f);
         return;
@@ -406,6 +429,7 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
     const int c = lane % kPer * kVec;
     const int64_t k = k0 + wn * kFrag + c;
     const int there = (int)max((int64_t)0, min((int64_t)kVec, a.in - k));
+    const bool whole_tile = o0 + T::kOut <= a.out && k0 + T::kIn <= a.in;
     Columns cols;
     cols.load(a, k, there, SUMS);
 #pragma unroll
@@ -425,7 +449,7 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
                 float v[kVec];
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) v[e] = mine[row * kRow + c + e];
-                finish(a, cols, group, o, k, o < a.out ? there : 0, v, SUMS ? row_sum[in_tile] : 0.0f);
+                finish<kRowsAtOnce / 2>(a, cols, group, o, k, o < a.out ? there : 0, whole_tile, v, SUMS ? row_sum[in_tile] : 0.0f);
             }
         }
 }
@@ -460,7 +484,7 @@ __global__ __launch_bounds__(kJoinThreads) void apm_wgrad_join_kernel(WgradArgs 
         }
     }
     if (SUMS && k == 0 && a.db.data) finish_sum(a, group, o, sum);
-    finish(a, cols, group, o, k, n, v, sum);
+    finish<0>(a, cols, group, o, k, n, false, v, sum);
 }
 
 // Which tile, and into how many parts the tokens are split, so that few tiles fill the chip.  Estimated in us, from calls that were timed: a round of

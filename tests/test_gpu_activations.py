@@ -567,6 +567,12 @@ def test_weight_gradient_of_large_matrices(tokens, out, k, pad, shift):
     check_weight_grad(tokens, out, k, A.F8, BF16, weight=False, bias=False, db=False, pad=pad, shift=shift)
 
 
+@pytest.mark.parametrize("tokens,out,k,pad,shift", [(130, 4096, 2048, 0, 0), (70, 2048, 2304, 1, 3), (1500, 1024, 1100, 4, 0), (40, 1400, 700, 0, 1)])
+def test_weight_gradient_in_fp32_of_large_matrices(tokens, out, k, pad, shift):
+    check_weight_grad(tokens, out, k, A.F8, F32, pad=pad, shift=shift, accumulate=shift > 0)
+    check_weight_grad(tokens, out, k, A.I8, F32, weight=False, bias=False, db=False, offsets=[0, 0, tokens // 2, tokens, tokens], pad=pad, shift=shift)
+
+
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_weight_gradient_of_groups_of_large_matrices(accumulate):
     check_weight_grad(300, 1100, 1030, A.F8, BF16, offsets=[0, 0, 129, 130, 130, 300, 300] + [300] * 10, accumulate=accumulate)
