@@ -165,7 +165,7 @@ constexpr int kXcds = 8;
 constexpr int kStrip = 4;  // rows of tiles that are walked together
 
 // Bound by what LDS gives (a fragment is read by transposing loads, at about 120 bytes a clock) beside the matrix cores, which are busy half the
-// time at 1.9 GHz: 1100 (I8) to 1180 TFLOP/s (F8) at 16384 tokens x 8192 x 2048, 515 and 495 us with sums; a library product of bf16 matrices in this
+// time at 1.9 GHz: 1160 (I8) to 1180 TFLOP/s (F8) at 16384 tokens x 8192 x 2048, 508 and 495 us with sums; a library product of bf16 matrices in this
 // order reaches 960, in the order that suits it 1300.
 template <class T, int FORMAT, bool SUMS>
 __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
