@@ -105,7 +105,8 @@ __device__ __forceinline__ void finish_sum(const WgradArgs& a, int64_t group, in
     if (a.accumulate) sum += load1(a.db.data, a.db.dtype, at);
     store1(a.db.data, a.db.dtype, at, sum);
 }
-// Eight sums of row o from column k on, n of them there, become dw: v weight + bias (sum of dy), added to what is there if asked for.
+// Eight sums of row o from column k on, n of them there, become dw: v weight + bias (sum of dy), added to what is there if asked for. Where the bias is
+// zero, as it is where there is none, no sum of dy is added: it may be an infinity where dw is a number.
 struct Columns {
     float w[kVec], b[kVec];
     __device__ __forceinline__ void load(const WgradArgs& a, int64_t k, int n, bool with_bias) {
@@ -128,7 +129,7 @@ template <int HOP>
 __device__ __forceinline__ void finish(const WgradArgs& a, const Columns& c, int64_t group, int64_t o, int64_t k, int n, bool whole, float (&v)[kVec], float sum) {
     char* row = a.dw + (group * a.group_stride + o * a.dw_stride) * (a.dw_type == APM_F32 ? 4 : 2);
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) v[e] = fmaf(v[e], c.w[e], c.b[e] * sum);
+    for (int e = 0; e < kVec; ++e) v[e] = fmaf(v[e], c.w[e], c.b[e] == 0.0f ? 0.0f : c.b[e] * sum);
     if (a.accumulate) {
         RawAny old;
         old.load(row, a.dw_type, (int)k, n);
