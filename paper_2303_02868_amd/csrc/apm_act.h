@@ -61,7 +61,7 @@ template <> struct Raw<bf16> {
 template <> struct Raw<float> {
     u32x4 a, b;
     template <bool NT = false> __device__ __forceinline__ void load(const void* row, int col, int n) {
-        const char* p = (const char*)row + (uint32_t)col * 4u;
+        const char* p = (const char*)row + (int64_t)col * 4;  // past 32 bits from column 2^30 on
         a = b = u32x4{0, 0, 0, 0};
         if (n >= kVec) {
             a = load_at<NT>((const u32x4_any*)p);
@@ -78,7 +78,7 @@ template <> struct Raw<float> {
     __device__ __forceinline__ float operator[](int i) const { return __builtin_bit_cast(float, i < 4 ? a[i & 3] : b[i & 3]); }
 };
 template <class T, bool NT = false> __device__ __forceinline__ void store8(void* row, int col, int n, const float (&v)[kVec]) {
-    char* p = (char*)row + (uint32_t)col * (uint32_t)sizeof(T);
+    char* p = (char*)row + (int64_t)col * (int64_t)sizeof(T);
     if constexpr (sizeof(T) == sizeof(float)) {
         if (n >= kVec) {
 #pragma unroll

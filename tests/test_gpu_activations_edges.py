@@ -1,12 +1,13 @@
-"""The activation calls where values leave the number range."""
+"""The activation calls where values leave the number range, and where rows are very wide."""
 from __future__ import annotations
 
+import numpy as np
 import pytest
 import torch
 
 import oracle.activations as A
 import paper_2303_02868_amd as apm
-from test_gpu_activations import BF16, DEV, F32, random_kept
+from test_gpu_activations import BF16, DEV, F32, f64, kept_blank, random_kept
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -57,3 +58,33 @@ def test_sums_of_dy_do_not_reach_dw_without_a_bias(tokens, split, fmt, weight):
     with_one, _ = weight_grad(dy, kept, fmt, weight=w, bias=some)
     others = torch.arange(k, device=DEV) != 7
     assert same_bits(plain[:, others].contiguous(), with_one[:, others].contiguous()) and torch.isinf(with_one[3, 7])
+
+
+# ---- 8-bit matrices of very wide rows -----------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", [A.I8, A.F8])
+def test_rows_of_fp32_beyond_4_gib(fmt):
+    """A buffer flattened to one row: byte offsets of its columns pass 32 bits at column 2^30."""
+    far = 2 ** 30
+    cols = far + 1005
+    x = torch.empty(1, cols, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(9)
+    for at in range(0, cols, 1 << 28):
+        x[:, at:at + (1 << 28)].normal_(generator=g)
+    x[:, far:] *= 8.0                                               # no scale byte as at the row's beginning
+    kept = kept_blank(1, cols)
+    apm.apm_ckpt_write(x, apm.make_ckpt(*kept, fmt))
+    whole = kept_blank(far >> 15, 1 << 15)                          # the same blocks, as rows of 2^15 columns
+    apm.apm_ckpt_write(x[0, :far].view(far >> 15, 1 << 15), apm.make_ckpt(*whole, fmt))
+    assert torch.equal(kept[0][0, :far], whole[0].view(-1)) and torch.equal(kept[1][0, :far // 32], whole[1].view(-1))
+    q, s = A.encode(f64(x[:, far:]), fmt)
+    assert np.array_equal(kept[0][:, far:].cpu().numpy(), q) and np.array_equal(kept[1][:, far // 32:].cpu().numpy(), s)
+    first = x[:, :1000].clone()
+    back = x.fill_(7.0)
+    apm.apm_ckpt_read(apm.make_ckpt(*kept, fmt), back)
+    assert np.array_equal(f64(back[:, far:]), A.decode(q, s, fmt))
+    q, s = A.encode(f64(first)[:, :992], fmt)
+    assert np.array_equal(f64(back[:, :992]), A.decode(q, s, fmt))
+    again = torch.empty(far >> 15, 1 << 15, device=DEV)
+    apm.apm_ckpt_read(apm.make_ckpt(*whole, fmt), again)
+    assert torch.equal(back[0, :far], again.view(-1))
