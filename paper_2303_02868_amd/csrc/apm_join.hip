@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
             cur.k2[v].settle(l[v], j.cols);
         }
         const bool there = row < j.rows;
-        const float r1 = through1 ? __builtin_bit_cast(float, cur.r1) : 1.0f, r2 = through2 ? __builtin_bit_cast(float, cur.r2) : 1.0f;
+        const float r1 = __builtin_bit_cast(float, cur.r1), r2 = __builtin_bit_cast(float, cur.r2);
         const float token = cur.token.get(j);
         if constexpr (kAhead) next.load(a, row + step, l);
         float* slots = lds + (turn * a.teams + team) * kSlotSums * kMaxWaves;
@@ -440,15 +440,15 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
                 team_sums<WAVE>(one, slots + 2 * kMaxWaves, in_team);
                 s[0] = one[0];
             }
-            // without a norm r2 = 1, and k = m = 0
-            const float k = through2 ? s[0] * a.inv_cols : 0.0f, m = mean2 ? s[1] * a.inv_cols : 0.0f;
+            if (through2) {  // without a norm hat2, which may be NaN, has no part in it
+                const float k = s[0] * a.inv_cols, m = mean2 ? s[1] * a.inv_cols : 0.0f;
 #pragma unroll
-            for (int v = 0; v < VECS; ++v) {
-                float o[kVec];
+                for (int v = 0; v < VECS; ++v)
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) o[i] = r2 * (D[v][i] - fmaf(z[v][i], k, m));
-                store_row<A>(a.g.dbranch, row, j.cols, there, l[v], o);
+                    for (int i = 0; i < kVec; ++i) D[v][i] = r2 * (D[v][i] - fmaf(z[v][i], k, m));
             }
+#pragma unroll
+            for (int v = 0; v < VECS; ++v) store_row<A>(a.g.dbranch, row, j.cols, there, l[v], D[v]);
         }
     }
     // The teams' sums of four columns, the `half`-th four of vector `vec` of the row

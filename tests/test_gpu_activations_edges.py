@@ -7,7 +7,7 @@ import torch
 
 import oracle.activations as A
 import paper_2303_02868_amd as apm
-from test_gpu_activations import BF16, DEV, F32, f64, kept_blank, random_kept
+from test_gpu_activations import BF16, DEV, F32, Join, f64, kept_blank, random_kept, room_for
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -88,3 +88,25 @@ def test_rows_of_fp32_beyond_4_gib(fmt):
     again = torch.empty(far >> 15, 1 << 15, device=DEV)
     apm.apm_ckpt_read(apm.make_ckpt(*whole, fmt), again)
     assert torch.equal(back[0, :far], again.view(-1))
+
+
+# ---- join gradients: values that are no numbers -------------------------------------------------
+
+@pytest.mark.parametrize("rows,cols", [(6, 100), (400, 600), (5, 9000)])
+@pytest.mark.parametrize("gate", [A.NO_GATE, A.CHANNEL, A.TOKEN, A.FULL])
+def test_without_a_norm_the_gradient_of_the_branch_does_not_depend_on_what_was_kept(rows, cols, gate):
+    """dbranch = gate D post.weight: a block of the branch that stands for NaN reaches the gradients of gate and weight alone."""
+    J = Join(rows, cols, post=A.NONE, gate=gate)
+    join = J.join()
+    apm.apm_norm_join_forward(join)
+    J.kept2[1][2, 1] = 255                                          # row 2, channels 32 .. 63
+    apm.apm_norm_join_backward(join, J.grads(join, dgate=None, dpost_weight=None), room_for(rows, cols))
+    alone = J.dbranch.clone()
+    assert bool(torch.isfinite(alone).all())
+    for more in ({}, {"dgate": None}, {"dpost_weight": None}):
+        J.dbranch.fill_(7.0)
+        apm.apm_norm_join_backward(join, J.grads(join, **more), room_for(rows, cols))
+        assert torch.equal(J.dbranch, alone)
+    apm.apm_norm_join_backward(join, J.grads(join), room_for(rows, cols))
+    nan = torch.isnan(J.dw2)
+    assert bool(nan[32:64].all()) and int(nan.sum()) == 32
