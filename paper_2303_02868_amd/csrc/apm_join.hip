@@ -682,8 +682,13 @@ int backward(const apm_norm_join* jp, const apm_norm_join_grads* gp, void* works
     else a.j.post.ckpt.q = nullptr;
     if (rc != APM_OK) return rc;
     if (j.rows > 0 && g.dn.data && j.pre.kind != APM_NORM_NONE && !j.pre.rstd) return fail(APM_EINVAL, "pre.rstd is missing");
-    if (!g.dn.data) a.j.pre.kind = APM_NORM_NONE;
     if (j.rows > 0 && g.dbranch.data && j.post.kind != APM_NORM_NONE && !j.post.rstd) return fail(APM_EINVAL, "post.rstd is missing");
+    // What the formulas do not name is not read, and 0 is no factor: a gradient that is missing stays zero beside an infinite weight.
+    if (!g.dn.data) a.j.pre.kind = APM_NORM_NONE, a.j.pre.weight.data = nullptr;
+    if (a.j.pre.kind == APM_NORM_NONE) a.j.pre.rstd = nullptr;
+    if (!g.dbranch.data || j.post.kind == APM_NORM_NONE) a.j.post.rstd = nullptr;
+    if (!g.dbranch.data && !g.dgate.data) a.j.post.weight.data = nullptr;
+    if (!g.dgate.data) a.j.post.bias.data = nullptr;
     if (workspace_bytes < apm_norm_join_workspace_bytes(j.rows, j.cols)) return fail(APM_ENOMEM, "the workspace is too small");
     if (!workspace || (uintptr_t)workspace % 16 != 0) return fail(APM_EINVAL, "the workspace is missing or not aligned to 16 bytes");
     const BackShape b = back_shape(j.rows, j.cols);

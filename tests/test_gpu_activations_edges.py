@@ -110,3 +110,19 @@ def test_without_a_norm_the_gradient_of_the_branch_does_not_depend_on_what_was_k
     apm.apm_norm_join_backward(join, J.grads(join), room_for(rows, cols))
     nan = torch.isnan(J.dw2)
     assert bool(nan[32:64].all()) and int(nan.sum()) == 32
+
+
+@pytest.mark.parametrize("rows,cols", [(6, 100), (400, 600), (5, 9000)])
+def test_a_gradient_that_is_missing_is_zero_whatever_it_would_be_multiplied_by(rows, cols):
+    """Without dn nothing of the first norm is needed: neither an infinite weight nor what rstd holds reaches a result."""
+    J = Join(rows, cols, gate=A.TOKEN)
+    join = J.join()
+    apm.apm_norm_join_forward(join)
+    J.w1[3], J.w1[40] = INF, float("nan")
+    J.r1.fill_(float("nan"))
+    apm.apm_norm_join_backward(join, J.grads(join, dn=None), room_for(rows, cols))
+    want = J.scale * J.dy.float()
+    assert bool(((J.dx.float() - want).abs() <= 2.0 ** -8 * want.abs()).all())
+    for t in (J.dbranch, J.dgate, J.dw2, J.db2):
+        assert bool(torch.isfinite(t).all())
+    assert bool((J.dw1 == 0).all()) and bool((J.db1 == 0).all())
