@@ -378,6 +378,12 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
                     for (int i = 0; i < kVec; ++i) D[v][i] = r1 * (D[v][i] - fmaf(z[v][i], k, m));
             }
         }
+        if (!there) {  // a team without a row adds nothing to the sums, also where a weight is infinite
+#pragma unroll
+            for (int v = 0; v < VECS; ++v)
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) D[v][i] = 0.0f;
+        }
 #pragma unroll
         for (int v = 0; v < VECS; ++v) {
             float o[kVec];

@@ -126,3 +126,23 @@ def test_a_gradient_that_is_missing_is_zero_whatever_it_would_be_multiplied_by(r
     for t in (J.dbranch, J.dgate, J.dw2, J.db2):
         assert bool(torch.isfinite(t).all())
     assert bool((J.dw1 == 0).all()) and bool((J.db1 == 0).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 100), (5, 100), (5, 700), (300, 100), (301, 700), (771, 2000), (3, 9000)])
+@pytest.mark.parametrize("gate", [A.CHANNEL, A.TOKEN])
+def test_rows_that_are_not_there_add_nothing_under_an_infinite_weight(rows, cols, gate):
+    """Without a first norm D = dy + dn pre.weight: with a weight of +inf, and dn and hat2 positive, the sums over rows are +inf, whatever their number."""
+    J = Join(rows, cols, F32, F32, F32, pre=A.NONE, gate=gate)
+    J.branch.abs_().add_(0.1)
+    J.dn.abs_().add_(0.1)
+    J.gate.abs_().add_(0.1)
+    join = J.join()
+    apm.apm_norm_join_forward(join)
+    J.w1[3] = INF
+    J.w2[3] = 0.5
+    J.kept2[0][:, 3] = 64                                           # in I8: 1 times the block's scale
+    apm.apm_norm_join_backward(join, J.grads(join), room_for(rows, cols))
+    for t in (J.dw2, J.db2):
+        assert float(t[3]) == INF
+    others = torch.arange(cols, device=DEV) != 3
+    assert bool(torch.isfinite(J.dw2[others]).all()) and bool(torch.isfinite(J.db2[others]).all()) and bool((J.dx[:, 3] == INF).all())
