@@ -570,7 +570,7 @@ int check_join(const apm_norm_join& j) {
     if (j.gate_kind == APM_GATE_NONE ? j.gate.data != nullptr : !j.gate.data && (j.rows > 0 || j.gate_kind == APM_GATE_CHANNEL)) return fail(APM_EINVAL, "gate and gate_kind contradict each other");
     int rc = check_norm("pre", j.pre, j.rows, j.cols);
     if (rc == APM_OK) rc = check_norm("post", j.post, j.rows, j.cols);
-    if (rc == APM_OK && j.gate.data) rc = check_matrix("gate", j.gate, j.rows, j.cols, false);
+    if (rc == APM_OK && j.gate.data) rc = check_matrix("gate", j.gate, j.gate_kind == APM_GATE_CHANNEL ? 1 : j.rows, j.cols, false);
     return rc;
 }
 
