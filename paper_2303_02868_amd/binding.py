@@ -765,7 +765,11 @@ def apm_norm_join_workspace_bytes(rows: int, cols: int) -> int:
 
 
 def _room(workspace):
-    return (None, 0) if workspace is None else (_on_gpu("workspace", workspace), workspace.numel() * workspace.element_size())
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():      # its size would not be what lies behind its address
+        raise ValueError(f"workspace: {tuple(workspace.shape)} with strides {workspace.stride()}, contiguous memory is needed")
+    return _on_gpu("workspace", workspace), workspace.numel() * workspace.element_size()
 
 
 def apm_norm_join_backward(join: apm_norm_join, grads: apm_norm_join_grads, workspace, stream=None) -> None:
