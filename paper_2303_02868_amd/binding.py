@@ -624,9 +624,9 @@ def apm_pool_read_timing(pool: Pool):
 
 
 # ---- activations --------------------------------------------------------------------------------
-# Tensors in, raw structures out: these look at shapes, strides, types and memory, which the structures do not all carry.  The large
-# structures are packed in one go: field by field they cost more than the smallest calls' kernels (a join of eight tokens, us of
-# host time: 33 field by field, 19 packed).
+# Tensors in, raw structures out: these look at shapes, strides, types and memory (that of the current device, on which the calls'
+# kernels run), which the structures do not all carry.  The large structures are packed in one go: field by field they cost more than
+# the smallest calls' kernels (a join of eight tokens, us of host time: 33 field by field, 19 packed).
 
 _DTYPES: dict = {}
 _NO_MATRIX, _NO_VECTOR, _NO_CKPT = (0, 0, 0, 0), (0, 0, 0), (0, 0, 0, 0, 0, 0)
@@ -647,42 +647,70 @@ def _dtype(t) -> int:
     return code
 
 
-def _on_gpu(name, t) -> int:
-    if not t.is_cuda and not t.is_pinned():
+_current_device = None
+
+
+def _here():
+    """The current device, on which a call's kernels run; None where the process has one GPU and nothing to tell apart (looking costs the smallest
+    calls 0.5 to 1 us of 6 to 16), -2 where none is in use."""
+    return _first_here() if _current_device is None else _current_device()
+
+
+def _first_here():
+    global _current_device
+    import torch
+    if not torch.cuda.is_initialized():
+        return -2
+    _current_device = torch.cuda.current_device if torch.cuda.device_count() > 1 else lambda: None
+    return _current_device()
+
+
+def _elsewhere(name, t, here) -> int:
+    device = t.get_device()                # -1: host memory
+    if device >= 0:                        # with several GPUs in use
+        raise ValueError(f"{name} is on GPU {device}, the current one is {here}")
+    if not t.is_pinned():
         raise ValueError(f"{name} is in memory that the GPU cannot address")
     return t.data_ptr()
 
 
-def _matrix(name, t, rows, cols):
+def _same_gpu(made, here) -> None:
+    if made != here and made is not None:  # None: a structure that its owner filled by hand
+        raise ValueError(f"the tensors were looked at for GPU {made}, the current one is {here}")
+
+
+def _matrix(name, t, rows, cols, here):
     if t is None:
         return _NO_MATRIX
     stride, code = t.stride(), _DTYPES.get(t.dtype)
     if t.shape != (rows, cols) or (stride[1] != 1 and cols > 1):
         raise ValueError(f"{name}: {tuple(t.shape)} with strides {stride}, {rows} rows of {cols} contiguous elements are needed")
-    return t.data_ptr() if t.is_cuda else _on_gpu(name, t), stride[0], _dtype(t) if code is None else code, 0
+    at = t.data_ptr() if (t.is_cuda if here is None else t.get_device() == here) else _elsewhere(name, t, here)
+    return at, stride[0], _dtype(t) if code is None else code, 0
 
 
-def _vector(name, t, n):
+def _vector(name, t, n, here):
     if t is None:
         return _NO_VECTOR
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()}, {n} contiguous elements are needed")
     code = _DTYPES.get(t.dtype)
-    return t.data_ptr() if t.is_cuda else _on_gpu(name, t), _dtype(t) if code is None else code, 0
+    at = t.data_ptr() if (t.is_cuda if here is None else t.get_device() == here) else _elsewhere(name, t, here)
+    return at, _dtype(t) if code is None else code, 0
 
 
 def make_matrix(name: str, t, rows: int, cols: int) -> apm_matrix:
     """The apm_matrix of a two-dimensional tensor (None: not given) that has to be rows x cols."""
-    return apm_matrix(*_matrix(name, t, rows, cols))
+    return apm_matrix(*_matrix(name, t, rows, cols, _here()))
 
 
 def make_vector(name: str, t, n: int) -> apm_vector:
-    return apm_vector(*_vector(name, t, n))
+    return apm_vector(*_vector(name, t, n, _here()))
 
 
 class Ckpt:
     """An 8-bit matrix: the tensors, and the words of its apm_ckpt."""
-    __slots__ = ("shape", "words", "tensors")
+    __slots__ = ("shape", "words", "tensors", "device")
 
 
 def make_ckpt(q, scale, format: int) -> Ckpt:
@@ -693,36 +721,42 @@ def make_ckpt(q, scale, format: int) -> Ckpt:
     q_stride, s_stride = q.stride(), scale.stride()
     if q.element_size() != 1 or scale.element_size() != 1 or scale.shape != (rows, nb) or (q_stride[1] != 1 and cols > 1) or (s_stride[1] != 1 and nb > 1):
         raise ValueError(f"an 8-bit matrix of {tuple(q.shape)} needs bytes, and scales of {(rows, nb)}: got {tuple(scale.shape)}")
-    c.words = (q.data_ptr() if q.is_cuda else _on_gpu("q", q), scale.data_ptr() if scale.is_cuda else _on_gpu("scale", scale),
+    here = c.device = _here()
+    c.words = (q.data_ptr() if (q.is_cuda if here is None else q.get_device() == here) else _elsewhere("q", q, here),
+               scale.data_ptr() if (scale.is_cuda if here is None else scale.get_device() == here) else _elsewhere("scale", scale, here),
                q_stride[0], s_stride[0], format, 0)
     c.tensors = q, scale
     return c
 
 
-def _ckpt_words(name, c, rows, cols):
+def _ckpt_words(name, c, rows, cols, here):
     if c is None:
         return _NO_CKPT
     if c.shape != (rows, cols):
         raise ValueError(f"{name}: {tuple(c.shape)}, {(rows, cols)} is needed")
+    if c.device != here:
+        _same_gpu(c.device, here)
     return c.words
 
 
 def apm_ckpt_write(x, ckpt: Ckpt, stream=None) -> None:
-    rows, cols = ckpt.shape
-    _check(lib().apm_ckpt_write(rows, cols, apm_matrix(*_matrix("x", x, rows, cols)), apm_ckpt(*ckpt.words), _stream(stream)))
+    (rows, cols), here = ckpt.shape, _here()
+    _check(lib().apm_ckpt_write(rows, cols, apm_matrix(*_matrix("x", x, rows, cols, here)), apm_ckpt(*_ckpt_words("ckpt", ckpt, rows, cols, here)),
+                                _stream(stream)))
 
 
 def apm_ckpt_read(ckpt: Ckpt, x, stream=None) -> None:
-    rows, cols = ckpt.shape
-    _check(lib().apm_ckpt_read(rows, cols, apm_ckpt(*ckpt.words), apm_matrix(*_matrix("x", x, rows, cols)), _stream(stream)))
+    (rows, cols), here = ckpt.shape, _here()
+    _check(lib().apm_ckpt_read(rows, cols, apm_ckpt(*_ckpt_words("ckpt", ckpt, rows, cols, here)), apm_matrix(*_matrix("x", x, rows, cols, here)),
+                               _stream(stream)))
 
 
 def _gate_shape(kind, rows, cols):
     return (1, cols) if kind == APM_GATE_CHANNEL else (rows, 1) if kind == APM_GATE_TOKEN else (rows, cols)
 
 
-def _rstd(name, t, rows):
-    data, dtype, _ = _vector(name, t, rows)
+def _rstd(name, t, rows, here):
+    data, dtype, _ = _vector(name, t, rows, here)
     if t is not None and dtype != APM_F32:
         raise ValueError(f"{name} must be float32")
     return data
@@ -732,14 +766,15 @@ def make_norm_join(rows: int, cols: int, *, x=None, branch=None, y=None, n=None,
                    pre_norm=APM_NORM_NONE, pre_eps=0.0, pre_weight=None, pre_bias=None, pre_ckpt=None, pre_rstd=None,
                    post_norm=APM_NORM_NONE, post_eps=0.0, post_weight=None, post_bias=None, post_ckpt=None, post_rstd=None) -> apm_norm_join:
     """What apm_norm_join_forward and _backward work on.  The tensors are kept alive by it."""
+    here = _here()
     j = apm_norm_join.from_buffer_copy(_pack_join(
-        rows, cols, residual_scale, *_matrix("x", x, rows, cols), *_matrix("branch", branch, rows, cols), *_matrix("y", y, rows, cols),
-        *_matrix("n", n, rows, cols), *_matrix("gate", gate, *_gate_shape(gate_kind, rows, cols)), gate_kind, 0,
-        pre_norm, 0, pre_eps, *_vector("pre_weight", pre_weight, cols), *_vector("pre_bias", pre_bias, cols),
-        *_ckpt_words("pre_ckpt", pre_ckpt, rows, cols), _rstd("pre_rstd", pre_rstd, rows),
-        post_norm, 0, post_eps, *_vector("post_weight", post_weight, cols), *_vector("post_bias", post_bias, cols),
-        *_ckpt_words("post_ckpt", post_ckpt, rows, cols), _rstd("post_rstd", post_rstd, rows)))
-    j.shape, j.kind = (rows, cols), gate_kind
+        rows, cols, residual_scale, *_matrix("x", x, rows, cols, here), *_matrix("branch", branch, rows, cols, here),
+        *_matrix("y", y, rows, cols, here), *_matrix("n", n, rows, cols, here), *_matrix("gate", gate, *_gate_shape(gate_kind, rows, cols), here), gate_kind, 0,
+        pre_norm, 0, pre_eps, *_vector("pre_weight", pre_weight, cols, here), *_vector("pre_bias", pre_bias, cols, here),
+        *_ckpt_words("pre_ckpt", pre_ckpt, rows, cols, here), _rstd("pre_rstd", pre_rstd, rows, here),
+        post_norm, 0, post_eps, *_vector("post_weight", post_weight, cols, here), *_vector("post_bias", post_bias, cols, here),
+        *_ckpt_words("post_ckpt", post_ckpt, rows, cols, here), _rstd("post_rstd", post_rstd, rows, here)))
+    j.shape, j.kind, j.device = (rows, cols), gate_kind, here
     j.tensors = (x, branch, y, n, gate, pre_weight, pre_bias, pre_ckpt, pre_rstd, post_weight, post_bias, post_ckpt, post_rstd)
     return j
 
@@ -747,16 +782,20 @@ def make_norm_join(rows: int, cols: int, *, x=None, branch=None, y=None, n=None,
 def make_norm_join_grads(join: apm_norm_join, *, dn=None, dy=None, dx=None, dbranch=None, dgate=None, dpre_weight=None, dpre_bias=None,
                          dpost_weight=None, dpost_bias=None) -> apm_norm_join_grads:
     """dgate has the gate's shape."""
-    rows, cols = join.shape
+    (rows, cols), here = join.shape, _here()
+    _same_gpu(join.device, here)
     g = apm_norm_join_grads.from_buffer_copy(_pack_grads(
-        *_matrix("dn", dn, rows, cols), *_matrix("dy", dy, rows, cols), *_matrix("dx", dx, rows, cols), *_matrix("dbranch", dbranch, rows, cols),
-        *_matrix("dgate", dgate, *_gate_shape(join.kind, rows, cols)), *_vector("dpre_weight", dpre_weight, cols), *_vector("dpre_bias", dpre_bias, cols),
-        *_vector("dpost_weight", dpost_weight, cols), *_vector("dpost_bias", dpost_bias, cols)))
+        *_matrix("dn", dn, rows, cols, here), *_matrix("dy", dy, rows, cols, here), *_matrix("dx", dx, rows, cols, here),
+        *_matrix("dbranch", dbranch, rows, cols, here), *_matrix("dgate", dgate, *_gate_shape(join.kind, rows, cols), here),
+        *_vector("dpre_weight", dpre_weight, cols, here), *_vector("dpre_bias", dpre_bias, cols, here),
+        *_vector("dpost_weight", dpost_weight, cols, here), *_vector("dpost_bias", dpost_bias, cols, here)))
     g.tensors = (dn, dy, dx, dbranch, dgate, dpre_weight, dpre_bias, dpost_weight, dpost_bias)
+    g.device = here
     return g
 
 
 def apm_norm_join_forward(join: apm_norm_join, stream=None) -> None:
+    _same_gpu(getattr(join, "device", None), _here())
     _check(lib().apm_norm_join_forward(join, _stream(stream)))
 
 
@@ -764,30 +803,36 @@ def apm_norm_join_workspace_bytes(rows: int, cols: int) -> int:
     return lib().apm_norm_join_workspace_bytes(rows, cols)
 
 
-def _room(workspace):
+def _room(workspace, here):
     if workspace is None:
         return None, 0
     if not workspace.is_contiguous():      # its size would not be what lies behind its address
         raise ValueError(f"workspace: {tuple(workspace.shape)} with strides {workspace.stride()}, contiguous memory is needed")
-    return _on_gpu("workspace", workspace), workspace.numel() * workspace.element_size()
+    at = workspace.data_ptr() if (workspace.is_cuda if here is None else workspace.get_device() == here) else _elsewhere("workspace", workspace, here)
+    return at, workspace.numel() * workspace.element_size()
 
 
 def apm_norm_join_backward(join: apm_norm_join, grads: apm_norm_join_grads, workspace, stream=None) -> None:
-    _check(lib().apm_norm_join_backward(join, grads, *_room(workspace), _stream(stream)))
+    here = _here()
+    _same_gpu(getattr(grads, "device", None), here)
+    _check(lib().apm_norm_join_backward(join, grads, *_room(workspace, here), _stream(stream)))
 
 
 def make_weight_grad(dy, kept: Ckpt, dw, *, db=None, weight=None, bias=None, offsets=None, accumulate=False) -> apm_weight_grad:
     """dw: [out, in], or with offsets (int64, groups + 1) [groups, out, in]; db: [out] or [groups, out]."""
-    tokens, k = kept.shape
+    (tokens, k), here = kept.shape, _here()
     out, groups, at = dy.shape[1], 0, 0
     if offsets is not None:
-        groups, at = offsets.numel() - 1, _on_gpu("offsets", offsets)
+        groups = offsets.numel() - 1
+        at = offsets.data_ptr() if (offsets.is_cuda if here is None else offsets.get_device() == here) else _elsewhere("offsets", offsets, here)
         if str(offsets.dtype) != "torch.int64" or not offsets.is_contiguous() or groups < 1 or dw.dim() != 3 or dw.shape[0] != groups:
             raise ValueError(f"offsets {offsets.dtype} of {tuple(offsets.shape)} for gradients of {tuple(dw.shape)}")
     w = apm_weight_grad.from_buffer_copy(_pack_weight_grad(
-        tokens, out, k, groups, at, *_matrix("dy", dy, tokens, out), *kept.words, *_vector("weight", weight, k), *_vector("bias", bias, k),
-        *_matrix("dw", dw[0] if groups else dw, out, k), dw.stride(0) if groups else 0, *_vector("db", db, max(1, groups) * out), int(accumulate), 0))
+        tokens, out, k, groups, at, *_matrix("dy", dy, tokens, out, here), *_ckpt_words("kept", kept, tokens, k, here),
+        *_vector("weight", weight, k, here), *_vector("bias", bias, k, here), *_matrix("dw", dw[0] if groups else dw, out, k, here),
+        dw.stride(0) if groups else 0, *_vector("db", db, max(1, groups) * out, here), int(accumulate), 0))
     w.tensors = (dy, kept, dw, db, weight, bias, offsets)
+    w.device = here
     return w
 
 
@@ -796,4 +841,6 @@ def apm_ckpt_weight_grad_workspace_bytes(grad: apm_weight_grad) -> int:
 
 
 def apm_ckpt_weight_grad(grad: apm_weight_grad, workspace=None, stream=None) -> None:
-    _check(lib().apm_ckpt_weight_grad(grad, *_room(workspace), _stream(stream)))
+    here = _here()
+    _same_gpu(getattr(grad, "device", None), here)
+    _check(lib().apm_ckpt_weight_grad(grad, *_room(workspace, here), _stream(stream)))
