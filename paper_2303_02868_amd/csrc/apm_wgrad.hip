@@ -601,3 +601,8 @@ extern "C" size_t apm_ckpt_weight_grad_workspace_bytes(const apm_weight_grad* w)
 extern "C" int apm_ckpt_weight_grad(const apm_weight_grad* w, void* workspace, size_t workspace_bytes, void* stream) {
     return apm::guarded([&]() -> int { return apm::weight_grad(w, workspace, workspace_bytes, stream); });
 }
+
+extern "C" int apm_test_weight_grad_tile(const apm_weight_grad* w) {
+    constexpr int kSide[] = {apm::Large::kOut, apm::Small::kOut, apm::Tiny::kOut};
+    return !w || apm::check_grad(*w) != APM_OK ? 0 : kSide[apm::wgrad_shape(*w).which];
+}

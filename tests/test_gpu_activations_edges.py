@@ -1,5 +1,7 @@
-"""The activation calls where values leave the number range, and where rows are very wide."""
+"""The activation calls where values leave the number range, where rows are very wide, and on every path of the weight gradients."""
 from __future__ import annotations
+
+import ctypes as C
 
 import numpy as np
 import pytest
@@ -7,7 +9,7 @@ import torch
 
 import oracle.activations as A
 import paper_2303_02868_amd as apm
-from test_gpu_activations import BF16, DEV, F32, Join, f64, kept_blank, random_kept, room_for
+from test_gpu_activations import BF16, DEV, F32, Join, check_weight_grad, f64, kept_blank, random_kept, room_for
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -146,3 +148,59 @@ def test_rows_that_are_not_there_add_nothing_under_an_infinite_weight(rows, cols
         assert float(t[3]) == INF
     others = torch.arange(cols, device=DEV) != 3
     assert bool(torch.isfinite(J.dw2[others]).all()) and bool(torch.isfinite(J.db2[others]).all()) and bool((J.dx[:, 3] == INF).all())
+
+
+# ---- weight gradients: every tile, with and without parts ---------------------------------------
+
+def path(tokens, out, k, groups=0):
+    """The tile that the rule takes for a shape, and into how many parts it splits the tokens."""
+    g = apm.apm_weight_grad()
+    g.tokens, g.out, g.n_groups, g.offsets, g.dw_group_stride = tokens, out, groups, 4096 if groups else None, out * k
+    setattr(g, "in", k)
+    g.dy, g.kept, g.dw = apm.apm_matrix(4096, out, apm.APM_BF16, 0), apm.apm_ckpt(4096, 4096, k, -(-k // 32), 0, 0), apm.apm_matrix(4096, k, apm.APM_F32, 0)
+    size = apm.apm_ckpt_weight_grad_workspace_bytes(g)
+    return apm.lib().apm_test_weight_grad_tile(C.byref(g)), max(1, size // (4 * max(1, groups) * out * (k + 1)))
+
+
+def shares(tokens, groups):
+    """Uneven groups, the second of them empty."""
+    if not groups:
+        return None
+    cut = np.sort(np.random.default_rng(tokens).integers(0, tokens, groups - 1)).tolist()
+    offsets = [0] + cut + [tokens]
+    offsets[2] = offsets[1] if groups > 2 else offsets[2]
+    return offsets if groups > 2 else [0, 0, tokens]
+
+
+SHAPES = [  # tile, parts, tokens, out, in, groups
+    (256, 1, 700, 2100, 4000, 0), (256, 1, 1500, 520, 2000, 8), (256, 3, 3000, 2100, 2100, 0), (256, 3, 6000, 1500, 1500, 2),
+    (128, 1, 500, 1000, 4000, 0), (128, 1, 1500, 200, 4000, 4), (128, 4, 4000, 130, 4000, 0), (128, 4, 6000, 200, 2000, 2),
+    (64, 1, 500, 130, 300, 0), (64, 1, 500, 130, 130, 3), (64, 6, 700, 130, 130, 0), (64, 6, 1500, 200, 130, 2),
+]
+
+
+@pytest.mark.parametrize("tile,parts,tokens,out,k,groups", SHAPES)
+@pytest.mark.parametrize("fmt,dtype,weight,bias,db,accumulate", [(A.I8, F32, True, True, True, False), (A.F8, BF16, False, False, False, False),
+                                                                  (A.F8, F32, True, False, True, True), (A.I8, BF16, True, False, False, True)])
+def test_every_tile_with_and_without_parts(tile, parts, tokens, out, k, groups, fmt, dtype, weight, bias, db, accumulate):
+    assert path(tokens, out, k, groups) == (tile, parts)
+    check_weight_grad(tokens, out, k, fmt, dtype, weight, bias, db, offsets=shares(tokens, groups), accumulate=accumulate)
+
+
+@pytest.mark.parametrize("tile,parts,tokens,out,k,groups", [s for s in SHAPES if s[5]])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_groups_without_tokens_take_no_weight_and_no_bias(tile, parts, tokens, out, k, groups, accumulate):
+    assert path(tokens, out, k, groups) == (tile, parts)
+    kept, _ = random_kept(tokens, k, A.I8, 2)
+    dy = torch.randn(tokens, out, device=DEV).bfloat16()
+    w = torch.full((k,), INF, device=DEV)
+    old = 3.0 if accumulate else 0.0
+    dw, db = torch.full((groups, out, k), 3.0, device=DEV), torch.full((groups, out), 3.0, device=DEV)
+    grad = apm.make_weight_grad(dy, apm.make_ckpt(*kept, A.I8), dw, db=db, weight=w, bias=w, offsets=torch.tensor(shares(tokens, groups), device=DEV),
+                                accumulate=accumulate)
+    size = apm.apm_ckpt_weight_grad_workspace_bytes(grad)
+    assert (size > 0) == (parts > 1)
+    apm.apm_ckpt_weight_grad(grad, torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV) if size else None)
+    empty = 1 if groups > 2 else 0
+    assert bool((dw[empty] == old).all()) and bool((db[empty] == old).all())
+    assert not bool(torch.isfinite(dw[-1]).any())
