@@ -7,7 +7,7 @@ A block is u = n W1^T, a = max(u, 0)^2, branch = a W2^T between two joins.  Join
 and a gate, and normalises the stream for the block behind it:
     y_i = y_(i-1) + gate_i post_i(branch_i),    n_i = pre_i(y_i)
 The backward pass finds everything in 8 bits: the joins their normalised tensors, the activation function u, and the two weight gradients
-of a block the a and the normalised stream that its products were fed.  Matrix products that are no operator of the library
+of a block the a and the normalised stream that its products were fed.  It reads neither y nor n, of which there is one buffer each.  Matrix products that are no operator of the library
 (forward, and gradients of activations) are torch's.  The task: another random network's output.
 """
 import argparse
@@ -66,12 +66,12 @@ class Network:
             return torch.empty(tokens, cols, dtype=dtype, device=DEV)
 
         v, g = self.p.value, self.p.grad
-        self.y = [make(width, torch.float32) for _ in range(blocks + 1)]     # the residual stream
-        self.n = [make(width) for _ in range(blocks + 1)]
+        self.y, self.n = make(width, torch.float32), make(width)             # the residual stream, and what goes into the next block
         self.u_kept = [kept_like(tokens, hidden, form) for _ in range(blocks)]
         self.a_kept = [kept_like(tokens, hidden, form) for _ in range(blocks)]
-        self.hats = [(kept_like(tokens, width, form), kept_like(tokens, width, form)) for _ in range(blocks + 1)]
-        self.rstd = [(torch.empty(tokens, device=DEV), torch.empty(tokens, device=DEV)) for _ in range(blocks + 1)]
+        # of the stream behind each join, and of the branches, which join 0 has none of
+        self.hats, self.branch_hats = [kept_like(tokens, width, form) for _ in range(blocks + 1)], [kept_like(tokens, width, form) for _ in range(blocks)]
+        self.rstd, self.branch_rstd = ([torch.empty(tokens, device=DEV) for _ in range(n)] for n in (blocks + 1, blocks))
         self.branch, self.u_back = make(width), make(hidden)
         self.dy, self.dn, self.dbranch = make(width, torch.float32), make(width), make(width)
         # All buffers stay where they are, so what the calls are told is made once.
@@ -80,25 +80,25 @@ class Network:
             more = {}
             if i > 0:
                 more = dict(branch=self.branch, gate_kind=apm.APM_GATE_CHANNEL, gate=v[f"{i}.gate"], post_norm=apm.APM_NORM_RMS, post_eps=EPS,
-                            post_weight=v[f"{i}.post"], post_ckpt=self.hats[i][1], post_rstd=self.rstd[i][1])
-            join = apm.make_norm_join(tokens, width, x=self.y[max(0, i - 1)], y=self.y[i] if i > 0 else None, n=self.n[i], pre_norm=apm.APM_NORM_RMS,
-                                      pre_eps=EPS, pre_weight=v[f"{i}.pre"], pre_ckpt=self.hats[i][0], pre_rstd=self.rstd[i][0], **more)
+                            post_weight=v[f"{i}.post"], post_ckpt=self.branch_hats[i - 1], post_rstd=self.branch_rstd[i - 1], y=self.y)
+            join = apm.make_norm_join(tokens, width, x=self.y, n=self.n, pre_norm=apm.APM_NORM_RMS, pre_eps=EPS, pre_weight=v[f"{i}.pre"],
+                                      pre_ckpt=self.hats[i], pre_rstd=self.rstd[i], **more)
             more = dict(dbranch=self.dbranch, dgate=g[f"{i}.gate"], dpost_weight=g[f"{i}.post"]) if i > 0 else {}
             self.joins.append(join)
             self.grads.append(apm.make_norm_join_grads(join, dn=self.dn, dy=self.dy if i < blocks else None, dx=self.dy, dpre_weight=g[f"{i}.pre"], **more))
         self.room = torch.empty(apm.apm_norm_join_workspace_bytes(tokens, width), dtype=torch.uint8, device=DEV)
 
     def forward(self, x):
-        self.y[0].copy_(x)
+        self.y.copy_(x)
         for i, join in enumerate(self.joins):
             if i > 0:
-                u = self.n[i - 1] @ self.p.value[f"{i}.w1"].T
+                u = self.n @ self.p.value[f"{i}.w1"].T
                 a = u.relu().square()
                 apm.apm_ckpt_write(u, self.u_kept[i - 1])
                 apm.apm_ckpt_write(a, self.a_kept[i - 1])
                 torch.matmul(a, self.p.value[f"{i}.w2"].T, out=self.branch)
             apm.apm_norm_join_forward(join)
-        return self.n[-1]
+        return self.n
 
     def weight_gradient(self, dy, kept, name, weight=None):
         grad = apm.make_weight_grad(dy, kept, self.p.grad[name], weight=weight)
@@ -113,19 +113,20 @@ class Network:
                 self.weight_gradient(self.dbranch, self.a_kept[i - 1], f"{i}.w2")
                 apm.apm_ckpt_read(self.u_kept[i - 1], self.u_back)
                 du = (self.dbranch @ self.p.value[f"{i}.w2"]) * (2 * self.u_back.relu())
-                self.weight_gradient(du, self.hats[i - 1][0], f"{i}.w1", weight=self.p.value[f"{i - 1}.pre"])
+                self.weight_gradient(du, self.hats[i - 1], f"{i}.w1", weight=self.p.value[f"{i - 1}.pre"])
                 torch.matmul(du, self.p.value[f"{i}.w1"], out=self.dn)
 
-    def kept_bytes(self):
-        pairs = [p for h in self.hats for p in h] + self.u_kept + self.a_kept
-        return sum(t.numel() for c in pairs for t in c.tensors)
+    def kept(self):
+        """(elements, bytes) of what the forward pass leaves for the backward pass; for each row of a hat 4 bytes of rstd."""
+        kept = self.hats + self.branch_hats + self.u_kept + self.a_kept
+        return sum(c.tensors[0].numel() for c in kept), sum(t.numel() for c in kept for t in c.tensors) + 4 * sum(r.numel() for r in self.rstd + self.branch_rstd)
 
 
 def train(steps=40, tokens=2048, width=512, hidden=1024, blocks=3, form=apm.APM_CKPT_I8, lr=2e-3, seed=0, say=print):
     net, teacher = Network(tokens, width, hidden, blocks, form, seed), Network(tokens, width, hidden, blocks, form, seed + 1)
     g = torch.Generator(device=DEV).manual_seed(seed + 2)
-    elems = sum(c.tensors[0].numel() for c in [h for pair in net.hats for h in pair] + net.u_kept + net.a_kept)
-    say(f"{sum(net.p.numels)} parameters in {net.p.pages} pages; kept for the backward pass: {net.kept_bytes() / 1e6:.1f} MB, in bf16 it were {2 * elems / 1e6:.1f}")
+    elems, size = net.kept()
+    say(f"{sum(net.p.numels)} parameters in {net.p.pages} pages; kept for the backward pass: {size / 1e6:.1f} MB, elements in bf16 would be {2 * elems / 1e6:.1f}")
     losses = []
     for step in range(steps):
         x = torch.randn(tokens, width, device=DEV, generator=g)
