@@ -692,7 +692,9 @@ enum apm_ckpt_format {
  * element of the block is rounded to a value out of range (none is saturated; s = 254 at most, where the largest
  * floats are).  A block that holds an infinity or a NaN has s = 255 and stands for NaN throughout.  Elements are rounded
  * to nearest, ties to even: I8 elements are off by at most 1/255 to 1/127 of the block's largest (by where that lies between two
- * powers of two), F8 elements by 2^-4 of their own size, or less than 2^-17 of the block's largest.  The values are bf16 numbers.
+ * powers of two), F8 elements by 2^-4 of their own size, or less than 2^-17 of the block's largest.  The values are bf16 numbers, but for
+ * those of F8 blocks with s < 3 (largest element below 2^-116), whose last digits may lie below bf16's smallest 2^-133, and 2^128, to which F8
+ * rounds the very largest floats.
  * q: rows of cols bytes, q_stride >= cols apart.  scale: rows of ceil(cols / 32) bytes, scale_stride apart.  Each lies in one allocation, as
  * an apm_matrix does.
  */
@@ -705,8 +707,8 @@ typedef struct {
     int32_t reserved;
 } apm_ckpt;
 
-/* x (bf16 or fp32) into 8 bits, and back, rounded to x's type: exact, but that 2^128, to which F8 rounds the very largest floats, is
- * read as an infinity.  rows == 0 does nothing. */
+/* x (bf16 or fp32) into 8 bits, and back, rounded to nearest in x's type: exact in fp32, and in bf16 where the values are bf16 numbers,
+ * but that 2^128 is read as an infinity.  cols: at most 2^31 - 33.  rows == 0 does nothing. */
 int apm_ckpt_write(int64_t rows, int64_t cols, const apm_matrix* x, const apm_ckpt* c, void* stream);
 int apm_ckpt_read(int64_t rows, int64_t cols, const apm_ckpt* c, const apm_matrix* x, void* stream);
 
@@ -786,8 +788,10 @@ int apm_norm_join_backward(const apm_norm_join* j, const apm_norm_join_grads* g,
  * n_groups > 0: that many such products, each over the tokens of its group: group g has tokens offsets[g] .. offsets[g+1] - 1
  * (n_groups + 1 device int64; read on the device, where anything outside [0, tokens] is taken as the end next to it and a group that would end before it
  * starts as empty).  dw is then [n_groups][out, in], dw_group_stride elements apart, db [n_groups][out] contiguous.  A group without tokens gets zeros.
- * accumulate: added to what dw and db hold, with one rounding.
- * Products are exact (kept values are bf16 numbers), sums fp32; weight and bias enter after the sum.  A second call gives the same bits.
+ * accumulate: added to what dw and db hold.  v weight + bias (sum of dy), with the sum v over the tokens, is rounded to fp32 once, the addition to
+ * what is there a second time, and the result to dw's type.
+ * Products are exact where they and their factors are zero or of size 2^-126 and up (smaller ones may be taken as zero), sums fp32; weight and
+ * bias enter after the sum, the bias only where it is not zero: elsewhere an infinite sum of dy does not reach dw.  A second call gives the same bits.
  * workspace: apm_ckpt_weight_grad_workspace_bytes(w) bytes (may be 0, as it is where the call would refuse w), 16-byte aligned, in use until
  * the call's work is done.
  */

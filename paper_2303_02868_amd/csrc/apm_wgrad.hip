@@ -1,6 +1,6 @@
 // Weight gradients of linear layers whose input was kept in 8 bits: dw[o, k] = sum over tokens of dy[t, o] z[t, k], one product or one
 // for each group of tokens.  On the matrix cores: the kept bytes become bf16 on their way into LDS, which is exact (a whole number of
-// seven bits, or a float of four, times a power of two), so products are exact and sums are fp32.  What the norm in front of the
+// seven bits, or a float of four, times a power of two; below 2^-126 it may become zero), so products are exact and sums are fp32.  What the norm in front of the
 // layer multiplies and adds per column enters after the sum: z = hat w + b gives (dy^T hat) w + (sum of dy) b.
 //
 // Both operands lie in memory with the tokens, over which is summed, as rows, so neither has the order that the matrix

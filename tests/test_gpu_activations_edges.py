@@ -204,3 +204,40 @@ def test_groups_without_tokens_take_no_weight_and_no_bias(tile, parts, tokens, o
     empty = 1 if groups > 2 else 0
     assert bool((dw[empty] == old).all()) and bool((db[empty] == old).all())
     assert not bool(torch.isfinite(dw[-1]).any())
+
+
+# ---- what the smallest and largest values become ------------------------------------------------
+
+@pytest.mark.parametrize("fmt", [A.I8, A.F8])
+def test_every_code_and_scale_read_to_bf16_is_the_nearest_bf16_number(fmt):
+    """Nothing is rounded but what no bf16 number is: F8 values under the scale bytes 0 to 2, and 2^128."""
+    q = torch.arange(256, device=DEV).to(torch.uint8).repeat(256, 1)
+    q[:, [128] if fmt == A.I8 else [127, 255]] = 0
+    s = torch.arange(256, device=DEV).to(torch.uint8)[:, None].repeat(1, 8).contiguous()
+    out = torch.empty(256, 256, dtype=BF16, device=DEV)
+    apm.apm_ckpt_read(apm.make_ckpt(q, s, fmt), out)
+    exact = A.decode(q.cpu().numpy(), s.cpu().numpy(), fmt)
+    with np.errstate(over="ignore"):
+        nearest = torch.from_numpy(exact.astype(np.float32)).bfloat16().double().numpy()
+    assert np.array_equal(f64(out), nearest, equal_nan=True)
+    rounded = ~np.isnan(exact) & (nearest != exact)
+    rows = np.unique(np.nonzero(rounded)[0]).tolist()
+    if fmt == A.I8:
+        assert rows == []
+    else:
+        assert rows[:3] == [0, 1, 2] and all(np.isinf(nearest[r][rounded[r]]).all() for r in rows[3:])
+
+
+def test_accumulation_rounds_as_stated():
+    """What is added to dw: v weight + bias (sum of dy) in one rounding to fp32, the sum with what is there in another, the type in a third."""
+    dy = torch.full((1, 1), 1.0, device=DEV).bfloat16()
+    kept = torch.full((1, 1), 64, dtype=torch.uint8, device=DEV), torch.full((1, 1), 127, dtype=torch.uint8, device=DEV)   # 1.0
+    w = torch.full((1,), 1 + 2.0 ** -23, device=DEV)
+    b = torch.full((1,), 2.0 ** -24, device=DEV)                   # w + b is a tie: 1 + 2^-22, the even one
+    for dtype, old, want in ((F32, 4.0, 5.0), (F32, 2.0 ** -23, 1 + 3 * 2.0 ** -23), (BF16, 2.0 ** -7, 1 + 2.0 ** -7), (BF16, 2.0 ** -8, 1 + 2.0 ** -7)):
+        dw, db = torch.full((1, 1), old, dtype=dtype, device=DEV), torch.full((1,), old, dtype=dtype, device=DEV)
+        grad = apm.make_weight_grad(dy, apm.make_ckpt(*kept, A.I8), dw, db=db, weight=w, bias=b, accumulate=True)
+        apm.apm_ckpt_weight_grad(grad)
+        step = torch.tensor(1 + 2.0 ** -22, device=DEV) + torch.tensor(old, device=DEV)        # each in fp32
+        assert float(dw) == float(step.to(dtype)) == want
+        assert float(db) == float((torch.tensor(1.0, device=DEV) + old).to(dtype))
