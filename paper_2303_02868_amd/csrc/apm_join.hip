@@ -446,15 +446,18 @@ __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs
                 team_sums<WAVE>(one, slots + 2 * kMaxWaves, in_team);
                 s[0] = one[0];
             }
-            if (through2) {  // without a norm hat2, which may be NaN, has no part in it
-                const float k = s[0] * a.inv_cols, m = mean2 ? s[1] * a.inv_cols : 0.0f;
+            const float k = s[0] * a.inv_cols, m = mean2 ? s[1] * a.inv_cols : 0.0f;
 #pragma unroll
-                for (int v = 0; v < VECS; ++v)
+            for (int v = 0; v < VECS; ++v) {
+                float o[kVec];
 #pragma unroll
-                    for (int i = 0; i < kVec; ++i) D[v][i] = r2 * (D[v][i] - fmaf(z[v][i], k, m));
+                for (int i = 0; i < kVec; ++i) o[i] = r2 * (D[v][i] - fmaf(z[v][i], k, m));
+                if (!through2) {  // without a norm hat2, which may be NaN, has no part in it
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) o[i] = D[v][i];
+                }
+                store_row<A>(a.g.dbranch, row, j.cols, there, l[v], o);
             }
-#pragma unroll
-            for (int v = 0; v < VECS; ++v) store_row<A>(a.g.dbranch, row, j.cols, there, l[v], D[v]);
         }
     }
     // The teams' sums of four columns, the `half`-th four of vector `vec` of the row
