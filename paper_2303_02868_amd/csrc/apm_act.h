@@ -150,7 +150,7 @@ struct RawAny {
 
 // A row as a buffer: what lies beyond it (or all of it, if there is no such row or matrix) reads as zero and is not written, so that every lane
 // loads and stores without a branch, and nothing waits for more than it needs.  The bound is checked for each 32-bit word of an access by itself: an
-// fp32 row may end anywhere.  Non-temporal: these streams are larger than the caches (gradients of a join of 8192 x 5120, fp32 stream: 119 us
+// fp32 row may end anywhere.  Non-temporal: these streams are larger than the caches (gradients of a join of 8192 x 5120, fp32 stream, when this was chosen: 119 us
 // with the default policy, 115 with non-temporal stores, 108.6 with loads too).
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 constexpr int kNT = 2;
@@ -233,7 +233,7 @@ __device__ __forceinline__ void store_short(uint8_t* p, int n, u32x2 w) {
 }
 
 // Row `row` of a matrix: load_row, and settle before the first look at it.  A bf16 row's last elements, fewer than eight, come as the end of the eight
-// that end with the row, where it has eight, and not one by one: a branch and a trip to memory for each took gradients of 8000 x 1501 71 us and not 42.
+// that end with the row, where it has eight, and not one by one: a branch and a trip to memory for each took gradients of 8000 x 1501 (RMS) 71 us and not 42.
 template <int CACHE = kNT> __device__ __forceinline__ u32x4 load_bf16(const void* data, int64_t byte_offset, int64_t cols, bool there, const LaneCols& l) {
     const bool eight = cols >= kVec;
     const int from = l.tail() && eight ? (int)cols - kVec : l.col;

@@ -41,7 +41,7 @@ namespace {
 // Loads are non-temporal where rows are aligned to them, stores of bf16 and bytes always: what a wavefront of fp32 stores with one
 // instruction are halves of cache lines, which then meet in memory.  16384 x 8192 bf16 into 8 bits 63-66 us = 6.2-6.4 TB/s, with the default policy 72;
 // 8192 x 20480 back 80 us = 6.3 TB/s, and 85; 8192 x 8192 back to fp32 102 us with non-temporal stores, 62 without; 16384 x 1001 into 8 bits 12.4 us with
-// non-temporal loads, 11.1 without.
+// non-temporal loads, 10.7 without.
 constexpr int kThreads = 256, kUnroll = 2;
 constexpr int kGroupBlocks = kThreads * kUnroll / kQuad;  // blocks of the 8-bit form that a workgroup takes
 

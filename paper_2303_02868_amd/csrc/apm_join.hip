@@ -251,7 +251,7 @@ struct RowRaw {
 // VECS 1: a lane has eight columns, and while a row is worked on the next one's loads are under way, so that the lanes of a CU's 16 wavefronts have two
 // rows' worth of loads out.  VECS 2, for rows that 16 wavefronts do not hold otherwise: no registers for either.
 // The first row is on its way before the weights are asked for, and they all before one of them is looked at (127 x 10215 in fp32: 54 us, so 42).
-// 8192 x 5120 with a fp32 stream: 106 us = 5.6 TB/s; of that 5 for the second kernel.
+// 8192 x 5120 with a fp32 stream: 106 us = 5.5 TB/s; of that 4.6 for the second kernel.
 constexpr int kSlotSums = 5;  // two for the first norm, three for the second and the gate
 template <class R, class A, int VECS, bool WAVE, bool BIAS, bool COLUMN, bool ONE>
 __global__ __launch_bounds__(kMaxThreads) void apm_join_backward_kernel(BackArgs a) {
@@ -635,8 +635,8 @@ int forward(const apm_norm_join* jp, void* stream) {
 }
 
 // How many workgroups walk the rows, and with how many teams: one workgroup a CU, of as many teams as 16 wavefronts make, so that there are few
-// sums of workgroups to add (16384 x 768, us: 50 with 16 wavefronts, 55 with workgroups of 4, of which four share a CU), but no more than all CUs
-// have rows for (256 x 768: 14.1 us with as many as there are, 10.5 with one).
+// sums of workgroups to add (16384 x 768, us when this was chosen: 50 with 16 wavefronts, 55 with workgroups of 4, of which four share a CU; with
+// LayerNorm and biases 42 now), but no more than all CUs have rows for (256 x 768: 14.1 us with as many as there are, 10.5 with one).
 constexpr int64_t kCus = 256;
 struct BackShape {
     int vecs, waves, teams;

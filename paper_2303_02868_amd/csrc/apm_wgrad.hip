@@ -30,10 +30,11 @@ struct Tile {
 };
 // 256 x 256: a byte that comes in is used most often, and one workgroup fills a CU's registers.  128 x 128: four times as many tiles, for small
 // dw; one set of registers more hides what the shorter work on a tile does not (256 x 256 over 16384 tokens by one workgroup each, us: 206
-// with one set, 181 with two).
+// with one set, 184 with two).
 typedef Tile<4, 2, 2, 4, 1> Large;
 typedef Tile<4, 2, 1, 2, 2> Small;
-// 64 x 64, of which four share a CU: the shortest way from the first load to the last store (1000 tokens x 768 x 768 11.3 us, by 128 x 128 in two parts 17.8).
+// 64 x 64, of which four share a CU: the shortest way from the first load to the last store (1000 tokens x 768 x 768 to fp32, without sums 11.3 us, by
+// 128 x 128 in two parts 16.5).
 // With one set of registers for later tiles 11.6 us there, and 2048 x 768 x 2304 (F8) 21.2 instead of 19.5; 64 tokens take 0.3 us more with two.
 typedef Tile<2, 2, 1, 1, 2> Tiny;
 
@@ -165,9 +166,10 @@ __device__ __forceinline__ void among_lanes() {
 constexpr int kXcds = 8;
 constexpr int kStrip = 4;  // rows of tiles that are walked together
 
-// Bound by what LDS gives (a fragment is read by transposing loads, at about 120 bytes a clock) beside the matrix cores, which are busy half the
-// time at 1.9 GHz: 1160 (I8) to 1180 TFLOP/s (F8) at 16384 tokens x 8192 x 2048, 508 and 495 us with sums; a library product of bf16 matrices in this
-// order reaches 960, in the order that suits it 1300.
+// 16384 tokens x 8192 x 2048: 495 us = 1110 TFLOP/s (I8), 483 (F8), with sums 536 and 533; a library product of bf16 matrices in this order 480, in the
+// order that suits it 369 (on another card 475, 507 with sums, and 462).  No unit alone bounds it: of a CU's cycles the matrix cores are busy for 54 %, other
+// vector instructions issue for 35 %, LDS works for 41 % (with transposing loads, which give about 120 bytes a clock, and a sixth of it conflicts), and
+// two wavefronts a SIMD overlap them in part.
 template <class T, int FORMAT, bool SUMS>
 __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
     constexpr int kRowA = T::kOut * 2, kRowB = T::kIn * 2, kTokens = T::kTokens, FO = T::FO, FK = T::FK, D = T::kDepth, kSteps = kTokens / kStep;
@@ -178,7 +180,7 @@ __global__ __launch_bounds__(T::kThreads) void apm_wgrad_kernel(WgradArgs a) {
     auto tile_b = [&](int buf) -> char* { return lds + 2 * kTileA + buf * kTileB; };
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     // Workgroups go to the XCDs in turn.  Each XCD takes a stretch of the order, in which tiles come strip by strip, so that its L2 meets few
-    // rows and columns (16384 x 8192 x 2048, TFLOP/s: 930 in launch order, 970 with strips of 4 rows, 920 of 16).
+    // rows and columns (16384 x 8192 x 2048, TFLOP/s when this was chosen: 930 in launch order, 970 with strips of 4 rows, 920 of 16).
     // Groups one after the other on all XCDs: they have different numbers of tokens.
     const uint32_t in_group = (uint32_t)(a.tiles * a.splits), nth = blockIdx.x % in_group, x = nth % kXcds;
     const uint32_t id = x * (in_group / kXcds) + min(x, in_group % kXcds) + nth / kXcds;
@@ -489,10 +491,11 @@ __global__ __launch_bounds__(kJoinThreads) void apm_wgrad_join_kernel(WgradArgs 
 }
 
 // Which tile, and into how many parts the tokens are split, so that few tiles fill the chip.  Estimated in us, from calls that were timed: a round of
-// workgroups costs `start`, and `turn` for each 64 tokens, or `busy` times the workgroups that share a CU where that is more (256 x 256 alone on a CU: 515 us
-// for 256 turns, 140 for 64, 18.7 for one; 128 x 128 alone: 181 for 256, 18.4 for 16; 64 x 64 with up to four: 156 for 256, 12.4 for 16, 45 for 32 with four).
-// Parts are written and read at 4 TB/s, by one kernel more.  With one part and the better split (tokens x out x in): 8192 x 768 x 768 97 / 30.5, 16384 x 256 x 256 by
-// 64 x 64 156 / 23, by 128 x 128 181 / 29; 8192 x 2048 x 2048 by 256 x 256 209 / 91, by 128 x 128 102 / 112.
+// workgroups costs `start`, and `turn` for each 64 tokens, or `busy` times the workgroups that share a CU where that is more (with sums; 256 x 256 alone on a CU:
+// 534 us for 256 turns, 140 for 64, 14.4 for one; 128 x 128 alone: 205 for 256, 18.4 for 16; 64 x 64 alone: 105 for 256, 12.7 for 16, four on a CU 44 for 32).
+// Parts are written and read at 4 TB/s, by one kernel more.  With one part and with several (tokens x out x in): 8192 x 768 x 768 97 / 28, 16384 x 256 x 256 by
+// 64 x 64 105 / 22, by 128 x 128 184 with one; 8192 x 2048 x 2048 by 256 x 256 212 / 91, by 128 x 128 103 / 117.  The constants are from an earlier state of the
+// tiles: they take a turn of 64 x 64 for 0.55 us, which is 0.41, and 256 x 256 in four parts for slower than 128 x 128 at the last size, where it is faster.
 constexpr int64_t kCus = 256, kMostSplits = 64;
 enum { kLarge, kSmall, kTiny };
 struct WgradShape {
