@@ -626,7 +626,8 @@ def apm_pool_read_timing(pool: Pool):
 # ---- activations --------------------------------------------------------------------------------
 # Tensors in, raw structures out: these look at shapes, strides, types and memory (that of the current device, on which the calls'
 # kernels run), which the structures do not all carry.  The large structures are packed in one go: field by field they cost more than
-# the smallest calls' kernels (a join of eight tokens, us of host time: 33 field by field, 19 packed).
+# the smallest calls' kernels (a join of eight tokens, us of host time: 33 field by field, 19 packed).  As everywhere here, stream=None is
+# the null stream and not torch's current one: inside torch.cuda.stream(s), or in a capture, pass stream=s.
 
 _DTYPES: dict = {}
 _NO_MATRIX, _NO_VECTOR, _NO_CKPT = (0, 0, 0, 0), (0, 0, 0), (0, 0, 0, 0, 0, 0)
