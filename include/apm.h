@@ -7,7 +7,8 @@
  * parameters run page by page (Alg. 2; Sec. 4.3, last paragraph), pages move between pinned host
  * memory and HBM asynchronously (Sec. 5 "Allocator") overlapped with the update (Sec. 4.2), and a
  * one-step-stale variant decouples gradient production from the update (Sec. 4.3, Alg. 2).
- * Calls that need no pool keep a step's activations in 8 bits and make the gradients that the update reads out of them.
+ * Calls that need no pool keep a step's activations in 8 bits and make the gradients that the update reads out of them, and carry tokens to
+ * their parameters and gradients back: sorting, lookup, the products of experts, dropout.
  *
  * Conventions
  *   - Every function returns an apm_status (0 = ok, negative = error) unless stated; nothing
@@ -811,6 +812,142 @@ typedef struct {
 
 size_t apm_ckpt_weight_grad_workspace_bytes(const apm_weight_grad* w);
 int apm_ckpt_weight_grad(const apm_weight_grad* w, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- tokens: which parameters they use ----------------------------------------------------------------------
+ *
+ * The two places of a model where a token picks its parameters, the rows of an embedding and the experts of a mixture: sorting the
+ * tokens by what they pick, looking rows up and the gradients of that, the products of the experts' layers, whose weight gradients
+ * apm_ckpt_weight_grad makes out of the same offsets; and dropout.  As the calls on activations these need no pool, work on the calling
+ * thread's current HIP device, keep and allocate nothing, and may be captured into a HIP graph; a workspace is in use until the call's work is
+ * done, so calls that may run at the same time need one each.  What is written must not overlap what else a call reads or writes, except
+ * where that is said to be allowed.  Errors as there. */
+
+enum apm_index_type { APM_I32 = 0, APM_I64 = 1 };
+
+/* Contiguous whole numbers with sign; data == NULL: not given. */
+typedef struct {
+    const void* data;
+    int32_t type; /* apm_index_type */
+    int32_t reserved;
+} apm_indices;
+
+/*
+ * n positions, per_token of them for each token one after the other, sorted by their ids:
+ *     order[i]    the position that comes i-th: by id, equal ids in the order of their positions; positions whose id is not in [0, rows) behind all
+ *                 others, in their order
+ *     offsets[r]  the first i whose position has id r or a larger one: those of row r are order[offsets[r]] .. order[offsets[r + 1] - 1]
+ *     place[p]    the i with order[i] = p, or -1 where p's id is not in [0, rows)
+ *     token[i]    order[i] / per_token
+ * order is always written, the others (rows + 1, n and n elements) if they are given.  n and rows: at most APM_MAX_POSITIONS.
+ * With expert numbers for ids, token lists the tokens' rows in the experts' order (ids of apm_lookup_forward), offsets the experts' groups
+ * (apm_grouped_product, apm_ckpt_weight_grad), and place where each token finds its experts' outputs.
+ * workspace: apm_sort_tokens_workspace_bytes(o) bytes (0 where the call would refuse o), 16-byte aligned.
+ */
+#define APM_MAX_POSITIONS 2147483000
+typedef struct {
+    int64_t n, per_token, rows;
+    apm_indices ids;
+    int32_t* order;
+    int64_t* offsets;
+    int32_t* place;
+    int32_t* token;
+} apm_token_order;
+
+size_t apm_sort_tokens_workspace_bytes(const apm_token_order* o);
+int apm_sort_tokens(const apm_token_order* o, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rows of a table for each token, with p = t per_token + j for j = 0 .. per_token - 1:
+ *     y[t] = scale (sum over j of weights[p] table[ids[p]])
+ * An id outside [0, rows) adds nothing, whatever its weight is.  weights not given: 1.  accumulate: added to what y holds.
+ * ids and weights: tokens x per_token, contiguous.  table and y: bf16 or fp32 each; arithmetic is fp32, each result is rounded once
+ * (accumulate: the sum with what is there a second time).  tokens per_token and rows: at most APM_MAX_POSITIONS; cols: at most 2^30.
+ * Of an embedding (per_token 1), of tokens for their experts (ids: apm_token_order.token), of experts' outputs for their tokens (ids: place).  The two
+ * last are each other's gradients for the table.
+ */
+typedef struct {
+    int64_t tokens, per_token, rows, cols;
+    double scale;
+    apm_indices ids;
+    apm_vector weights;
+    apm_matrix table, y;
+    int32_t accumulate;
+    int32_t reserved;
+} apm_lookup;
+
+int apm_lookup_forward(const apm_lookup* l, void* stream);
+
+/*
+ * The gradients:
+ *     dtable[r] = scale (sum over the positions p with ids[p] = r, in their order, of weights[p] dy[p / per_token])
+ *     dweights[p] = scale (sum over columns of dy[p / per_token] table[ids[p]]), 0 where the id is outside [0, rows)
+ * Each is written if it is given: dtable whole, zeros in rows without positions; accumulate: added to what dtable holds, rows without positions
+ * are not touched.  dtable needs order and offsets as apm_sort_tokens leaves them for these ids and rows (other contents give other values in
+ * dtable, nothing else).  Of `l` the call reads sizes, scale, ids and weights, and for dweights the table; dy: bf16 or fp32, dtable and dweights: bf16 or
+ * fp32.  Sums are fp32 and do not depend on anything but the arguments: a second call gives the same bits.
+ * workspace: apm_lookup_workspace_bytes(l) bytes (0 where l would be refused; needed for dtable only), 16-byte aligned.
+ */
+typedef struct {
+    apm_matrix dy, dtable;
+    apm_vector dweights;
+    const int32_t* order;
+    const int64_t* offsets;
+    int32_t accumulate;
+    int32_t reserved;
+} apm_lookup_grads;
+
+size_t apm_lookup_workspace_bytes(const apm_lookup* l);
+int apm_lookup_backward(const apm_lookup* l, const apm_lookup_grads* g, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Linear layers, one for each group of tokens:
+ *     y[t, o] = sum over k of x[t, k] w_g[o, k] + bias_g[o]          (w_g: out x in)
+ *     y[t, o] = sum over k of x[t, k] w_g[k, o] + bias_g[o]          (transposed; w_g: in x out)
+ * The second with dy for x is the gradient of the first's input.  Group g has tokens offsets[g] .. offsets[g+1] - 1 (n_groups + 1 device int64, read on
+ * the device, where anything outside [0, tokens] is taken as the end next to it and a group that would end before it starts as empty; groups must not
+ * overlap: if they do, y holds anything).  Rows of y that are in no group are left as they were.  n_groups 0: one product over all tokens.
+ * x, w: bf16.  w's groups are w_group_stride elements apart, bias's [n_groups][out] contiguous (optional, bf16 or fp32).  y: bf16 or fp32; accumulate:
+ * added to what y holds.  Products are exact where they and their factors are zero or of size 2^-126 and up (smaller ones may be taken as zero), sums fp32; the
+ * bias is added to the sum in fp32, then what y held; the result is rounded to y's type.  A second call gives the same bits.
+ * out and in: at most 2^30; n_groups: at most APM_MAX_POSITIONS.
+ * workspace: apm_grouped_product_workspace_bytes(p) bytes (may be 0, as it is where the call would refuse p), 16-byte aligned.
+ */
+typedef struct {
+    int64_t tokens, out, in;
+    int64_t n_groups;
+    const int64_t* offsets; /* NULL if n_groups is 0 */
+    apm_matrix x, w, y;
+    int64_t w_group_stride; /* only with n_groups > 1 */
+    apm_vector bias;
+    int32_t transposed, accumulate;
+} apm_grouped_product_desc;
+
+size_t apm_grouped_product_workspace_bytes(const apm_grouped_product_desc* p);
+int apm_grouped_product(const apm_grouped_product_desc* p, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Dropout whose mask is made of the element's place and never stored:
+ *     y[r, c] = residual[r, c] + (u[r, c] < T ? 0 : x[r, c] 65536 / (65536 - T)),      T = 65536 p rounded to nearest
+ * u: 16 bits of Philox4x32 of ten rounds (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", SC 2011) with counter words c / 8,
+ * the low and the high half of first_row + r, layer, and for key the two halves of seed + *seed_at modulo 2^64, low first: of the four words that
+ * come out, the low halves are for the even columns of the eight, the high ones for the odd, so columns 8 i and 8 i + 1 share word 0.
+ * The mask depends on these alone: the gradient (x: dy, y: dx, no residual) and a recomputed forward pass are the same call, a batch may
+ * be cut into calls with first_row.  seed_at: a device word that is read when the kernel runs, so that replays of a graph differ; NULL: 0.
+ * x: bf16 or fp32; residual (optional) and y: bf16 or fp32, the same.  Arithmetic is fp32, rounded once.  What is dropped is not read as a number:
+ * an infinity or a NaN there leaves no trace.  y may be x itself or residual itself (same address, stride and type).  cols: at most 2^30.
+ */
+typedef struct {
+    int64_t rows, cols;
+    double p; /* 0 .. 1 */
+    uint64_t seed;
+    const uint64_t* seed_at;
+    int64_t first_row; /* >= 0 */
+    uint32_t layer;
+    uint32_t reserved;
+    apm_matrix x, residual, y;
+} apm_dropout;
+
+int apm_dropout_apply(const apm_dropout* d, void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,6 +27,8 @@ APM_CKPT_I8, APM_CKPT_F8, APM_CKPT_BLOCK = 0, 1, 32
 APM_NORM_NONE, APM_NORM_RMS, APM_NORM_LAYER = 0, 1, 2
 APM_GATE_NONE, APM_GATE_CHANNEL, APM_GATE_TOKEN, APM_GATE_FULL = 0, 1, 2, 3
 APM_JOIN_MAX_COLS = 16384
+APM_I32, APM_I64 = 0, 1
+APM_MAX_POSITIONS = 2147483000
 ALL_STATES = 0b11111
 FP32_STATES = 0b00111
 B16_STATES = 0b11000
@@ -43,6 +45,8 @@ EXPORTS = [
     "apm_streamer_set_host_write_through",
     "apm_ckpt_write", "apm_ckpt_read", "apm_norm_join_forward", "apm_norm_join_backward",
     "apm_norm_join_workspace_bytes", "apm_ckpt_weight_grad", "apm_ckpt_weight_grad_workspace_bytes",
+    "apm_sort_tokens", "apm_sort_tokens_workspace_bytes", "apm_lookup_forward", "apm_lookup_backward", "apm_lookup_workspace_bytes",
+    "apm_grouped_product", "apm_grouped_product_workspace_bytes", "apm_dropout_apply",
 ]
 
 
@@ -119,6 +123,38 @@ class apm_weight_grad(C.Structure):
                 ("offsets", C.c_void_p), ("dy", apm_matrix), ("kept", apm_ckpt), ("weight", apm_vector),
                 ("bias", apm_vector), ("dw", apm_matrix), ("dw_group_stride", C.c_int64), ("db", apm_vector),
                 ("accumulate", C.c_int32), ("reserved", C.c_int32)]
+
+
+class apm_indices(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class apm_token_order(C.Structure):
+    _fields_ = [("n", C.c_int64), ("per_token", C.c_int64), ("rows", C.c_int64), ("ids", apm_indices), ("order", C.c_void_p),
+                ("offsets", C.c_void_p), ("place", C.c_void_p), ("token", C.c_void_p)]
+
+
+class apm_lookup(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("per_token", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64), ("scale", C.c_double),
+                ("ids", apm_indices), ("weights", apm_vector), ("table", apm_matrix), ("y", apm_matrix),
+                ("accumulate", C.c_int32), ("reserved", C.c_int32)]
+
+
+class apm_lookup_grads(C.Structure):
+    _fields_ = [("dy", apm_matrix), ("dtable", apm_matrix), ("dweights", apm_vector), ("order", C.c_void_p), ("offsets", C.c_void_p),
+                ("accumulate", C.c_int32), ("reserved", C.c_int32)]
+
+
+class apm_grouped_product_desc(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("out", C.c_int64), ("in", C.c_int64), ("n_groups", C.c_int64), ("offsets", C.c_void_p),
+                ("x", apm_matrix), ("w", apm_matrix), ("y", apm_matrix), ("w_group_stride", C.c_int64), ("bias", apm_vector),
+                ("transposed", C.c_int32), ("accumulate", C.c_int32)]
+
+
+class apm_dropout(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("p", C.c_double), ("seed", C.c_uint64), ("seed_at", C.c_void_p),
+                ("first_row", C.c_int64), ("layer", C.c_uint32), ("reserved", C.c_uint32), ("x", apm_matrix), ("residual", apm_matrix),
+                ("y", apm_matrix)]
 
 
 class ApmError(RuntimeError):
@@ -205,6 +241,17 @@ def lib() -> C.CDLL:
     L.apm_ckpt_weight_grad.argtypes = [P(apm_weight_grad), vp, C.c_size_t, vp]
     L.apm_ckpt_weight_grad_workspace_bytes.argtypes = [P(apm_weight_grad)]
     L.apm_ckpt_weight_grad_workspace_bytes.restype = C.c_size_t
+    L.apm_sort_tokens.argtypes = [P(apm_token_order), vp, C.c_size_t, vp]
+    L.apm_sort_tokens_workspace_bytes.argtypes = [P(apm_token_order)]
+    L.apm_sort_tokens_workspace_bytes.restype = C.c_size_t
+    L.apm_lookup_forward.argtypes = [P(apm_lookup), vp]
+    L.apm_lookup_backward.argtypes = [P(apm_lookup), P(apm_lookup_grads), vp, C.c_size_t, vp]
+    L.apm_lookup_workspace_bytes.argtypes = [P(apm_lookup)]
+    L.apm_lookup_workspace_bytes.restype = C.c_size_t
+    L.apm_grouped_product.argtypes = [P(apm_grouped_product_desc), vp, C.c_size_t, vp]
+    L.apm_grouped_product_workspace_bytes.argtypes = [P(apm_grouped_product_desc)]
+    L.apm_grouped_product_workspace_bytes.restype = C.c_size_t
+    L.apm_dropout_apply.argtypes = [P(apm_dropout), vp]
     for name in EXPORTS:
         getattr(L, name)              # every declared entry point must be exported
     _lib = L
@@ -845,3 +892,163 @@ def apm_ckpt_weight_grad(grad: apm_weight_grad, workspace=None, stream=None) -> 
     here = _here()
     _same_gpu(getattr(grad, "device", None), here)
     _check(lib().apm_ckpt_weight_grad(grad, *_room(workspace, here), _stream(stream)))
+
+
+# ---- tokens -------------------------------------------------------------------------------------
+# As with the activation calls: tensors in, structures out that keep them alive, no stream means the null stream.
+
+_INDEX_TYPES: dict = {}
+_pack_order = struct.Struct("<qqqQiiQQQQ").pack
+_pack_lookup = struct.Struct("<qqqqdQii" + _VECTOR + _MATRIX * 2 + "ii").pack
+_pack_lookup_grads = struct.Struct("<" + _MATRIX * 2 + _VECTOR + "QQii").pack
+_pack_product = struct.Struct("<qqqqQ" + _MATRIX * 3 + "q" + _VECTOR + "ii").pack
+_pack_dropout = struct.Struct("<qqdQQqII" + _MATRIX * 3).pack
+
+
+def _address(name, t, here) -> int:
+    return t.data_ptr() if (t.is_cuda if here is None else t.get_device() == here) else _elsewhere(name, t, here)
+
+
+def _indices(name, t, here):
+    """Words of an apm_indices, of any shape."""
+    code = _INDEX_TYPES.get(t.dtype)
+    if code is None:
+        code = {"torch.int32": APM_I32, "torch.int64": APM_I64}.get(str(t.dtype))
+        if code is None:
+            raise ValueError(f"{name}: a tensor of {t.dtype}, int32 or int64 is needed")
+        _INDEX_TYPES[t.dtype] = code
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()}, contiguous elements are needed")
+    return _address(name, t, here), code, 0
+
+
+def _whole(name, t, n, dtype, here) -> int:
+    """Address of n whole numbers of one type (None: not given)."""
+    if t is None:
+        return 0
+    if t.numel() != n or not t.is_contiguous() or str(t.dtype) != dtype:
+        raise ValueError(f"{name}: {t.dtype} of {tuple(t.shape)} with strides {t.stride()}, {n} contiguous elements of {dtype} are needed")
+    return _address(name, t, here)
+
+
+def _per_token(name, ids):
+    """(tokens, ids of a token) of a tensor [tokens] or [tokens, per_token]."""
+    if ids.dim() == 1:
+        return ids.shape[0], 1
+    if ids.dim() != 2 or ids.shape[1] < 1:
+        raise ValueError(f"{name}: {tuple(ids.shape)}, [tokens] or [tokens, ids of a token] is needed")
+    return ids.shape
+
+
+def make_token_order(ids, rows: int, order, *, offsets=None, place=None, token=None) -> apm_token_order:
+    """ids: [tokens] or [tokens, per_token], int32 or int64; order, place and token: int32, one for each id; offsets: int64, rows + 1."""
+    here = _here()
+    tokens, per = _per_token("ids", ids)
+    n = tokens * per
+    o = apm_token_order.from_buffer_copy(_pack_order(n, per, rows, *_indices("ids", ids, here), _whole("order", order, n, "torch.int32", here),
+                                                     _whole("offsets", offsets, rows + 1, "torch.int64", here), _whole("place", place, n, "torch.int32", here),
+                                                     _whole("token", token, n, "torch.int32", here)))
+    o.tensors, o.device = (ids, order, offsets, place, token), here
+    return o
+
+
+def apm_sort_tokens_workspace_bytes(order: apm_token_order) -> int:
+    return lib().apm_sort_tokens_workspace_bytes(order)
+
+
+def apm_sort_tokens(order: apm_token_order, workspace=None, stream=None) -> None:
+    here = _here()
+    _same_gpu(getattr(order, "device", None), here)
+    _check(lib().apm_sort_tokens(order, *_room(workspace, here), _stream(stream)))
+
+
+def make_lookup(ids, table, y=None, *, scale=1.0, weights=None, accumulate=False, rows=None, cols=None) -> apm_lookup:
+    """ids (and weights): [tokens] or [tokens, per_token].  table: [rows, cols]; a backward call that makes no gradient of the weights needs neither it
+    nor y, but rows and cols then."""
+    here = _here()
+    tokens, per = _per_token("ids", ids)
+    if table is not None:
+        rows, cols = table.shape
+    if rows is None or cols is None:
+        raise ValueError("a lookup without a table needs rows and cols")
+    u = apm_lookup.from_buffer_copy(_pack_lookup(tokens, per, rows, cols, scale, *_indices("ids", ids, here), *_vector("weights", weights, tokens * per, here),
+                                                 *_matrix("table", table, rows, cols, here), *_matrix("y", y, tokens, cols, here), int(accumulate), 0))
+    u.tensors, u.device, u.shape = (ids, table, y, weights), here, (tokens, per, rows, cols)
+    return u
+
+
+def make_lookup_grads(lookup: apm_lookup, dy, *, order: Optional[apm_token_order] = None, dtable=None, dweights=None, accumulate=False) -> apm_lookup_grads:
+    """order: of apm_sort_tokens for the lookup's ids and rows, with offsets; needed for dtable."""
+    (tokens, per, rows, cols), here = lookup.shape, _here()
+    _same_gpu(lookup.device, here)
+    at = (0, 0)
+    if order is not None:
+        if (order.n, order.per_token, order.rows) != (tokens * per, per, rows):
+            raise ValueError(f"order: {(order.n, order.per_token, order.rows)} positions, positions of a token and rows, {(tokens * per, per, rows)} are needed")
+        _same_gpu(getattr(order, "device", None), here)
+        at = order.order or 0, order.offsets or 0
+    g = apm_lookup_grads.from_buffer_copy(_pack_lookup_grads(*_matrix("dy", dy, tokens, cols, here), *_matrix("dtable", dtable, rows, cols, here),
+                                                             *_vector("dweights", dweights, tokens * per, here), *at, int(accumulate), 0))
+    g.tensors, g.device = (dy, dtable, dweights, order), here
+    return g
+
+
+def apm_lookup_forward(lookup, stream=None) -> None:
+    _same_gpu(getattr(lookup, "device", None), _here())
+    _check(lib().apm_lookup_forward(lookup, _stream(stream)))
+
+
+def apm_lookup_workspace_bytes(lookup) -> int:
+    return lib().apm_lookup_workspace_bytes(lookup)
+
+
+def apm_lookup_backward(lookup, grads: "apm_lookup_grads", workspace=None, stream=None) -> None:
+    here = _here()
+    _same_gpu(getattr(grads, "device", None), here)
+    _check(lib().apm_lookup_backward(lookup, grads, *_room(workspace, here), _stream(stream)))
+
+
+def make_grouped_product(x, w, y, *, offsets=None, bias=None, transposed=False, accumulate=False) -> apm_grouped_product_desc:
+    """w: [out, in] (transposed: [in, out]), or with offsets (int64, groups + 1) [groups, ...]; bias: [out] or [groups, out]."""
+    here = _here()
+    (tokens, k), out, groups, at = x.shape, y.shape[1], 0, 0
+    if offsets is not None:
+        groups = offsets.numel() - 1
+        if groups < 1 or w.dim() != 3 or w.shape[0] != groups:
+            raise ValueError(f"offsets of {tuple(offsets.shape)} for weights of {tuple(w.shape)}")
+        at = _whole("offsets", offsets, groups + 1, "torch.int64", here)
+    p = apm_grouped_product_desc.from_buffer_copy(_pack_product(
+        tokens, out, k, groups, at, *_matrix("x", x, tokens, k, here), *_matrix("w", w[0] if groups else w, *((k, out) if transposed else (out, k)), here),
+        *_matrix("y", y, tokens, out, here), w.stride(0) if groups else 0, *_vector("bias", bias, max(1, groups) * out, here), int(transposed), int(accumulate)))
+    p.tensors, p.device = (x, w, y, offsets, bias), here
+    return p
+
+
+def apm_grouped_product_workspace_bytes(product: apm_grouped_product_desc) -> int:
+    return lib().apm_grouped_product_workspace_bytes(product)
+
+
+def apm_grouped_product(product: apm_grouped_product_desc, workspace=None, stream=None) -> None:
+    here = _here()
+    _same_gpu(getattr(product, "device", None), here)
+    _check(lib().apm_grouped_product(product, *_room(workspace, here), _stream(stream)))
+
+
+def make_dropout(x, y, *, p: float, seed: int, layer: int = 0, first_row: int = 0, residual=None, seed_at=None) -> apm_dropout:
+    """seed: 64 bits; seed_at: one int64 or uint64 in device memory that is added to it when the kernel runs."""
+    here = _here()
+    rows, cols = x.shape
+    at = 0
+    if seed_at is not None:
+        if seed_at.numel() != 1 or seed_at.element_size() != 8:
+            raise ValueError(f"seed_at: {seed_at.dtype} of {tuple(seed_at.shape)}, one word of 64 bits is needed")
+        at = _address("seed_at", seed_at, here)
+    d = apm_dropout.from_buffer_copy(_pack_dropout(rows, cols, p, seed, at, first_row, layer, 0, *_matrix("x", x, rows, cols, here),
+                                                   *_matrix("residual", residual, rows, cols, here), *_matrix("y", y, rows, cols, here)))
+    d.tensors, d.device = (x, residual, y, seed_at), here
+    return d
+
+
+def apm_dropout_apply(dropout, stream=None) -> None:
+    _same_gpu(getattr(dropout, "device", None), _here())
+    _check(lib().apm_dropout_apply(dropout, _stream(stream)))

@@ -430,6 +430,12 @@ template <bool HALVES> __device__ __forceinline__ float swap_add(float x) {
 }
 __device__ __forceinline__ float wave_sum(float x) { return swap_add<true>(swap_add<false>(row_sum16(x))); }  // the same in every lane
 
+// What lanes of a wavefront hand each other through LDS: its accesses are carried out in order, so it is the compiler's order that counts.
+__device__ __forceinline__ void among_lanes() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // ---- argument checks ----------------------------------------------------------------------------
 int check_matrix(const char* name, const apm_matrix& m, int64_t rows, int64_t cols, bool written);
 int check_vector(const char* name, const apm_vector& v);

@@ -157,12 +157,6 @@ __device__ __forceinline__ void finish(const WgradArgs& a, const Columns& c, int
     else store8<bf16, true>(row, (int)k, n, v);
 }
 
-// What lanes of a wavefront hand each other through LDS: its accesses are carried out in order, so it is the compiler's order that counts.
-__device__ __forceinline__ void among_lanes() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 constexpr int kXcds = 8;
 constexpr int kStrip = 4;  // rows of tiles that are walked together
 
