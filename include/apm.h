@@ -861,7 +861,7 @@ int apm_sort_tokens(const apm_token_order* o, void* workspace, size_t workspace_
  *     y[t] = scale (sum over j of weights[p] table[ids[p]])
  * An id outside [0, rows) adds nothing, whatever its weight is.  weights not given: 1.  accumulate: added to what y holds.
  * ids and weights: tokens x per_token, contiguous.  table and y: bf16 or fp32 each; arithmetic is fp32, each result is rounded once
- * (accumulate: the sum with what is there a second time).  tokens per_token and rows: at most APM_MAX_POSITIONS; cols: at most 2^30.
+ * (accumulate: the sum with what is there a second time).  tokens per_token and rows: at most APM_MAX_POSITIONS; cols: at most 2^28.
  * Of an embedding (per_token 1), of tokens for their experts (ids: apm_token_order.token), of experts' outputs for their tokens (ids: place).  The two
  * last are each other's gradients for the table.
  */
@@ -885,6 +885,7 @@ int apm_lookup_forward(const apm_lookup* l, void* stream);
  * are not touched.  dtable needs order and offsets as apm_sort_tokens leaves them for these ids and rows (other contents give other values in
  * dtable, nothing else).  Of `l` the call reads sizes, scale, ids and weights, and for dweights the table; dy: bf16 or fp32, dtable and dweights: bf16 or
  * fp32.  Sums are fp32 and do not depend on anything but the arguments: a second call gives the same bits.
+ * A dtable for more than 2^31 pieces of 512 columns of a few positions is refused (APM_EINVAL).
  * workspace: apm_lookup_workspace_bytes(l) bytes (0 where l would be refused; needed for dtable only), 16-byte aligned.
  */
 typedef struct {
@@ -909,7 +910,7 @@ int apm_lookup_backward(const apm_lookup* l, const apm_lookup_grads* g, void* wo
  * x, w: bf16.  w's groups are w_group_stride elements apart, bias's [n_groups][out] contiguous (optional, bf16 or fp32).  y: bf16 or fp32; accumulate:
  * added to what y holds.  Products are exact where they and their factors are zero or of size 2^-126 and up (smaller ones may be taken as zero), sums fp32; the
  * bias is added to the sum in fp32, then what y held; the result is rounded to y's type.  A second call gives the same bits.
- * out and in: at most 2^30; n_groups: at most APM_MAX_POSITIONS.
+ * out and in: at most 2^28; n_groups: at most APM_MAX_POSITIONS.
  * workspace: apm_grouped_product_workspace_bytes(p) bytes (may be 0, as it is where the call would refuse p), 16-byte aligned.
  */
 typedef struct {
@@ -934,7 +935,7 @@ int apm_grouped_product(const apm_grouped_product_desc* p, void* workspace, size
  * The mask depends on these alone: the gradient (x: dy, y: dx, no residual) and a recomputed forward pass are the same call, a batch may
  * be cut into calls with first_row.  seed_at: a device word that is read when the kernel runs, so that replays of a graph differ; NULL: 0.
  * x: bf16 or fp32; residual (optional) and y: bf16 or fp32, the same.  Arithmetic is fp32, rounded once.  What is dropped is not read as a number:
- * an infinity or a NaN there leaves no trace.  y may be x itself or residual itself (same address, stride and type).  cols: at most 2^30.
+ * an infinity or a NaN there leaves no trace.  y may be x itself or residual itself (same address, stride and type).  cols: at most 2^28.
  */
 typedef struct {
     int64_t rows, cols;

@@ -244,13 +244,13 @@ template <int CACHE = kNT> __device__ __forceinline__ u32x4 load_bf16(const void
 __device__ __forceinline__ void settle_bf16(u32x4& a, const LaneCols& l, int64_t cols) {
     if (l.whole != (uint32_t)cols && cols >= kVec && l.tail()) move_down(a, l.n);
 }
-__device__ __forceinline__ void load_row(Raw<bf16>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
-    x.a = load_bf16(m.data, row * m.stride * 2, cols, there, l);
+template <int CACHE = kNT> __device__ __forceinline__ void load_row(Raw<bf16>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
+    x.a = load_bf16<CACHE>(m.data, row * m.stride * 2, cols, there, l);
 }
-__device__ __forceinline__ void load_row(Raw<float>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
+template <int CACHE = kNT> __device__ __forceinline__ void load_row(Raw<float>& x, const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l) {
     const Rsrc r = row_buffer(m.data, row * m.stride * 4, there ? (uint32_t)cols * 4u : 0u);
-    x.a = load_b128(r, l.at4);
-    x.b = load_b128(r, l.at4 + LaneCols::kStep4);
+    x.a = load_b128<CACHE>(r, l.at4);
+    x.b = load_b128<CACHE>(r, l.at4 + LaneCols::kStep4);
 }
 __device__ __forceinline__ void settle(Raw<bf16>& x, const LaneCols& l, int64_t cols) { settle_bf16(x.a, l, cols); }
 __device__ __forceinline__ void settle(Raw<float>& x, const LaneCols&, int64_t) { swap_halves(x.a, x.b); }

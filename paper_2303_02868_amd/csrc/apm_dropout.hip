@@ -8,19 +8,17 @@
 namespace apm {
 namespace {
 
-constexpr int kThreads = 256, kUnroll = 2;
+constexpr int kWave = 64, kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kSlice = kWave * kVec;  // columns of a wavefront
+constexpr int kRows = 2;     // rows of a wavefront, whose loads are under way together
 
 struct DropoutArgs {
-    const char* x;
-    const char* residual;
-    char* y;
+    apm_matrix x, residual, y;
     const uint64_t* seed_at;
     uint64_t seed;
-    int64_t x_stride, residual_stride, y_stride;
-    int64_t first_row;  // of the launch
-    uint64_t counter;   // of that row
-    uint32_t rows, vecs;
-    float inv_vecs;
+    uint64_t first_row;
+    int64_t rows, first_item;
+    uint32_t slices;
     int32_t cols;
     uint32_t bound, layer;
     float scale;
@@ -46,29 +44,32 @@ struct Philox {
 
 template <class X, class Y, bool RESIDUAL>
 __global__ __launch_bounds__(kThreads) void apm_dropout_kernel(DropoutArgs a) {
-    const uint32_t first = blockIdx.x * (uint32_t)(kThreads * kUnroll), row0 = first / a.vecs, vec0 = first - row0 * a.vecs;
-    const uint64_t seed = a.seed + (a.seed_at ? *a.seed_at : 0);
-    Raw<X> x[kUnroll];
-    Raw<Y> residual[kUnroll];
+    const int lane = (int)threadIdx.x % kWave;
+    const int64_t item = a.first_item + (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int64_t r0 = item / a.slices * kRows;
+    if (r0 >= a.rows) return;
+    LaneCols l;
+    l.set((int)(item % a.slices) * kSlice + lane * kVec, a.cols);
+    Raw<X> x[kRows];
+    Raw<Y> residual[kRows];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const VecPlace p(row0, vec0, (uint32_t)(u * kThreads) + threadIdx.x, a.vecs, a.inv_vecs, a.cols);
-        const int64_t row = a.first_row + p.row;
-        const int n = p.row < a.rows ? p.n : 0;
-        x[u].load(a.x + row * a.x_stride * (int64_t)sizeof(X), p.col, n);
-        if constexpr (RESIDUAL) residual[u].load(a.residual + row * a.residual_stride * (int64_t)sizeof(Y), p.col, n);
+    for (int u = 0; u < kRows; ++u) {
+        load_row(x[u], a.x, r0 + u, a.cols, r0 + u < a.rows, l);
+        if constexpr (RESIDUAL) load_row(residual[u], a.residual, r0 + u, a.cols, r0 + u < a.rows, l);
     }
+    const uint64_t seed = a.seed + (a.seed_at ? *a.seed_at : 0);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const VecPlace p(row0, vec0, (uint32_t)(u * kThreads) + threadIdx.x, a.vecs, a.inv_vecs, a.cols);
-        const Philox random((uint32_t)p.col / kVec, a.counter + p.row, a.layer, seed);
+    for (int u = 0; u < kRows; ++u) {
+        const Philox random((uint32_t)l.col / kVec, a.first_row + (uint64_t)(r0 + u), a.layer, seed);
+        settle(x[u], l, a.cols);
+        if constexpr (RESIDUAL) settle(residual[u], l, a.cols);
         float v[kVec];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             v[i] = random[i] < a.bound ? 0.0f : x[u][i] * a.scale;
             if constexpr (RESIDUAL) v[i] += residual[u][i];
         }
-        store8<Y>(a.y + (a.first_row + p.row) * a.y_stride * (int64_t)sizeof(Y), p.col, p.row < a.rows ? p.n : 0, v);
+        store_row<Y>(a.y, r0 + u, a.cols, r0 + u < a.rows, l, v);
     }
 }
 
@@ -84,17 +85,14 @@ int apply(const apm_dropout* dp, void* stream) {
     if (rc != APM_OK || d.rows == 0) return rc;
     if (d.residual.data && d.residual.dtype != d.y.dtype) return fail(APM_EINVAL, "residual and y have different types");
     DropoutArgs a{};
-    a.x = (const char*)d.x.data, a.residual = (const char*)d.residual.data, a.y = (char*)d.y.data;
-    a.seed_at = d.seed_at, a.seed = d.seed, a.layer = d.layer;
-    a.x_stride = d.x.stride, a.residual_stride = d.residual.stride, a.y_stride = d.y.stride;
-    a.cols = (int32_t)d.cols, a.vecs = (uint32_t)div_up(d.cols, kVec), a.inv_vecs = 1.0f / (float)a.vecs;
+    a.x = d.x, a.residual = d.residual, a.y = d.y;
+    a.seed_at = d.seed_at, a.seed = d.seed, a.layer = d.layer, a.first_row = (uint64_t)d.first_row;
+    a.rows = d.rows, a.cols = (int32_t)d.cols, a.slices = (uint32_t)div_up(d.cols, kSlice);
     a.bound = (uint32_t)std::llround(d.p * 65536.0);
     a.scale = a.bound < 65536 ? (float)(65536.0 / (65536.0 - a.bound)) : 0.0f;
-    const int64_t most = std::max<int64_t>(1, kMostVecs / a.vecs);
-    for (a.first_row = 0; a.first_row < d.rows; a.first_row += most) {
-        a.rows = (uint32_t)std::min(most, d.rows - a.first_row);
-        a.counter = (uint64_t)d.first_row + (uint64_t)a.first_row;
-        const dim3 grid((unsigned)div_up((int64_t)a.rows * a.vecs, kThreads * kUnroll)), block(kThreads);
+    const int64_t items = div_up(d.rows, kRows) * a.slices, most = max_workgroups(kThreads) * kWaves / 2;
+    for (a.first_item = 0; a.first_item < items; a.first_item += most) {
+        const dim3 grid((unsigned)div_up(std::min(most, items - a.first_item), kWaves)), block(kThreads);
         const hipStream_t s = (hipStream_t)stream;
         auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
         auto with = [&](auto x, auto y) {

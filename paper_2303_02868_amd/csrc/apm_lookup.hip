@@ -1,6 +1,6 @@
 // Rows of a table for each token, y[t] = scale sum w[p] table[ids[p]], and the gradients of that.  HBM-bound, all of it.
 //
-// Forward, a lane has eight columns of a token and adds up its rows.  The gradient of the table goes by the sorted positions, so that each of its rows is
+// Forward, a wavefront has 512 columns of a few tokens and adds up their rows.  The gradient of the table goes by the sorted positions, so that each of its rows is
 // written once and nothing is added atomically: the sorted positions are cut into chunks of equal size, whatever rows they belong to, a wavefront adds up what it
 // has of each row, and a row that goes beyond a chunk is put together from the chunks' parts, in their order.
 #include <algorithm>
@@ -12,75 +12,72 @@ namespace {
 
 constexpr int kWave = 64, kThreads = 256, kWaves = kThreads / kWave;
 
+constexpr int kSlice = kWave * kVec;                        // columns of a wavefront
+constexpr int kTokens = 4, kTurn = kWave / kTokens;         // tokens of a wavefront, whose loads are under way together; ids of a token that it takes at a time
+
 struct LookupArgs {
     const void* ids;
-    const char* table;
-    char* y;
+    apm_matrix table, y;
     apm_vector weights;
-    int64_t table_stride, y_stride;
-    int64_t first_token;  // of the launch
-    uint32_t tokens, vecs;
-    float inv_vecs;
-    int32_t cols;
-    uint32_t rows;
-    int32_t per_token, id_type, accumulate;
+    int64_t tokens, first_item;
+    uint32_t slices, rows;
+    int32_t cols, per_token, id_type, accumulate;
     float scale;
 };
 
 __device__ __forceinline__ float weight_of(const apm_vector& w, int64_t p) { return w.data ? load1(w.data, w.dtype, p) : 1.0f; }
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ float of_lane(float v, int lane) { return __builtin_bit_cast(float, of_lane(__builtin_bit_cast(uint32_t, v), lane)); }
 
-constexpr int kRowsAhead = 4;  // of a token's rows, loads under way
-template <class T, class Y, int UNROLL>
+template <class T, class Y>
 __global__ __launch_bounds__(kThreads) void apm_lookup_kernel(LookupArgs a) {
-    const uint32_t first = blockIdx.x * (uint32_t)(kThreads * UNROLL), row0 = first / a.vecs, vec0 = first - row0 * a.vecs;
-    auto place = [&](int u) { return VecPlace(row0, vec0, (uint32_t)(u * kThreads) + threadIdx.x, a.vecs, a.inv_vecs, a.cols); };
-    float sum[UNROLL][kVec];
+    const int lane = (int)threadIdx.x % kWave;
+    const int64_t item = a.first_item + (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int64_t t0 = item / a.slices * kTokens;
+    if (t0 >= a.tokens) return;
+    LaneCols l;
+    l.set((int)(item % a.slices) * kSlice + lane * kVec, a.cols);
+    float sum[kTokens][kVec] = {};
+    for (int j0 = 0; j0 < a.per_token; j0 += kTurn) {
+        const int64_t t = t0 + lane / kTurn, j = j0 + lane % kTurn;
+        uint32_t my_row = a.rows;
+        float my_weight = 0.0f;
+        if (t < a.tokens && j < a.per_token) {
+            const int64_t p = t * a.per_token + j;
+            my_row = row_of(a.ids, a.id_type, p, a.rows);
+            if (my_row < a.rows) my_weight = weight_of(a.weights, p);
+        }
+        const int turn = min(kTurn, a.per_token - j0);
+        for (int k = 0; k < turn; ++k) {
+            Raw<T> x[kTokens];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u)
+            for (int u = 0; u < kTokens; ++u) {  // no such row: zeros, by a factor of zero
+                const uint32_t row = of_lane(my_row, u * kTurn + k);
+                load_row<0>(x[u], a.table, row, a.cols, row < a.rows, l);
+            }
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) sum[u][i] = 0.0f;
-    constexpr int AHEAD = UNROLL > 1 ? 1 : kRowsAhead;
-    for (int j = 0; j < a.per_token; j += AHEAD) {
-        Raw<T> x[UNROLL][AHEAD];
-        float w[UNROLL][AHEAD];
-        bool there[UNROLL][AHEAD];
+            for (int u = 0; u < kTokens; ++u) {
+                const float w = of_lane(my_weight, u * kTurn + k);
+                settle(x[u], l, a.cols);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const VecPlace at = place(u);
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int64_t p = (a.first_token + at.row) * a.per_token + j + k;
-                const bool in = at.row < a.tokens && j + k < a.per_token;
-                const uint32_t row = in ? row_of(a.ids, a.id_type, p, a.rows) : a.rows;
-                there[u][k] = row < a.rows;
-                w[u][k] = there[u][k] ? weight_of(a.weights, p) : 0.0f;
-                x[u][k].load(a.table + (int64_t)row * a.table_stride * (int64_t)sizeof(T), at.col, there[u][k] ? at.n : 0);
+                for (int i = 0; i < kVec; ++i) sum[u][i] = fmaf(w, x[u][i], sum[u][i]);
             }
         }
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u)
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k)
-                if (there[u][k]) {
-#pragma unroll
-                    for (int i = 0; i < kVec; ++i) sum[u][i] = fmaf(w[u][k], x[u][k][i], sum[u][i]);
-                }
     }
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const VecPlace at = place(u);
-        char* y = a.y + (a.first_token + at.row) * a.y_stride * (int64_t)sizeof(Y);
-        const int n = at.row < a.tokens ? at.n : 0;
+    for (int u = 0; u < kTokens; ++u) {
+        const bool there = t0 + u < a.tokens;
         float v[kVec];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] = sum[u][i] * a.scale;
         if (a.accumulate) {
             Raw<Y> old;
-            old.load(y, at.col, n);
+            load_row(old, a.y, t0 + u, a.cols, there, l);
+            settle(old, l, a.cols);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) v[i] += old[i];
         }
-        store8<Y>(y, at.col, n, v);
+        store_row<Y>(a.y, t0 + u, a.cols, there, l, v);
     }
 }
 
@@ -102,62 +99,51 @@ int forward(const apm_lookup* lp, void* stream) {
     const int rc = check_lookup(l, true);
     if (rc != APM_OK || l.tokens == 0) return rc;
     LookupArgs a{};
-    a.ids = l.ids.data, a.id_type = l.ids.type, a.table = (const char*)l.table.data, a.y = (char*)l.y.data, a.weights = l.weights;
-    a.table_stride = l.table.stride, a.y_stride = l.y.stride;
-    a.vecs = (uint32_t)div_up(l.cols, kVec), a.inv_vecs = 1.0f / (float)a.vecs, a.cols = (int32_t)l.cols;
+    a.ids = l.ids.data, a.id_type = l.ids.type, a.table = l.table, a.y = l.y, a.weights = l.weights;
+    a.tokens = l.tokens, a.slices = (uint32_t)div_up(l.cols, kSlice), a.cols = (int32_t)l.cols;
     a.rows = (uint32_t)l.rows, a.per_token = (int32_t)l.per_token, a.accumulate = l.accumulate, a.scale = (float)l.scale;
-    const int64_t most = std::max<int64_t>(1, kMostVecs / a.vecs);
-    for (a.first_token = 0; a.first_token < l.tokens; a.first_token += most) {
-        a.tokens = (uint32_t)std::min(most, l.tokens - a.first_token);
+    const int64_t items = div_up(l.tokens, kTokens) * a.slices, most = max_workgroups(kThreads) * kWaves / 2;
+    for (a.first_item = 0; a.first_item < items; a.first_item += most) {
+        const dim3 grid((unsigned)div_up(std::min(most, items - a.first_item), kWaves)), block(kThreads);
         const hipStream_t s = (hipStream_t)stream;
-        auto start = [&](auto kernel, int unroll) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)div_up((int64_t)a.tokens * a.vecs, kThreads * unroll)), dim3(kThreads), 0, s, a);
-        };
-        auto with = [&](auto t, auto y) {
-            typedef decltype(t) T;
-            typedef decltype(y) Y;
-            if (a.per_token == 1) start(apm_lookup_kernel<T, Y, 2>, 2);
-            else start(apm_lookup_kernel<T, Y, 1>, 1);
-        };
-        if (l.table.dtype == APM_F32) l.y.dtype == APM_F32 ? with(float(), float()) : with(float(), bf16());
-        else l.y.dtype == APM_F32 ? with(bf16(), float()) : with(bf16(), bf16());
+        auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
+        if (l.table.dtype == APM_F32) l.y.dtype == APM_F32 ? start(apm_lookup_kernel<float, float>) : start(apm_lookup_kernel<float, bf16>);
+        else l.y.dtype == APM_F32 ? start(apm_lookup_kernel<bf16, float>) : start(apm_lookup_kernel<bf16, bf16>);
         APM_HIP(hipGetLastError());
     }
     return APM_OK;
 }
 
 // ---- the gradient of the table ------------------------------------------------------------------
-constexpr int kChunk = 64;                  // sorted positions of a wavefront, one of each lane to begin with
-constexpr int kSlice = kWave * kVec;        // columns of a wavefront
+constexpr int kChunkMost = kWave;           // sorted positions of a wavefront, one of each lane to begin with
+constexpr int kChunkLeast = 8;
 constexpr int kAhead = 8;                   // rows of dy under way
-constexpr int kEmptyRows = 32;              // rows of dtable that a wavefront looks through for those without positions
+constexpr int kEmptyRows = 8;              // rows of dtable that a wavefront looks through for those without positions
 
 struct TableGradArgs {
     const void* ids;
-    const char* dy;
-    char* dtable;
     const int32_t* order;
     const int64_t* offsets;
     float* parts;  // [chunks][2][cols_8]: of the row that began before the chunk, and of the row that goes on behind it
+    apm_matrix dy, dtable;
     apm_vector weights;
-    int64_t dy_stride, table_stride;
-    uint32_t n, rows, per_token, chunks, slices, empty;  // empty: wavefronts that write zeros
-    uint32_t first_item;
+    uint32_t n, rows, per_token, chunk, chunks, slices, empty;  // empty: wavefronts that write zeros
+    uint32_t first_item, last_item;
     int32_t cols, cols_8, id_type, accumulate;
     float scale;
 };
 
-template <class T, bool NT = true> __device__ __forceinline__ void finish_row(const TableGradArgs& a, uint32_t row, int col, int n, float (&v)[kVec]) {
-    char* to = a.dtable + (int64_t)row * a.table_stride * (int64_t)sizeof(T);
+template <class T> __device__ __forceinline__ void finish_row(const TableGradArgs& a, uint32_t row, const LaneCols& l, float (&v)[kVec]) {
 #pragma unroll
     for (int i = 0; i < kVec; ++i) v[i] *= a.scale;
     if (a.accumulate) {
         Raw<T> old;
-        old.load(to, col, n);
+        load_row(old, a.dtable, row, a.cols, true, l);
+        settle(old, l, a.cols);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] += old[i];
     }
-    store8<T, NT>(to, col, n, v);
+    store_row<T>(a.dtable, row, a.cols, true, l, v);
 }
 __device__ __forceinline__ float* part_of(const TableGradArgs& a, uint32_t chunk, int which, int col) {
     return a.parts + ((uint64_t)chunk * 2 + (uint32_t)which) * (uint32_t)a.cols_8 + (uint32_t)col;
@@ -172,6 +158,7 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs 
     const int lane = (int)threadIdx.x % kWave;
     const uint32_t item = a.first_item + (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + threadIdx.x / kWave));
     const uint32_t summing = a.chunks * a.slices;
+    LaneCols l;
     if (item >= summing) {  // rows without positions
         const uint32_t e = item - summing;
         if (e >= a.empty) return;
@@ -182,12 +169,16 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs 
         while (mask) {
             const uint32_t row = first + (uint32_t)__builtin_ctzll(mask);
             mask &= mask - 1;
-            for (int col = lane * kVec; col < a.cols; col += kSlice) store8<T, true>(a.dtable + (int64_t)row * a.table_stride * (int64_t)sizeof(T), col, min(kVec, a.cols - col), zero);
+            for (int col = 0; col < a.cols; col += kSlice) {
+                l.set(col + lane * kVec, a.cols);
+                store_row<T>(a.dtable, row, a.cols, true, l, zero);
+            }
         }
         return;
     }
-    const uint32_t chunk = item / a.slices, start = chunk * kChunk;
-    const int col = (int)(item - chunk * a.slices) * kSlice + lane * kVec, there = max(0, min(kVec, a.cols - col)), n = (int)min((uint32_t)kChunk, a.n - start);
+    const uint32_t chunk = item / a.slices, start = chunk * a.chunk;
+    const int n = (int)min(a.chunk, a.n - start);
+    l.set((int)(item - chunk * a.slices) * kSlice + lane * kVec, a.cols);
     // lane l: the chunk's l-th position
     uint32_t my_row = a.rows, my_token = 0;
     float my_weight = 0.0f;
@@ -199,19 +190,18 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs 
             if (my_row < a.rows) my_weight = weight_of(a.weights, p);
         }
     }
-    auto of_lane = [](uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
     uint32_t row = of_lane(my_row, 0);
     if (row >= a.rows) return;  // so are all behind it
     bool before = start > 0 && row_at(a, start - 1) == row;  // the row began in an earlier chunk
-    const uint32_t after = start + kChunk < a.n ? row_at(a, start + kChunk) : a.rows;
+    const uint32_t after = start + a.chunk < a.n ? row_at(a, start + a.chunk) : a.rows;
     float sum[kVec] = {};
     auto flush = [&](bool goes_on) {
-        if (!before && !goes_on) return finish_row<T>(a, row, col, there, sum);
-        if (there <= 0) return;
+        if (!before && !goes_on) return finish_row<T>(a, row, l, sum);
+        if (l.n <= 0) return;
         u32x4 w[2];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) w[i / 4][i % 4] = __builtin_bit_cast(uint32_t, sum[i]);
-        u32x4* to = (u32x4*)part_of(a, chunk, before ? 0 : 1, col);
+        u32x4* to = (u32x4*)part_of(a, chunk, before ? 0 : 1, l.col);
         to[0] = w[0], to[1] = w[1];
     };
     for (int i0 = 0; i0 < n; i0 += kAhead) {
@@ -220,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs 
         for (int k = 0; k < kAhead; ++k) {
             const int i = i0 + k;
             const bool in = i < n && of_lane(my_row, i & (kWave - 1)) < a.rows;
-            x[k].load(a.dy + (int64_t)of_lane(my_token, i & (kWave - 1)) * a.dy_stride * (int64_t)sizeof(D), col, in ? there : 0);
+            load_row(x[k], a.dy, of_lane(my_token, i & (kWave - 1)), a.cols, in, l);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -234,7 +224,8 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs 
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) sum[e] = 0.0f;
             }
-            const float w = __builtin_bit_cast(float, of_lane(__builtin_bit_cast(uint32_t, my_weight), i));
+            const float w = of_lane(my_weight, i);
+            settle(x[k], l, a.cols);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) sum[e] = fmaf(w, x[k][e], sum[e]);
         }
@@ -242,46 +233,68 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs 
     flush(after == row);
 }
 
-// A row that goes beyond the chunk in which it begins: that chunk's part and those of the chunks behind it.
+// A row that goes beyond the chunk in which it begins: that chunk's part and those of the chunks behind it.  Each wavefront looks at a chunk; what there is
+// to do, which is little, the workgroup does together, a stretch of the parts for each wavefront.
+constexpr int kPartsAhead = 8;
 template <class T>
 __global__ __launch_bounds__(kThreads) void apm_table_grad_join_kernel(TableGradArgs a) {
+    __shared__ float sums[kWaves][kVec][kWave];
+    __shared__ uint32_t rows[kWaves], parts_of[kWaves];
     const int lane = (int)threadIdx.x % kWave;
-    const uint32_t item = a.first_item + (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + threadIdx.x / kWave));
-    if (item >= a.chunks * a.slices) return;
-    const uint32_t chunk = item / a.slices, start = chunk * kChunk, next = start + kChunk;
-    if (next >= a.n) return;
-    const uint32_t row = row_at(a, next - 1);
-    if (row >= a.rows || row_at(a, next) != row) return;
-    if (start > 0 && row_at(a, start - 1) == row) return;  // began earlier still
-    const int64_t end = min(max(a.offsets[row + 1], (int64_t)next + 1), (int64_t)a.n);
-    const uint32_t last = (uint32_t)(end - 1) / kChunk;
-    const int col = (int)(item - chunk * a.slices) * kSlice + lane * kVec, there = max(0, min(kVec, a.cols - col));
-    if (there <= 0) return;
-    float sum[kVec];
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    auto item_of = [&](uint32_t w) { return a.first_item + blockIdx.x + w * gridDim.x; };  // neighbours, which may have the same row's slices, are for different workgroups
     {
-        const float* p = part_of(a, chunk, 1, col);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) sum[i] = p[i];
+        const uint32_t item = item_of(wave), chunk = item / a.slices, start = chunk * a.chunk, next = start + a.chunk;
+        uint32_t row = 0, parts = 0;
+        if (item < a.last_item && next < a.n) {
+            row = row_at(a, next - 1);
+            const uint32_t behind = row_at(a, next), ahead = start > 0 ? row_at(a, start - 1) : a.rows;
+            if (row < a.rows && behind == row && ahead != row) {  // neither ends here nor began earlier still
+                const int64_t end = min(max(a.offsets[row + 1], (int64_t)next + 1), (int64_t)a.n);
+                parts = (uint32_t)(end - 1) / a.chunk - chunk + 1;
+            }
+        }
+        if (lane == 0) rows[wave] = row, parts_of[wave] = parts;
     }
-    for (uint32_t c = chunk + 1; c <= last; c += 4) {
-        Raw<float> x[4];
+    __syncthreads();
+    for (uint32_t w = 0; w < kWaves; ++w) {
+        const uint32_t parts = (uint32_t)__builtin_amdgcn_readfirstlane((int)parts_of[w]), row = (uint32_t)__builtin_amdgcn_readfirstlane((int)rows[w]);
+        if (parts == 0) continue;
+        const uint32_t chunk = item_of(w) / a.slices, each = (parts + kWaves - 1) / kWaves, from = min(wave * each, parts), to = min(from + each, parts);
+        LaneCols l;
+        l.set((int)(item_of(w) - chunk * a.slices) * kSlice + lane * kVec, a.cols);
+        float sum[kVec] = {};
+        for (uint32_t c = from; c < to; c += kPartsAhead) {
+            Raw<float> x[kPartsAhead];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k].load(part_of(a, min(c + (uint32_t)k, last), 0, 0), col, c + (uint32_t)k <= last ? kVec : 0);
+            for (int k = 0; k < kPartsAhead; ++k) {
+                const uint32_t i = min(c + (uint32_t)k, to - 1);
+                x[k].load(part_of(a, chunk + i, i == 0 ? 1 : 0, 0), l.col, c + (uint32_t)k < to && l.n > 0 ? kVec : 0);
+            }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < kPartsAhead; ++k)
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) sum[i] += x[k][i];
+                for (int i = 0; i < kVec; ++i) sum[i] += x[k][i];
+        }
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sums[wave][i][lane] = sum[i];
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int v = 1; v < kWaves; ++v)
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) sum[i] += sums[v][i][lane];
+            finish_row<T>(a, row, l, sum);
+        }
+        __syncthreads();
     }
-    finish_row<T>(a, row, col, there, sum);
 }
 
 // ---- the gradient of the weights ----------------------------------------------------------------
 struct WeightGradArgs {
     const void* ids;
-    const char* dy;
-    const char* table;
+    apm_matrix dy, table;
     apm_vector dweights;
-    int64_t dy_stride, table_stride;
     int64_t n, first;
     int32_t per_token, cols, id_type;
     uint32_t rows;
@@ -292,28 +305,46 @@ __global__ __launch_bounds__(kThreads) void apm_lookup_weights_kernel(WeightGrad
     const int lane = (int)threadIdx.x % kWave;
     const int64_t p = a.first + (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     if (p >= a.n) return;
-    const uint32_t row = row_of(a.ids, a.id_type, p, a.rows);
+    const uint32_t row = (uint32_t)__builtin_amdgcn_readfirstlane((int)row_of(a.ids, a.id_type, p, a.rows));
     float sum = 0.0f;
     if (row < a.rows) {
-        const char* dy = a.dy + p / a.per_token * a.dy_stride * (int64_t)sizeof(D);
-        const char* x = a.table + (int64_t)row * a.table_stride * (int64_t)sizeof(T);
-#pragma unroll 2
-        for (int col = lane * kVec; col < a.cols; col += kSlice) {
-            const int n = min(kVec, a.cols - col);
-            Raw<D> d;
-            Raw<T> t;
-            d.load(dy, col, n);
-            t.load(x, col, n);
+        const int64_t token = p / a.per_token;
+        constexpr int kSlices = 2;  // under way
+        for (int col = 0; col < a.cols; col += kSlices * kSlice) {
+            LaneCols l[kSlices];
+            Raw<D> d[kSlices];
+            Raw<T> t[kSlices];
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) sum = fmaf(d[i], t[i], sum);
+            for (int s = 0; s < kSlices; ++s) {
+                l[s].set(col + s * kSlice + lane * kVec, a.cols);
+                const bool there = col + s * kSlice < a.cols;
+                load_row<0>(d[s], a.dy, token, a.cols, there, l[s]);
+                load_row<0>(t[s], a.table, row, a.cols, there, l[s]);
+            }
+#pragma unroll
+            for (int s = 0; s < kSlices; ++s) {
+                settle(d[s], l[s], a.cols);
+                settle(t[s], l[s], a.cols);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) sum = fmaf(d[s][i], t[s][i], sum);
+            }
         }
         sum = wave_sum(sum) * a.scale;
     }
     if (lane == 0) store1(a.dweights.data, a.dweights.dtype, p, sum);
 }
 
+// Positions of a wavefront: few, so that there are wavefronts for the whole chip, but no more of them than that, since rows that go beyond a chunk are
+// written and read once more.
+constexpr int64_t kChunksWanted = 4096;
+int64_t chunk_of(const apm_lookup& l) {
+    const int64_t n = l.tokens * l.per_token, slices = div_up(l.cols, kSlice);
+    int64_t chunk = kChunkLeast;
+    while (chunk < kChunkMost && div_up(n, chunk) * slices > kChunksWanted) chunk *= 2;
+    return chunk;
+}
 size_t room_of(const apm_lookup& l) {
-    return (size_t)div_up(l.tokens * l.per_token, kChunk) * 2 * (size_t)div_up(l.cols, kVec) * kVec * sizeof(float);
+    return (size_t)div_up(l.tokens * l.per_token, chunk_of(l)) * 2 * (size_t)div_up(l.cols, kVec) * kVec * sizeof(float);
 }
 
 int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, size_t workspace_bytes, void* stream) {
@@ -338,10 +369,10 @@ int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, 
     const int64_t most_items = max_workgroups(kThreads) * kWaves / 2;
     if (g.dtable.data) {
         TableGradArgs a{};
-        a.ids = l.ids.data, a.id_type = l.ids.type, a.dy = (const char*)g.dy.data, a.dtable = (char*)g.dtable.data, a.order = g.order, a.offsets = g.offsets;
-        a.parts = (float*)workspace, a.weights = l.weights, a.dy_stride = g.dy.stride, a.table_stride = g.dtable.stride;
+        a.ids = l.ids.data, a.id_type = l.ids.type, a.dy = g.dy, a.dtable = g.dtable, a.order = g.order, a.offsets = g.offsets;
+        a.parts = (float*)workspace, a.weights = l.weights;
         a.n = (uint32_t)n, a.rows = (uint32_t)l.rows, a.per_token = (uint32_t)l.per_token, a.cols = (int32_t)l.cols, a.cols_8 = (int32_t)(div_up(l.cols, kVec) * kVec);
-        a.chunks = (uint32_t)div_up(n, kChunk), a.slices = (uint32_t)div_up(l.cols, kSlice), a.empty = g.accumulate ? 0 : (uint32_t)div_up(l.rows, kEmptyRows);
+        a.chunk = (uint32_t)chunk_of(l), a.chunks = (uint32_t)div_up(n, a.chunk), a.slices = (uint32_t)div_up(l.cols, kSlice), a.empty = g.accumulate ? 0 : (uint32_t)div_up(l.rows, kEmptyRows);
         a.accumulate = g.accumulate, a.scale = (float)l.scale;
         const int64_t summing = (int64_t)a.chunks * a.slices, items = summing + a.empty;
         if (items > INT32_MAX) return fail(APM_EINVAL, "too many positions for so many columns");
@@ -356,8 +387,8 @@ int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, 
         }
         if (a.chunks > 1) {
             for (int64_t at = 0; at < summing; at += most_items) {
-                a.first_item = (uint32_t)at;
-                const dim3 grid((unsigned)div_up(std::min(most_items, summing - at), kWaves)), block(kThreads);
+                a.first_item = (uint32_t)at, a.last_item = (uint32_t)std::min(summing, at + most_items);
+                const dim3 grid((unsigned)div_up(a.last_item - at, kWaves)), block(kThreads);
                 if (g.dtable.dtype == APM_F32) hipLaunchKernelGGL(apm_table_grad_join_kernel<float>, grid, block, 0, s, a);
                 else hipLaunchKernelGGL(apm_table_grad_join_kernel<bf16>, grid, block, 0, s, a);
                 APM_HIP(hipGetLastError());
@@ -366,8 +397,8 @@ int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, 
     }
     if (g.dweights.data && n > 0) {
         WeightGradArgs a{};
-        a.ids = l.ids.data, a.id_type = l.ids.type, a.dy = (const char*)g.dy.data, a.table = (const char*)l.table.data, a.dweights = g.dweights;
-        a.dy_stride = g.dy.stride, a.table_stride = l.table.stride, a.n = n, a.per_token = (int32_t)l.per_token, a.cols = (int32_t)l.cols;
+        a.ids = l.ids.data, a.id_type = l.ids.type, a.dy = g.dy, a.table = l.table, a.dweights = g.dweights;
+        a.n = n, a.per_token = (int32_t)l.per_token, a.cols = (int32_t)l.cols;
         a.rows = (uint32_t)l.rows, a.scale = (float)l.scale;
         for (a.first = 0; a.first < n; a.first += most_items) {
             const dim3 grid((unsigned)div_up(std::min(most_items, n - a.first), kWaves)), block(kThreads);

@@ -1,4 +1,4 @@
-// What the kernels on tokens share: ids, and matrices taken eight columns at a time.
+// What the calls on tokens share: ids, and checks of arguments.
 #pragma once
 
 #include "apm_act.h"
@@ -11,24 +11,7 @@ __device__ __forceinline__ uint32_t row_of(const void* ids, int32_t type, int64_
     return id < rows ? (uint32_t)id : rows;
 }
 
-// Vectors of eight columns of a matrix, numbered row by row.  A workgroup divides once, for its first vector, and each lane makes up for what it is
-// further on: `at` / vecs is below 2^10 there, so that one correction makes up for the reciprocal's rounding.
-struct VecPlace {
-    uint32_t row;
-    int col, n;  // the first column, and how many of the eight exist
-    __device__ __forceinline__ VecPlace(uint32_t row0, uint32_t vec0, uint32_t further, uint32_t vecs, float inv_vecs, int cols) {
-        const uint32_t at = vec0 + further;
-        uint32_t r = (uint32_t)((float)at * inv_vecs);
-        int32_t left = (int32_t)(at - r * vecs);
-        if (left < 0) r -= 1, left += (int32_t)vecs;
-        else if (left >= (int32_t)vecs) r += 1, left -= (int32_t)vecs;
-        row = row0 + r;
-        col = left * kVec;
-        n = min(kVec, cols - col);
-    }
-};
-constexpr int64_t kMostCols = (int64_t)1 << 30;
-constexpr int64_t kMostVecs = (int64_t)1 << 30;  // of a launch
+constexpr int64_t kMostCols = (int64_t)1 << 28;  // a row is under 2^31 bytes
 
 inline int check_indices(const char* name, const apm_indices& i) {
     if (!i.data) return fail(APM_EINVAL, "%s is missing", name);

@@ -73,7 +73,7 @@ template <class Key> __device__ __forceinline__ uint32_t first_of(const Key* key
 // ---- one workgroup ------------------------------------------------------------------------------
 // Positions lie in LDS in the order of the passes so far, each wavefront takes a stretch of them into registers: counts of each digit in each
 // stretch, what stands before, and back to LDS in the new order.
-constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / kWave, kOneMost = 16;  // positions of a thread
+constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / kWave, kOneMost = 2;  // positions of a thread
 constexpr uint32_t kOnePositions = kOneThreads * kOneMost;
 template <int PER>
 __global__ __launch_bounds__(kOneThreads) void apm_sort_one_kernel(SortArgs a, uint32_t* sorted) {
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kOneThreads) void apm_sort_one_kernel(SortArgs a, u
 }
 
 // ---- many workgroups ----------------------------------------------------------------------------
-constexpr int kManyThreads = 256, kManyWaves = kManyThreads / kWave;
+constexpr int kManyThreads = 1024, kManyWaves = kManyThreads / kWave;
 
 struct PassArgs {
     const uint32_t* keys;  // nullptr: the ids, positions in their order
@@ -167,74 +167,141 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs& a, const PassArgs& s,
     return s.keys ? s.keys[i] : row_of(a.ids, a.id_type, i, a.rows);
 }
 
-__global__ __launch_bounds__(kManyThreads) void apm_sort_count_kernel(SortArgs a, PassArgs s) {
-    __shared__ uint32_t counts[kDigits];
-    counts[threadIdx.x] = 0;
-    __syncthreads();
-    const uint32_t begin = blockIdx.x * s.tile, end = (uint32_t)min((uint64_t)a.n, (uint64_t)begin + s.tile);
-#pragma unroll 4
-    for (uint32_t i = begin + threadIdx.x; i < end; i += kManyThreads) atomicAdd(&counts[(key_of(a, s, i) >> s.shift) & (kDigits - 1)], 1u);
-    __syncthreads();
-    s.counts[(uint64_t)blockIdx.x * kDigits + threadIdx.x] = counts[threadIdx.x];
+// Adds the wavefront's digits to counts in LDS.  Keys that earlier passes have put side by side are often equal, and additions to one place come one after the
+// other: the first lane of a run of equal digits adds the whole run (16384 words, the second pass: 15 us each for itself, so 7).
+__device__ __forceinline__ void count(uint32_t* counts, uint32_t digit, bool there) {
+    const uint32_t lane = threadIdx.x % kWave, left = (uint32_t)__shfl_up((int)digit, 1);
+    const uint64_t in = __ballot(there), first = __ballot(there && (lane == 0 || left != digit));
+    if (!((first >> lane) & 1)) return;
+    const uint64_t above = lane == kWave - 1 ? 0 : first >> (lane + 1);
+    const uint32_t next = above ? lane + 1 + (uint32_t)__builtin_ctzll(above) : (uint32_t)__popcll(in);  // lanes that are there are the first ones
+    atomicAdd(&counts[digit], next - lane);
 }
 
+__global__ __launch_bounds__(kManyThreads) void apm_sort_count_kernel(SortArgs a, PassArgs s) {
+    __shared__ uint32_t counts[kDigits];
+    const uint32_t begin = blockIdx.x * s.tile, end = (uint32_t)min((uint64_t)a.n, (uint64_t)begin + s.tile);
+    uint32_t key = key_of(a, s, min(begin + threadIdx.x, end - 1));
+    if (threadIdx.x < kDigits) counts[threadIdx.x] = 0;
+    __syncthreads();
+    for (uint32_t base = begin; base < end; base += kManyThreads) {
+        count(counts, (key >> s.shift) & (kDigits - 1), base + threadIdx.x < end);
+        if (base + kManyThreads < end) key = key_of(a, s, min(base + kManyThreads + threadIdx.x, end - 1));
+    }
+    __syncthreads();
+    if (threadIdx.x < kDigits) s.counts[(uint64_t)blockIdx.x * kDigits + threadIdx.x] = counts[threadIdx.x];
+}
+
+// ONCE: a tile is a position for each thread.  Otherwise each wavefront goes through its stretch twice, to count it and to put it in place.
+template <bool ONCE>
 __global__ __launch_bounds__(kManyThreads) void apm_sort_place_kernel(SortArgs a, PassArgs s) {
-    static_assert(kManyThreads == kDigits, "a thread has a digit");
     __shared__ uint32_t next[kManyWaves][kDigits];
+    __shared__ uint32_t seen[2][kDigits];  // positions with a digit: of the tiles before this one, of the others
     __shared__ uint32_t of_waves[kDigits / kWave];
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    uint32_t all = 0, mine = 0;  // positions with the thread's digit: of all tiles, of those before this one
-#pragma unroll 8
-    for (uint32_t t = 0; t < s.tiles; ++t) {
-        const uint32_t c = s.counts[(uint64_t)t * kDigits + (uint32_t)tid];
-        if (t < blockIdx.x) mine += c;
-        all += c;
-    }
-    const uint32_t before = before_among_digits(all, of_waves);
-    // One pass sorts all, and its digits are the rows: their counts are the offsets.
-    if (a.offsets && a.passes == 1 && blockIdx.x == 0 && (uint32_t)tid <= a.rows) a.offsets[tid] = before;
     const uint32_t begin = blockIdx.x * s.tile, end = (uint32_t)min((uint64_t)a.n, (uint64_t)begin + s.tile), each = s.tile / kManyWaves;
     const uint32_t from = (uint32_t)min((uint64_t)begin + (uint64_t)wave * each, (uint64_t)end), to = (uint32_t)min((uint64_t)from + each, (uint64_t)end);
-#pragma unroll
-    for (int w = 0; w < kManyWaves; ++w) next[w][tid] = 0;
+    auto key_at = [&](uint32_t i) { return i < to ? key_of(a, s, i) : 0u; };
+    auto position_at = [&](uint32_t i) { return s.at && i < to ? (uint32_t)s.at[i] : i; };
+    const uint32_t key0 = key_at(from + (uint32_t)lane), p0 = position_at(from + (uint32_t)lane);
+    uint32_t sum[2] = {0, 0};
+    constexpr uint32_t kParts = kManyThreads / kDigits;
+#pragma unroll 8
+    for (uint32_t t = (uint32_t)tid / kDigits; t < s.tiles; t += kParts) {
+        const uint32_t c = s.counts[(uint64_t)t * kDigits + (uint32_t)tid % kDigits];
+        sum[0] += t < blockIdx.x ? c : 0;
+        sum[1] += t < blockIdx.x ? 0 : c;
+    }
+    for (int i = tid; i < kManyWaves * kDigits; i += kManyThreads) (&next[0][0])[i] = 0;
+    if (tid < 2 * kDigits) (&seen[0][0])[tid] = 0;
     __syncthreads();
-    for (uint32_t i = from + (uint32_t)lane; i < to; i += kWave) atomicAdd(&next[wave][(key_of(a, s, i) >> s.shift) & (kDigits - 1)], 1u);
+    uint64_t same = 0;
+    uint32_t below = 0;
+    if constexpr (ONCE) {
+        const uint32_t digit = (key0 >> s.shift) & (kDigits - 1);
+        const bool there = from + (uint32_t)lane < to;
+        same = same_digit(digit, there), below = lanes_below(same);
+        if (there && below == 0) next[wave][digit] = (uint32_t)__popcll(same);
+    } else {
+        for (uint32_t base = from; base < to; base += kWave) count(next[wave], (key_at(base + (uint32_t)lane) >> s.shift) & (kDigits - 1), base + (uint32_t)lane < to);
+    }
+    atomicAdd(&seen[0][tid % kDigits], sum[0]);
+    atomicAdd(&seen[1][tid % kDigits], sum[1]);
     __syncthreads();
-    uint32_t sum = before + mine;
+    const uint32_t mine = tid < kDigits ? seen[0][tid] : 0, all = tid < kDigits ? mine + seen[1][tid] : 0;
+    const uint32_t before = before_among_digits(all, of_waves);
+    if (tid < kDigits) {
+        // One pass sorts all, and its digits are the rows: their counts are the offsets.
+        if (a.offsets && a.passes == 1 && blockIdx.x == 0 && (uint32_t)tid <= a.rows) a.offsets[tid] = before;
+        uint32_t sum = before + mine;
 #pragma unroll
-    for (int w = 0; w < kManyWaves; ++w) {
-        const uint32_t c = next[w][tid];
-        next[w][tid] = sum;
-        sum += c;
+        for (int w = 0; w < kManyWaves; ++w) {
+            const uint32_t c = next[w][tid];
+            next[w][tid] = sum;
+            sum += c;
+        }
     }
     __syncthreads();
+    auto place = [&](uint32_t at, uint32_t key, uint32_t p) {
+        if (s.keys_out) s.keys_out[at] = key;
+        if (s.at_out) s.at_out[at] = (int32_t)p;
+        else put(a, at, p, key);
+    };
+    if constexpr (ONCE) {
+        if (from + (uint32_t)lane < to) place(next[wave][(key0 >> s.shift) & (kDigits - 1)] + below, key0, p0);
+        return;
+    }
     for (uint32_t base = from; base < to; base += kWave) {
         const uint32_t i = base + (uint32_t)lane;
         const bool there = i < to;
-        const uint32_t key = there ? key_of(a, s, i) : 0u, digit = (key >> s.shift) & (kDigits - 1), p = there && s.at ? (uint32_t)s.at[i] : i;
-        const uint64_t same = same_digit(digit, there);
-        const uint32_t below = lanes_below(same);
+        const uint32_t key = key_at(i), digit = (key >> s.shift) & (kDigits - 1), p = position_at(i);
+        same = same_digit(digit, there), below = lanes_below(same);
         uint32_t at = 0;
         if (there) at = next[wave][digit] + below;
         among_lanes();
         if (there && below == 0) next[wave][digit] = at + (uint32_t)__popcll(same);
         among_lanes();
-        if (!there) continue;
-        if (s.keys_out) s.keys_out[at] = key;
-        if (s.at_out) s.at_out[at] = (int32_t)p;
-        else put(a, at, p, key);
+        if (there) place(at, key, p);
     }
 }
 
-// offsets where the sorted keys are in memory: each row looks for its first.
+// offsets where the sorted keys are in memory: a workgroup finds where its rows begin and end, all lanes of a wavefront looking at once, and each of its rows
+// looks between.
 constexpr int kOffsetThreads = 256;
+constexpr uint32_t kKeysMost = 4096;
+__device__ __forceinline__ uint32_t first_of_wave(const uint32_t* keys, uint32_t n, uint32_t row) {
+    const uint32_t lane = threadIdx.x % kWave;
+    uint32_t lo = 0, hi = n;  // it is one of lo .. hi
+    while (lo < hi) {
+        const uint32_t step = (hi - lo + kWave - 1) / kWave, i = lo + lane * step;
+        const uint32_t below = (uint32_t)__popcll(__ballot(i < hi && keys[i < hi ? i : lo] < row));  // of the lanes' keys, sorted as they are
+        if (below == 0) return lo;
+        hi = min(hi, lo + below * step);
+        lo += (below - 1) * step + 1;
+    }
+    return lo;
+}
 __global__ __launch_bounds__(kOffsetThreads) void apm_sort_offsets_kernel(const uint32_t* keys, uint32_t n, uint32_t rows, int64_t* offsets) {
-    const uint32_t r = blockIdx.x * kOffsetThreads + threadIdx.x;
-    if (r <= rows) offsets[r] = first_of(keys, n, r);
+    __shared__ uint32_t ends[2];
+    __shared__ uint32_t near[kKeysMost];
+    const uint32_t first = blockIdx.x * kOffsetThreads, wave = threadIdx.x / kWave;
+    if (wave < 2) {
+        const uint32_t at = first_of_wave(keys, n, wave == 0 ? first : (uint32_t)min((uint64_t)first + kOffsetThreads, (uint64_t)rows + 1));
+        if (threadIdx.x % kWave == 0) ends[wave] = at;
+    }
+    __syncthreads();
+    const uint32_t lo = ends[0], count = ends[1] - lo, r = first + threadIdx.x;
+    if (count <= kKeysMost) {
+        for (uint32_t i = threadIdx.x; i < count; i += kOffsetThreads) near[i] = keys[lo + i];
+        __syncthreads();
+        if (r <= rows) offsets[r] = lo + first_of(near, count, r);
+    } else if (r <= rows) {
+        offsets[r] = lo + first_of(keys + lo, count, r);
+    }
 }
 
-constexpr int64_t kTilesMost = 512, kTileLeast = 4096;
-constexpr uint32_t kOneRows = 4096;  // offsets of so many rows are written by the one workgroup
+constexpr int64_t kTilesMost = 512, kTileLeast = kManyThreads;
+constexpr uint32_t kOneRows = 4096;        // offsets of so many rows are written by the one workgroup
 
 struct SortShape {
     bool one;
@@ -290,7 +357,6 @@ int sort_tokens(const apm_token_order* op, void* workspace, size_t workspace_byt
         sorted = (const uint32_t*)workspace, search = !a.alone;
         auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(1), dim3(kOneThreads), 0, st, a, (uint32_t*)workspace); };
         if (a.n <= kOneThreads) start(apm_sort_one_kernel<1>);
-        else if (a.n <= 4 * kOneThreads) start(apm_sort_one_kernel<4>);
         else start(apm_sort_one_kernel<kOneMost>);
         APM_HIP(hipGetLastError());
     } else {
@@ -307,7 +373,8 @@ int sort_tokens(const apm_token_order* op, void* workspace, size_t workspace_byt
             s.keys_out = !last || (o.offsets && pass > 0) ? keys[pass % 2] : nullptr, s.at_out = last ? nullptr : at[pass % 2];
             s.counts = counts, s.shift = pass * kDigitBits, s.tile = shape.tile, s.tiles = shape.tiles;
             hipLaunchKernelGGL(apm_sort_count_kernel, dim3(shape.tiles), dim3(kManyThreads), 0, st, a, s);
-            hipLaunchKernelGGL(apm_sort_place_kernel, dim3(shape.tiles), dim3(kManyThreads), 0, st, a, s);
+            auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(shape.tiles), dim3(kManyThreads), 0, st, a, s); };
+            shape.tile == kManyThreads ? start(apm_sort_place_kernel<true>) : start(apm_sort_place_kernel<false>);
             APM_HIP(hipGetLastError());
             if (last) sorted = s.keys_out, search = o.offsets && pass > 0;
         }

@@ -46,7 +46,7 @@ def lookup(**over):
 
 def test_lookup_forward():
     go = lambda **o: apm.lib().apm_lookup_forward(lookup(**o), None)
-    for bad in (dict(tokens=-1), dict(per_token=0), dict(rows=0), dict(rows=apm.APM_MAX_POSITIONS + 1), dict(cols=0), dict(cols=2 ** 30 + 1),
+    for bad in (dict(tokens=-1), dict(per_token=0), dict(rows=0), dict(rows=apm.APM_MAX_POSITIONS + 1), dict(cols=0), dict(cols=2 ** 28 + 1),
                 dict(tokens=2 ** 30, per_token=2), dict(tokens=2 ** 62, per_token=8), dict(tokens=1, per_token=2 ** 62)):
         refused(go(**bad), apm.APM_EINVAL, "bad size")
         assert apm.apm_lookup_workspace_bytes(lookup(**bad)) == 0
@@ -94,7 +94,7 @@ def product(**over):
 
 def test_grouped_product():
     go = lambda room=PTR, size=1 << 40, **o: apm.lib().apm_grouped_product(product(**o), room, size, None)
-    for bad in (dict(tokens=-1), dict(tokens=2 ** 41), dict(out=0), dict(out=2 ** 30 + 1), dict(n_groups=-1), dict(n_groups=2 ** 31), {"in": 0}, {"in": 2 ** 31}):
+    for bad in (dict(tokens=-1), dict(tokens=2 ** 41), dict(out=0), dict(out=2 ** 28 + 1), dict(n_groups=-1), dict(n_groups=2 ** 31), {"in": 0}, {"in": 2 ** 31}):
         refused(go(**bad), apm.APM_EINVAL, "bad size")
         assert apm.apm_grouped_product_workspace_bytes(product(**bad)) == 0
     refused(go(offsets=None), apm.APM_EINVAL, "contradict")
@@ -109,7 +109,7 @@ def test_grouped_product():
     refused(go(bias=apm.apm_vector(PTR + 1, apm.APM_BF16, 0)), apm.APM_EINVAL, "bias is not aligned")
     refused(go(y=matrix(None)), apm.APM_EINVAL, "y is missing")
     refused(go(y=matrix(stride=63)), apm.APM_EINVAL, "y: a row stride")
-    refused(go(tokens=2 ** 40, out=2 ** 30, y=matrix(stride=2 ** 30), x=matrix(stride=0), size=1 << 62), apm.APM_EINVAL, "")
+    refused(go(tokens=2 ** 40, out=2 ** 28, y=matrix(stride=2 ** 28), x=matrix(stride=0), size=1 << 62), apm.APM_EINVAL, "")
     refused(apm.lib().apm_grouped_product(None, None, 0, None), apm.APM_EINVAL, "missing")
     assert go(tokens=0) == apm.APM_OK
 
@@ -120,7 +120,7 @@ def dropout(**over):
 
 def test_dropout():
     go = lambda **o: apm.lib().apm_dropout_apply(dropout(**o), None)
-    for bad in (dict(rows=-1), dict(cols=0), dict(cols=2 ** 30 + 1), dict(first_row=-1)):
+    for bad in (dict(rows=-1), dict(cols=0), dict(cols=2 ** 28 + 1), dict(first_row=-1)):
         refused(go(**bad), apm.APM_EINVAL, "bad size")
     for p in (-0.1, 1.1, float("nan")):
         refused(go(p=p), apm.APM_EINVAL, "no probability")
