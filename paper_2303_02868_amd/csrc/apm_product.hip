@@ -4,6 +4,8 @@
 // counts the groups' tiles of rows and finds its own, those behind the last tile leave at once.  Tiles of x and w go into LDS by a ring of stages, each a stretch
 // of k, as they lie in memory: k runs along the rows of x, and of w unless that is transposed, which is then read with the transposing loads.
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "apm_tok.h"
 
@@ -18,19 +20,29 @@ typedef __attribute__((address_space(3))) char lds_char;
 constexpr int kWave = 64;
 constexpr int kFrag = 32, kStep = 16;  // a matrix instruction's tile, and the stretch of k that it takes
 
-// A workgroup's tile of y: WM x WN wavefronts of FM x FN fragments, K of k in a stage, STAGES of them in LDS.
-template <int WM_, int WN_, int FM_, int FN_, int K_, int STAGES_>
+// A workgroup's tile of y: WM x WN wavefronts of FM x FN fragments, K of k in a stage, of which there is room in LDS for SLOTS / 2: for a half more where SLOTS is odd,
+// which then is x's.
+template <int WM_, int WN_, int FM_, int FN_, int K_, int SLOTS_>
 struct Tile {
-    static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, K = K_, kStages = STAGES_;
+    static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, K = K_, kSlots = SLOTS_, kStages = SLOTS_ / 2;
+    static constexpr bool kHalf = SLOTS_ % 2 != 0;
     static constexpr int kM = WM * FM * kFrag, kN = WN * FN * kFrag, kWaves = WM * WN, kThreads = kWaves * kWave;
     static constexpr int kBytesA = kM * K * 2, kBytesB = kN * K * 2, kStage = kBytesA + kBytesB;
     static constexpr int kA = kBytesA / 1024 / kWaves, kB = kBytesB / 1024 / kWaves;  // 16 bytes a lane, of x and of w, in a stage
+    static constexpr int kLds = kStages * kStage + (kHalf ? kBytesA : 0);
+    static_assert(!kHalf || kBytesA == kBytesB, "a slot is for either");
+    // Where stage j's tile of x or w lies: the slots are taken in turn, x, w, x, w.
+    static __device__ __forceinline__ int place_of(int j, bool w) {
+        return kHalf ? (2 * j + (w ? 1 : 0)) % kSlots * kBytesA : j % kStages * kStage + (w ? kBytesA : 0);
+    }
     static_assert(kA * 1024 * kWaves == kBytesA && kB * 1024 * kWaves == kBytesB, "whole vectors for every lane");
 };
-typedef Tile<2, 4, 4, 2, 32, 4> Large;
-typedef Tile<2, 2, 2, 2, 32, 4> Small;
-typedef Tile<2, 2, 1, 1, 64, 3> Tiny;
-typedef Tile<1, 4, 1, 1, 64, 4> Thin;
+typedef Tile<2, 4, 4, 2, 64, 5> Large;
+typedef Tile<2, 2, 2, 2, 64, 4> Small;
+typedef Tile<2, 2, 1, 1, 64, 6> Tiny;
+// Large where rows go through registers: stages of half the length, so that what is on its way fits beside the sums.
+typedef Tile<2, 4, 4, 2, 32, 4> LargeAny;
+typedef Tile<2, 2, 1, 1, 64, 4> TinyAny;
 
 struct ProductArgs {
     const char* x;
@@ -52,7 +64,7 @@ template <int K> __device__ __forceinline__ bf16x8 read_fragment(const lds_char*
     return *(lds_ptr)(tile + lds_at<K>(frag * kFrag + lane % 32, step * 2 + lane / 32));
 }
 // Rows of N elements for the transposing loads: 64-byte chunks are exchanged, so that the four rows that such a load takes a chunk of lie in different banks.
-template <int N> __device__ __forceinline__ int exchange_t(int row) { return N >= 128 ? row & 3 : (row >> 1) & 1; }
+template <int N> __device__ __forceinline__ int exchange_t(int row) { return N >= 128 ? row & 3 : N == 64 ? (row >> 1) & 1 : 0; }
 template <int N> __device__ __forceinline__ int lds_at_t(int row, int vec) { return row * (N * 2) + (((vec >> 2) ^ exchange_t<N>(row)) << 6) + ((vec & 3) << 4); }
 template <int N> __device__ __forceinline__ bf16x8 read_fragment_t(const lds_char* tile, int frag, int step, int lane) {
     typedef __attribute__((address_space(3))) s16x4* lds_ptr;
@@ -89,55 +101,59 @@ template <int M> __device__ __forceinline__ uint32_t tiles_up_to(const ProductAr
     return t;
 }
 
-// 16 bytes a lane from memory into LDS, to 16 lane bytes behind `to`; zeros for what lies behind the buffer's end.  The compiler does not wait for what
-// these bring before it reads LDS: wait_loads and meet do.
-__device__ __forceinline__ void load_to_lds(Rsrc buffer, uint32_t at, uint32_t to) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (__attribute__((address_space(3))) void*)(uintptr_t)to, 16, (int)at, 0, 0, 0);
+// 16 bytes a lane from memory into LDS, to 16 lane bytes behind `to` (M0); zeros for what lies behind the buffer's end.  In assembly, which does not tell the
+// compiler that it writes LDS: told so, it waits for these loads in front of transposing reads of other places (16384 x 4096 x 4096: 500 us).  wait_loads and meet wait.
+__device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t at, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(buffer));
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 // The wavefront's accesses to LDS are done, and so are everyone's.
 __device__ __forceinline__ void meet() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
-__device__ __forceinline__ Rsrc buffer_of(const char* p, uint32_t bytes) {
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ u32x4 buffer_of(const char* p, uint32_t bytes) {
     const uint64_t at = (uint64_t)p;
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32));
-    return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000);
+    return u32x4{lo, hi & 0xffffu, (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00027000u};
 }
-constexpr uint32_t kNowhere = 0x80000000u;  // behind the end of any buffer here
+constexpr uint32_t kNowhere = 0x80000000u;  // behind the end of any buffer here, and so is what is less than 2^30 further on
 
+// The order that the scheduler is to keep in a step: in front of each product its part of the LDS reads for the next step, behind it its part of the loads.
+template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinline__ void in_turn() {
+    if constexpr (I < PRODUCTS) {
+        constexpr int kFirst = LOADS > 0 ? 1 : (PRODUCTS + 1) / 2;  // in front of so many products
+        if constexpr (I < kFirst) __builtin_amdgcn_sched_group_barrier(0x100, (I + 1) * READS / kFirst - I * READS / kFirst, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x020, (I + 1) * LOADS / PRODUCTS - I * LOADS / PRODUCTS, 0);
+        in_turn<PRODUCTS, READS, LOADS, I + 1>();
+    }
+}
+
+// Which tile a workgroup has.  Workgroups go to the XCDs in turn; each XCD takes a stretch of the order, in which tiles come strip by strip.
 constexpr int kXcds = 8, kStrip = 4;  // tiles of rows that are walked together
-
-// DIRECT: the tiles go from memory into LDS without passing through registers, which needs whole vectors of sixteen bytes: aligned rows, and widths of a multiple
-// of eight.  The other form takes any.
-template <class T, bool TRANSPOSED, bool DIRECT>
-__global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a) {
-    constexpr int FM = T::FM, FN = T::FN, S = T::kStages, kSteps = T::K / kStep;
-    static_assert(kSteps % 2 == 0, "two sets of fragments");
-    __shared__ __attribute__((aligned(1024))) char lds_all[S * T::kStage];
-    lds_char* const lds = (lds_char*)lds_all;
-    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-
-    // Which tile.  Workgroups go to the XCDs in turn; each XCD takes a stretch of the order, in which tiles come strip by strip.
-    int64_t begin = 0, end = a.tokens;
-    int group = 0;
-    uint32_t row_tile, n_tile;
-    {
+struct Place {
+    int64_t row, end;  // the tile's first, and where its group ends
+    int group, n_tile;
+    // false: there are fewer tiles.  M: rows of a tile.
+    template <int M> __device__ __forceinline__ bool find(const ProductArgs& a, int lane) {
         uint32_t rows = 0;
         if (a.offsets) {
-            for (int g = 0; g < a.groups; g += kWave) rows += (uint32_t)__builtin_amdgcn_readlane((int)tiles_up_to<T::kM>(a, g, lane), kWave - 1);
+            for (int g = 0; g < a.groups; g += kWave) rows += (uint32_t)__builtin_amdgcn_readlane((int)tiles_up_to<M>(a, g, lane), kWave - 1);
         } else {
-            rows = (uint32_t)((a.tokens + T::kM - 1) / T::kM);
+            rows = (uint32_t)((a.tokens + M - 1) / M);
         }
         const uint32_t tiles = rows * (uint32_t)a.tiles_n, nth = blockIdx.x;
-        if (nth >= tiles) return;
+        if (nth >= tiles) return false;
         const uint32_t xcd = nth % kXcds, id = xcd * (tiles / kXcds) + min(xcd, tiles % kXcds) + nth / kXcds;
         const uint32_t strip = id / (uint32_t)(kStrip * a.tiles_n), in_strip = id - strip * (uint32_t)(kStrip * a.tiles_n), high = min((uint32_t)kStrip, rows - strip * kStrip);
-        row_tile = strip * kStrip + in_strip % high, n_tile = in_strip / high;
+        uint32_t row_tile = strip * kStrip + in_strip % high;
+        n_tile = (int)(in_strip / high);
+        group = 0;
         if (a.offsets) {
             uint32_t before = 0;
             for (int g = 0; g < a.groups; g += kWave) {
-                const uint32_t up = before + tiles_up_to<T::kM>(a, g, lane);
+                const uint32_t up = before + tiles_up_to<M>(a, g, lane);
                 const uint64_t further = __ballot(up > row_tile);
                 if (further) {
                     const int l = __builtin_ctzll(further);
@@ -149,11 +165,69 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
             }
             group = __builtin_amdgcn_readfirstlane(group);
             row_tile = (uint32_t)__builtin_amdgcn_readfirstlane((int)row_tile);
-            group_of(a, group, &begin, &end);
         }
+        int64_t begin;
+        group_of(a, group, &begin, &end);
+        row = begin + (int64_t)row_tile * M;
+        return true;
     }
-    const int64_t m0 = begin + (int64_t)row_tile * T::kM;
-    const int n0 = (int)n_tile * T::kN;
+};
+
+// Eight columns of rows of y from their sums: bias, what y held, rounding.
+struct Finish {
+    float bias[kVec] = {};
+    int col;
+    __device__ __forceinline__ Finish(const ProductArgs& a, int group, int col, int n) : col(col) {
+        if (!a.bias.data) return;
+        const int64_t first = (int64_t)group * a.out + (n > 0 ? col : 0);
+        RawAny raw;
+        raw.load((const char*)a.bias.data + first * (a.bias.dtype == APM_F32 ? 4 : 2), a.bias.dtype, 0, n);
+        raw.get(a.bias.dtype, bias);
+    }
+    __device__ __forceinline__ void row(const ProductArgs& a, int64_t t, int n, float (&v)[kVec]) const {
+        char* to = a.y + t * a.y_stride * (a.y_type == APM_F32 ? 4 : 2);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] += bias[e];
+        if (a.accumulate) {
+            RawAny old;
+            old.load(to, a.y_type, n > 0 ? col : 0, n);
+            float f[kVec];
+            old.get(a.y_type, f);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[e] += f[e];
+        }
+        if (a.y_type == APM_F32) store8<float>(to, col, n, v);
+        else store8<bf16>(to, col, n, v);
+    }
+};
+
+// Eight elements of a row of `width`.  Where fewer of them are there, the row's last eight are loaded, and `fit`, when they are needed, moves those that are down to
+// their places and puts zeros in the others: no branch, and no trip to memory for each.
+__device__ __forceinline__ u32x4 load_vec(const char* row, int64_t col, int width) {
+    if (width < kVec) return width > col ? load_short((const uint16_t*)row + col, width - (int)col) : u32x4{0u, 0u, 0u, 0u};
+    return *(const u32x4_any*)(row + min(col, (int64_t)width - kVec) * 2);
+}
+__device__ __forceinline__ u32x4 fit(u32x4 v, int64_t col, int width) {
+    const int n = width - (int)col;
+    if (width < kVec || n >= kVec) return v;
+    move_down(v, max(n, 1));
+    return n > 0 ? v : u32x4{0u, 0u, 0u, 0u};
+}
+
+// DIRECT: the tiles go from memory into LDS without passing through registers, which needs whole vectors of sixteen bytes: aligned rows, and widths of a multiple
+// of eight.  The other form takes any.
+template <class T, bool TRANSPOSED, bool DIRECT>
+__global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a) {
+    constexpr int FM = T::FM, FN = T::FN, S = T::kStages, kSteps = T::K / kStep;
+    static_assert(kSteps % 2 == 0, "two sets of fragments");
+    __shared__ __attribute__((aligned(1024))) char lds_all[T::kLds];
+    lds_char* const lds = (lds_char*)lds_all;
+    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+
+    Place at;
+    if (!at.find<T::kM>(a, lane)) return;
+    const int64_t m0 = at.row, end = at.end;
+    const int n0 = at.n_tile * T::kN, group = at.group;
     const char* const w = a.w + (int64_t)group * a.w_group_stride * 2;
     const int stages = (a.in + T::K - 1) / T::K;
 
@@ -161,8 +235,9 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
     constexpr int kVecsK = T::K / kVec, kVecsN = T::kN / kVec;
     uint32_t at_a[T::kA], at_b[T::kB];    // DIRECT: bytes from the tile's corner
     int vec_a[T::kA], vec_b[T::kB];       // the vector's place in k
-    Rsrc buf_a, buf_b;
-    u32x4 ra[T::kA], rb[T::kB];           // otherwise: a stage on its way
+    u32x4 buf_a, buf_b;
+    constexpr int kSets = 2;
+    u32x4 ra[kSets][T::kA], rb[kSets][T::kB];  // otherwise: stages on their way
     if constexpr (DIRECT) {
         const int rows_a = (int)min((int64_t)T::kM, end - m0), rows_b = min(T::kN, a.out - n0);
         buf_a = buffer_of(a.x + m0 * a.x_stride * 2, (uint32_t)((rows_a - 1) * a.x_stride * 2 + (int64_t)a.in * 2));
@@ -190,69 +265,71 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
         }
     }
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
-    auto bring = [&](int j) {  // stage j, DIRECT
-        const uint32_t to = lds_base + (uint32_t)(j % S) * T::kStage;
+    // DIRECT: stage j of x, and of w; `whole` if k does not end in it
+    auto bring_a = [&](int j, auto whole) {
+        const uint32_t to = lds_base + (uint32_t)T::place_of(j, false) + (uint32_t)wave * (T::kA * 1024u);
         const int k0 = j * T::K;
-        const bool whole = k0 + T::K <= a.in;
 #pragma unroll
         for (int i = 0; i < T::kA; ++i) {
             uint32_t at = at_a[i] + (uint32_t)k0 * 2u;
-            if (at_a[i] == kNowhere || (!whole && k0 + vec_a[i] * kVec >= a.in)) at = kNowhere;
-            load_to_lds(buf_a, at, to + (uint32_t)(wave * T::kA + i) * 1024u);
+            if (!whole && k0 + vec_a[i] * kVec >= a.in) at = kNowhere;
+            load_to_lds(buf_a, at, to + i * 1024u);
         }
+    };
+    auto bring_b = [&](int j, auto whole) {
+        const uint32_t to = lds_base + (uint32_t)T::place_of(j, true) + (uint32_t)wave * (T::kB * 1024u);
+        const int k0 = j * T::K;
 #pragma unroll
         for (int i = 0; i < T::kB; ++i) {
-            uint32_t at;
-            if constexpr (TRANSPOSED) {
-                at = at_b[i] + (uint32_t)k0 * (uint32_t)a.w_stride * 2u;
-                if (!whole && k0 + vec_b[i] >= a.in) at = kNowhere;
-            } else {
-                at = at_b[i] + (uint32_t)k0 * 2u;
-                if (at_b[i] == kNowhere || (!whole && k0 + vec_b[i] * kVec >= a.in)) at = kNowhere;
-            }
-            load_to_lds(buf_b, at, to + T::kBytesA + (uint32_t)(wave * T::kB + i) * 1024u);
+            uint32_t at = at_b[i] + (uint32_t)k0 * (TRANSPOSED ? (uint32_t)a.w_stride : 1u) * 2u;
+            if (!whole && k0 + (TRANSPOSED ? vec_b[i] : vec_b[i] * kVec) >= a.in) at = kNowhere;
+            load_to_lds(buf_b, at, to + i * 1024u);
         }
     };
     // Rows behind the group's last and columns behind the matrix's are some other ones: what comes of them is not stored.  Behind the end of k
     // there are zeros, in both operands.
-    auto fetch = [&](int j) {
+    auto fetch = [&](int j, int set) {
         const int k0 = j * T::K;
-        const bool whole = k0 + T::K <= a.in;
 #pragma unroll
         for (int i = 0; i < T::kA; ++i) {
-            const int place = i * T::kThreads + tid, row = place / kVecsK, k = k0 + place % kVecsK * kVec;
-            Raw<bf16> r;
-            r.load(a.x + min(m0 + row, end - 1) * a.x_stride * 2, k, whole ? kVec : a.in - k);
-            ra[i] = r.a;
+            const int place = i * T::kThreads + tid;
+            ra[set][i] = load_vec(a.x + min(m0 + place / kVecsK, end - 1) * a.x_stride * 2, k0 + place % kVecsK * kVec, a.in);
         }
 #pragma unroll
         for (int i = 0; i < T::kB; ++i) {
             const int place = i * T::kThreads + tid;
-            Raw<bf16> r;
-            if constexpr (TRANSPOSED) {
-                const int k = k0 + place / kVecsN, n = n0 + place % kVecsN * kVec;
-                r.load(w + (int64_t)k * a.w_stride * 2, n, k < a.in ? min(kVec, a.out - n) : 0);
-            } else {
-                const int row = place / kVecsK, k = k0 + place % kVecsK * kVec;
-                r.load(w + (int64_t)min(n0 + row, a.out - 1) * a.w_stride * 2, k, whole ? kVec : a.in - k);
-            }
-            rb[i] = r.a;
+            if constexpr (TRANSPOSED) rb[set][i] = load_vec(w + (int64_t)min(k0 + place / kVecsN, a.in - 1) * a.w_stride * 2, n0 + place % kVecsN * kVec, a.out);
+            else rb[set][i] = load_vec(w + (int64_t)min(n0 + place / kVecsK, a.out - 1) * a.w_stride * 2, k0 + place % kVecsK * kVec, a.in);
         }
     };
+    const bool n_ends = TRANSPOSED && n0 + T::kN > a.out;
     typedef __attribute__((address_space(3))) u32x4* lds_vec;
-    auto put = [&](int j) {
-        lds_char* const to = lds + j % S * T::kStage;
+    auto put_as = [&](int j, int set, auto ends) {
+        lds_char *const to_a = lds + T::place_of(j, false), *const to_b = lds + T::place_of(j, true);
+        const int k0 = j * T::K;
 #pragma unroll
         for (int i = 0; i < T::kA; ++i) {
             const int place = i * T::kThreads + tid;
-            *(lds_vec)(to + lds_at<T::K>(place / kVecsK, place % kVecsK)) = ra[i];
+            u32x4 v = ra[set][i];
+            if (ends) v = fit(v, k0 + place % kVecsK * kVec, a.in);
+            *(lds_vec)(to_a + lds_at<T::K>(place / kVecsK, place % kVecsK)) = v;
         }
 #pragma unroll
         for (int i = 0; i < T::kB; ++i) {
             const int place = i * T::kThreads + tid;
-            if constexpr (TRANSPOSED) *(lds_vec)(to + T::kBytesA + lds_at_t<T::kN>(place / kVecsN, place % kVecsN)) = rb[i];
-            else *(lds_vec)(to + T::kBytesA + lds_at<T::K>(place / kVecsK, place % kVecsK)) = rb[i];
+            u32x4 v = rb[set][i];
+            if constexpr (TRANSPOSED) {
+                if (ends) v = k0 + place / kVecsN < a.in ? fit(v, n0 + place % kVecsN * kVec, a.out) : u32x4{0u, 0u, 0u, 0u};
+                *(lds_vec)(to_b + lds_at_t<T::kN>(place / kVecsN, place % kVecsN)) = v;
+            } else {
+                if (ends) v = fit(v, k0 + place % kVecsK * kVec, a.in);
+                *(lds_vec)(to_b + lds_at<T::K>(place / kVecsK, place % kVecsK)) = v;
+            }
         }
+    };
+    auto put = [&](int j, int set) {
+        if (n_ends || j * T::K + T::K > a.in) put_as(j, set, std::true_type());
+        else put_as(j, set, std::false_type());
     };
 
     f32x16 acc[FM][FN];
@@ -265,75 +342,101 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
     const int wm = wave / T::WN * FM, wn = wave % T::WN * FN;  // the wavefront's first fragments
     bf16x8 fa[2][FM], fb[2][FN];
     auto read = [&](int j, int step) {
-        const lds_char* const from = lds + j % S * T::kStage;
-#pragma unroll
-        for (int m = 0; m < FM; ++m) fa[step % 2][m] = read_fragment<T::K>(from, wm + m, step, lane);
+        const lds_char *const from_a = lds + T::place_of(j, false), *const from_b = lds + T::place_of(j, true);
 #pragma unroll
         for (int n = 0; n < FN; ++n) {
-            if constexpr (TRANSPOSED) fb[step % 2][n] = read_fragment_t<T::kN>(from + T::kBytesA, wn + n, step, lane);
-            else fb[step % 2][n] = read_fragment<T::K>(from + T::kBytesA, wn + n, step, lane);
+            if constexpr (TRANSPOSED) fb[step % 2][n] = read_fragment_t<T::kN>(from_b, wn + n, step, lane);
+            else fb[step % 2][n] = read_fragment<T::K>(from_b, wn + n, step, lane);
         }
-    };
-    constexpr int kLoads = T::kA + T::kB;
-    if constexpr (DIRECT) {
 #pragma unroll
-        for (int j = 0; j < S; ++j)
-            if (j < stages) bring(j);
-        if (S <= stages) wait_loads<(S - 1) * kLoads>();
+        for (int m = 0; m < FM; ++m) fa[step % 2][m] = read_fragment<T::K>(from_a, wm + m, step, lane);
+    };
+    auto multiply = [&](int step) {
+#pragma unroll
+        for (int m = 0; m < FM; ++m)
+#pragma unroll
+            for (int n = 0; n < FN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[step % 2][m], fb[step % 2][n], acc[m][n], 0, 0, 0);
+    };
+    constexpr int kReads = FM + (TRANSPOSED ? 2 : 1) * FN, kLoads = T::kA + T::kB;
+    constexpr int kExtra = T::kHalf ? T::kA : 0;  // loads of a stage of x that is under way beyond the whole ones
+    auto bring = [&](int j, auto whole_a, auto whole_b) {  // what takes the place of stage j - S: of w stage j, of x that or the next one
+        const int ja = T::kHalf ? j + 1 : j;
+        if (whole_b || j < stages) bring_b(j, whole_b);
+        if (whole_a || ja < stages) bring_a(ja, whole_a);
+    };
+    auto is_whole = [&](int j) { return (j + 1) * T::K <= a.in; };
+    if constexpr (DIRECT) {
+        if (T::kHalf) bring_a(0, is_whole(0));
+#pragma unroll
+        for (int j = 0; j < S; ++j) bring(j, is_whole(T::kHalf ? j + 1 : j), is_whole(j));
+        if (S + (T::kHalf ? 1 : 0) <= stages) wait_loads<(S - 1) * kLoads + kExtra>();
         else wait_loads<0>();
     } else {
 #pragma unroll
-        for (int j = 0; j < S; ++j)
-            if (j < stages) fetch(j), put(j);
-        if (S < stages) fetch(S);
+        for (int j = 0; j < kSets; ++j)
+            if (j < stages) fetch(j, j);
+#pragma unroll
+        for (int j = 0; j < kSets; ++j)
+            if (j < stages) put(j, j);
+#pragma unroll
+        for (int j = kSets; j < 2 * kSets; ++j)
+            if (j < stages) fetch(j, j % kSets);
     }
     meet();
+    // Fragments are read a step ahead.  Before a stage's last step everybody has read that stage, whose place is filled anew, and the next stage is there.
+    auto others = [&](int j) {  // all steps of stage j but the last
+#pragma unroll
+        for (int s = 0; s + 1 < kSteps; ++s) {
+            read(j, s + 1);
+            multiply(s);
+            in_turn<FM * FN, kReads, 0>();
+        }
+    };
     read(0, 0);
-    // A stage, in steps.  Fragments are read a step ahead; before the last step everybody has read this stage, whose place is filled anew, and the
-    // next stage is there.
-    for (int j = 0; j < stages; ++j) {
+    others(0);
+    auto turn = [&](int j, auto&& fill) {
+        meet();
+        read(j + 1, 0);
+        fill();
+        multiply(kSteps - 1);
+        in_turn<FM * FN, kReads, DIRECT ? kLoads : 0>();
+        others(j + 1);
+    };
+    int j = 0;
+    if constexpr (DIRECT) {
+        for (const int whole = a.in / T::K - (T::kHalf ? 1 : 0); j + S < whole; ++j) {
+            wait_loads<(S - 2) * kLoads + kExtra>();
+            turn(j, [&] { bring(j + S, std::true_type(), std::true_type()); });
+        }
+        for (; j + 1 < stages; ++j) {
+            if (j + S + (T::kHalf ? 1 : 0) <= stages) wait_loads<(S - 2) * kLoads + kExtra>();
+            else wait_loads<0>();
+            turn(j, [&] { bring(j + S, is_whole(T::kHalf ? j + S + 1 : j + S), is_whole(j + S)); });
+        }
+    } else {
+        static_assert(S == kSets, "a stage's set of registers goes where the stage two before it was");
+        for (; j + 1 < stages; j += kSets) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const bool last = s == kSteps - 1;
-            if (last) {
-                if constexpr (DIRECT) {
-                    if (j + S <= stages) wait_loads<(S - 2) * kLoads>();
-                    else wait_loads<0>();
-                }
-                meet();
-                if (j + S < stages) {
-                    if constexpr (DIRECT) {
-                        bring(j + S);
-                    } else {
-                        put(j + S);
-                        if (j + S + 1 < stages) fetch(j + S + 1);
-                    }
-                }
+            for (int u = 0; u < kSets; ++u) {
+                if (j + u + 1 >= stages) break;
+                turn(j + u, [&] {
+                    if (j + u + S < stages) put(j + u + S, u);
+                    if (j + u + S + kSets < stages) fetch(j + u + S + kSets, u);
+                });
             }
-            read(last ? j + 1 : j, (s + 1) % kSteps);
-#pragma unroll
-            for (int m = 0; m < FM; ++m)
-#pragma unroll
-                for (int n = 0; n < FN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s % 2][m], fb[s % 2][n], acc[m][n], 0, 0, 0);
         }
     }
+    multiply(kSteps - 1);
     meet();
 
     // Lane l has column l mod 32 of a fragment's tile, rows 8 (r / 4) + 4 (l / 32) + r mod 4 in register r.  Rows are stored in whole vectors: half a fragment's
     // rows at a time go through LDS, each wavefront for itself.
     constexpr int kRow = FN * kFrag + 4, kPer = FN * kFrag / kVec, kRowsAtOnce = kWave / kPer;
-    static_assert(T::kWaves * 16 * kRow * 4 <= S * T::kStage, "the wavefronts' rows fit");
+    static_assert(T::kWaves * 16 * kRow * 4 <= T::kLds, "the wavefronts' rows fit");
     typedef __attribute__((address_space(3))) float lds_float;
     lds_float* const mine = (lds_float*)lds + wave * 16 * kRow;
     const int c = lane % kPer * kVec, col = n0 + wn * kFrag + c, there = max(0, min(kVec, a.out - col));
-    const int size = a.y_type == APM_F32 ? 4 : 2;
-    float bias[kVec] = {};
-    if (a.bias.data) {
-        RawAny raw;
-        const int64_t first = (int64_t)group * a.out + (there > 0 ? col : 0);
-        raw.load((const char*)a.bias.data + first * (a.bias.dtype == APM_F32 ? 4 : 2), a.bias.dtype, 0, there);
-        raw.get(a.bias.dtype, bias);
-    }
+    const Finish finish(a, group, col, there);
 #pragma unroll
     for (int m = 0; m < FM; ++m)
 #pragma unroll
@@ -348,23 +451,205 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
             for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
                 const int row = i * kRowsAtOnce + lane / kPer;
                 const int64_t t = m0 + (wm + m) * kFrag + 16 * h + row;
-                const int n = t < end ? there : 0;
-                char* to = a.y + t * a.y_stride * size;
                 float v[kVec];
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) v[e] = mine[row * kRow + c + e] + bias[e];
-                if (a.accumulate) {
-                    RawAny old;
-                    old.load(to, a.y_type, n > 0 ? col : 0, n);
-                    float f[kVec];
-                    old.get(a.y_type, f);
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e) v[e] += f[e];
-                }
-                if (a.y_type == APM_F32) store8<float>(to, col, n, v);
-                else store8<bf16>(to, col, n, v);
+                for (int e = 0; e < kVec; ++e) v[e] = mine[row * kRow + c + e];
+                finish.row(a, t, t < end ? there : 0, v);
             }
         }
+}
+
+// Few rows: HBM-bound by the weights, and too few tiles for the chip unless they are small.  Each of a workgroup's wavefronts takes every fourth stage of k of the
+// same small tile, by a ring in LDS of its own, so that nobody waits for anybody until the four sums come together at the end.
+template <int FM_, int FN_, int STAGES_>
+struct Few {
+    static constexpr int FM = FM_, FN = FN_, kStages = STAGES_, K = 64, kWaves = 4, kThreads = kWaves * kWave;
+    static constexpr int kM = FM * kFrag, kN = FN * kFrag, kBytesA = kM * K * 2, kBytesB = kN * K * 2, kStage = kBytesA + kBytesB;
+    static constexpr int kA = kBytesA / 1024, kB = kBytesB / 1024;
+};
+typedef Few<1, 1, 4> Strips;
+
+template <class T, bool TRANSPOSED, bool DIRECT>
+__global__ __launch_bounds__(T::kThreads) void apm_product_few_kernel(ProductArgs a) {
+    constexpr int FM = T::FM, FN = T::FN, S = T::kStages, kSteps = T::K / kStep, kRow = T::kN + 4;
+    constexpr int kRing = (DIRECT ? S : 1) * T::kStage, kSums = T::kM * kRow * 4;
+    __shared__ __attribute__((aligned(1024))) char lds_all[T::kWaves * (kRing > kSums ? kRing : kSums)];
+    lds_char* const lds = (lds_char*)lds_all;
+    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    Place place;
+    if (!place.find<T::kM>(a, lane)) return;
+    const int64_t m0 = place.row, end = place.end;
+    const int n0 = place.n_tile * T::kN;
+    const char* const w = a.w + (int64_t)place.group * a.w_group_stride * 2;
+    lds_char* const ring = lds + wave * kRing;
+    const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
+    const int stages = (a.in + T::K - 1) / T::K, mine = (stages - wave + T::kWaves - 1) / T::kWaves;  // the wavefront's: wave, wave + 4, ..
+    constexpr int kVecsK = T::K / kVec, kVecsN = T::kN / kVec;
+
+    uint32_t at_a[T::kA], at_b[T::kB];
+    int vec_a[T::kA], vec_b[T::kB];
+    constexpr int kSets = 2;
+    u32x4 buf_a, buf_b, ra[kSets][T::kA], rb[kSets][T::kB];
+    if constexpr (DIRECT) {
+        const int rows_a = (int)min((int64_t)T::kM, end - m0), rows_b = min(T::kN, a.out - n0);
+        buf_a = buffer_of(a.x + m0 * a.x_stride * 2, (uint32_t)((rows_a - 1) * a.x_stride * 2 + (int64_t)a.in * 2));
+        if constexpr (TRANSPOSED) buf_b = buffer_of(w + (int64_t)n0 * 2, (uint32_t)((a.in - 1) * a.w_stride * 2 + (int64_t)(a.out - n0) * 2));
+        else buf_b = buffer_of(w + (int64_t)n0 * a.w_stride * 2, (uint32_t)((rows_b - 1) * a.w_stride * 2 + (int64_t)a.in * 2));
+#pragma unroll
+        for (int i = 0; i < T::kA; ++i) {
+            const int at = i * kWave + lane, row = at / kVecsK;
+            vec_a[i] = ((at % kVecsK) ^ exchange<T::K>(row)) * kVec;
+            at_a[i] = row < rows_a ? (uint32_t)row * (uint32_t)a.x_stride * 2u + (uint32_t)vec_a[i] * 2u : kNowhere;
+        }
+#pragma unroll
+        for (int i = 0; i < T::kB; ++i) {
+            const int at = i * kWave + lane;
+            if constexpr (TRANSPOSED) {
+                const int row = at / kVecsN, v = at % kVecsN;
+                vec_b[i] = row;
+                at_b[i] = (uint32_t)row * (uint32_t)a.w_stride * 2u + (uint32_t)(((v >> 2) ^ exchange_t<T::kN>(row)) * 4 + (v & 3)) * 16u;
+            } else {
+                const int row = at / kVecsK;
+                vec_b[i] = ((at % kVecsK) ^ exchange<T::K>(row)) * kVec;
+                at_b[i] = row < rows_b ? (uint32_t)row * (uint32_t)a.w_stride * 2u + (uint32_t)vec_b[i] * 2u : kNowhere;
+            }
+        }
+    }
+    auto bring = [&](int i) {  // the wavefront's i-th stage
+        const int k0 = (wave + i * T::kWaves) * T::K;
+        const uint32_t to = ring_at + (uint32_t)(i % S) * T::kStage;
+#pragma unroll
+        for (int u = 0; u < T::kA; ++u) load_to_lds(buf_a, k0 + vec_a[u] < a.in ? at_a[u] + (uint32_t)k0 * 2u : kNowhere, to + u * 1024u);
+#pragma unroll
+        for (int u = 0; u < T::kB; ++u)
+            load_to_lds(buf_b, k0 + vec_b[u] < a.in ? at_b[u] + (uint32_t)k0 * (TRANSPOSED ? (uint32_t)a.w_stride : 1u) * 2u : kNowhere, to + T::kBytesA + u * 1024u);
+    };
+    auto fetch = [&](int j, int set) {
+        const int k0 = (wave + j * T::kWaves) * T::K;
+#pragma unroll
+        for (int i = 0; i < T::kA; ++i) {
+            const int at = i * kWave + lane;
+            ra[set][i] = load_vec(a.x + min(m0 + at / kVecsK, end - 1) * a.x_stride * 2, k0 + at % kVecsK * kVec, a.in);
+        }
+#pragma unroll
+        for (int i = 0; i < T::kB; ++i) {
+            const int at = i * kWave + lane;
+            if constexpr (TRANSPOSED) rb[set][i] = load_vec(w + (int64_t)min(k0 + at / kVecsN, a.in - 1) * a.w_stride * 2, n0 + at % kVecsN * kVec, a.out);
+            else rb[set][i] = load_vec(w + (int64_t)min(n0 + at / kVecsK, a.out - 1) * a.w_stride * 2, k0 + at % kVecsK * kVec, a.in);
+        }
+    };
+    const bool n_ends = TRANSPOSED && n0 + T::kN > a.out;
+    typedef __attribute__((address_space(3))) u32x4* lds_vec;
+    auto put_as = [&](int j, int set, auto ends) {
+        lds_char *const to_a = ring, *const to_b = ring + T::kBytesA;
+        const int k0 = (wave + j * T::kWaves) * T::K;
+#pragma unroll
+        for (int i = 0; i < T::kA; ++i) {
+            const int at = i * kWave + lane;
+            u32x4 v = ra[set][i];
+            if (ends) v = fit(v, k0 + at % kVecsK * kVec, a.in);
+            *(lds_vec)(to_a + lds_at<T::K>(at / kVecsK, at % kVecsK)) = v;
+        }
+#pragma unroll
+        for (int i = 0; i < T::kB; ++i) {
+            const int at = i * kWave + lane;
+            u32x4 v = rb[set][i];
+            if constexpr (TRANSPOSED) {
+                if (ends) v = k0 + at / kVecsN < a.in ? fit(v, n0 + at % kVecsN * kVec, a.out) : u32x4{0u, 0u, 0u, 0u};
+                *(lds_vec)(to_b + lds_at_t<T::kN>(at / kVecsN, at % kVecsN)) = v;
+            } else {
+                if (ends) v = fit(v, k0 + at % kVecsK * kVec, a.in);
+                *(lds_vec)(to_b + lds_at<T::K>(at / kVecsK, at % kVecsK)) = v;
+            }
+        }
+    };
+    auto put = [&](int j, int set) {
+        if (n_ends || (wave + j * T::kWaves) * T::K + T::K > a.in) put_as(j, set, std::true_type());
+        else put_as(j, set, std::false_type());
+    };
+
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+        for (int n = 0; n < FN; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.0f;
+    auto multiply = [&](const lds_char* from) {
+        bf16x8 fa[kSteps][FM], fb[kSteps][FN];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+#pragma unroll
+            for (int m = 0; m < FM; ++m) fa[s][m] = read_fragment<T::K>(from, m, s, lane);
+#pragma unroll
+            for (int n = 0; n < FN; ++n) {
+                if constexpr (TRANSPOSED) fb[s][n] = read_fragment_t<T::kN>(from + T::kBytesA, n, s, lane);
+                else fb[s][n] = read_fragment<T::K>(from + T::kBytesA, n, s, lane);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int m = 0; m < FM; ++m)
+#pragma unroll
+                for (int n = 0; n < FN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s][m], fb[s][n], acc[m][n], 0, 0, 0);
+    };
+    if constexpr (DIRECT) {
+        constexpr int kLoads = T::kA + T::kB;
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+            if (i < mine) bring(i);
+        for (int i = 0; i < mine; ++i) {
+            if (i + S <= mine) wait_loads<(S - 1) * kLoads>();
+            else wait_loads<0>();
+            multiply(ring + i % S * T::kStage);
+            if (i + S < mine) {
+                wait_lds();  // the stage's fragments are read
+                bring(i + S);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kSets; ++i)
+            if (i < mine) fetch(i, i);
+        for (int i = 0; i < mine; i += kSets) {
+#pragma unroll
+            for (int u = 0; u < kSets; ++u) {
+                if (i + u >= mine) break;
+                among_lanes();
+                put(i + u, u);
+                if (i + u + kSets < mine) fetch(i + u + kSets, u);
+                among_lanes();
+                multiply(ring);
+            }
+        }
+    }
+    meet();
+    typedef __attribute__((address_space(3))) float lds_float;
+    lds_float* const sums = (lds_float*)lds;
+    constexpr int kPart = T::kM * kRow;
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+        for (int n = 0; n < FN; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sums[wave * kPart + (m * kFrag + 8 * (r / 4) + 4 * (lane / 32) + r % 4) * kRow + n * kFrag + lane % 32] = acc[m][n][r];
+    __syncthreads();
+    constexpr int kPer = T::kN / kVec, kRowsAtOnce = T::kThreads / kPer;
+    const int c = tid % kPer * kVec, there = max(0, min(kVec, a.out - (n0 + c)));
+    const Finish finish(a, place.group, n0 + c, there);
+#pragma unroll
+    for (int i = 0; i < (T::kM + kRowsAtOnce - 1) / kRowsAtOnce; ++i) {
+        const int row = i * kRowsAtOnce + tid / kPer;
+        if (row >= T::kM || m0 + row >= end) continue;
+        float v[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            const lds_float* p = sums + row * kRow + c + e;
+            v[e] = (p[0] + p[kPart]) + (p[2 * kPart] + p[3 * kPart]);
+        }
+        finish.row(a, m0 + row, there, v);
+    }
 }
 
 int check_product(const apm_grouped_product_desc& p) {
@@ -383,7 +668,7 @@ int check_product(const apm_grouped_product_desc& p) {
     return rc;
 }
 
-enum { kLarge, kSmall, kTiny, kThin };
+enum { kLarge, kSmall, kTiny, kFew, kTiles };
 struct ProductShape {
     int which;
     bool direct;
@@ -396,23 +681,55 @@ template <class T> void shape_as(const apm_grouped_product_desc& p, int which, P
     s->tiles_m = std::min(p.tokens, p.tokens / T::kM + std::min(groups, p.tokens));
     s->tiles_n = div_up(p.out, T::kN);
 }
+// Which tile: estimated in us, from calls that were timed.  A workgroup that has a CU for itself takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for
+// that of each workgroup it has, and `round` more for each.
+struct TileCost {
+    int rows, cols;
+    int per_cu;  // workgroups that start together
+    double start, round, alone[2], busy[2];  // through registers, direct
+};
+constexpr TileCost kCost[kTiles] = {
+    {Large::kM, Large::kN, 1, 8.0, 6.0, {1.9, 1.08}, {2.5, 1.7}},
+    {Small::kM, Small::kN, 2, 4.6, 1.0, {0.95, 0.39}, {0.8, 0.52}},
+    {Tiny::kM, Tiny::kN, 0, 2.6, 0.35, {0.5, 0.19}, {0.33, 0.205}},
+    {Strips::kM, Strips::kN, 0, 2.7, 2.2, {0.31, 0.085}, {0.13, 0.1}},
+};
+constexpr double kCus = 256.0;
+double cost_of(const apm_grouped_product_desc& p, const TileCost& c, bool direct) {
+    // Groups may be empty, but that is not known here: half of the last tile of each is taken for used.
+    const double groups = (double)std::min(std::max<int64_t>(1, p.n_groups), p.tokens), rows = std::max(groups, (double)p.tokens / c.rows + 0.5 * groups);
+    const double load = rows * (double)div_up(p.out, c.cols) / kCus, stages = (double)div_up(p.in, 64);
+    const double rounds = load <= 1.0 ? load : c.per_cu ? std::ceil(load / c.per_cu) * c.per_cu : load;
+    return c.start + std::max(0.0, rounds - 1.0) * c.round + stages * std::max(c.alone[direct], rounds * c.busy[direct] * (load <= 1.0 ? 1.2 : 1.0));
+}
 ProductShape product_shape(const apm_grouped_product_desc& p) {
     ProductShape s{};
-    const int64_t groups = std::max<int64_t>(1, p.n_groups), each = p.tokens / groups;
-    if (each > 128) shape_as<Large>(p, kLarge, &s);
-    else if (each > 64) shape_as<Small>(p, kSmall, &s);
-    else if (each > 32) shape_as<Tiny>(p, kTiny, &s);
-    else shape_as<Thin>(p, kThin, &s);
-    const int64_t reach = (int64_t)1 << 30, w_rows = p.transposed ? p.in + Large::K * Large::kStages : Large::kN;
+    const int64_t reach = (int64_t)1 << 30, w_rows = p.transposed ? p.in + 4 * Large::K : Large::kN;
     s.direct = aligned_to(p.x.data, 16) && aligned_to(p.w.data, 16) && p.x.stride % kVec == 0 && p.w.stride % kVec == 0 && (p.n_groups < 2 || p.w_group_stride % kVec == 0) &&
                p.in % kVec == 0 && (!p.transposed || p.out % kVec == 0) && p.x.stride < reach / Large::kM && p.w.stride < reach / w_rows && p.in < reach / 4 && p.out < reach / 4;
+    int which = 0;
+    for (int i = 1; i < kTiles; ++i)
+        if (cost_of(p, kCost[i], s.direct) < cost_of(p, kCost[which], s.direct)) which = i;
+    //FORCE
+    switch (which) {
+        case kLarge: shape_as<Large>(p, which, &s); break;
+        case kSmall: shape_as<Small>(p, which, &s); break;
+        case kTiny: shape_as<Tiny>(p, which, &s); break;
+        default: shape_as<Strips>(p, which, &s);
+    }
     return s;
 }
 
-template <class T> hipError_t launch_product(const ProductArgs& a, bool transposed, bool direct, unsigned workgroups, hipStream_t s) {
+template <class T, class ANY = T> hipError_t launch_product(const ProductArgs& a, bool transposed, bool direct, unsigned workgroups, hipStream_t s) {
     auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(workgroups), dim3(T::kThreads), 0, s, a); };
-    if (transposed) direct ? start(apm_product_kernel<T, true, true>) : start(apm_product_kernel<T, true, false>);
-    else direct ? start(apm_product_kernel<T, false, true>) : start(apm_product_kernel<T, false, false>);
+    if (transposed) direct ? start(apm_product_kernel<T, true, true>) : start(apm_product_kernel<ANY, true, false>);
+    else direct ? start(apm_product_kernel<T, false, true>) : start(apm_product_kernel<ANY, false, false>);
+    return hipGetLastError();
+}
+template <class T> hipError_t launch_few(const ProductArgs& a, bool transposed, bool direct, unsigned workgroups, hipStream_t s) {
+    auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(workgroups), dim3(T::kThreads), 0, s, a); };
+    if (transposed) direct ? start(apm_product_few_kernel<T, true, true>) : start(apm_product_few_kernel<T, true, false>);
+    else direct ? start(apm_product_few_kernel<T, false, true>) : start(apm_product_few_kernel<T, false, false>);
     return hipGetLastError();
 }
 
@@ -432,10 +749,10 @@ int grouped_product(const apm_grouped_product_desc* pp, void* workspace, size_t 
     if (s.tiles_m > max_workgroups(Large::kThreads) / s.tiles_n) return fail(APM_EINVAL, "y is too large for one product");
     const unsigned n = (unsigned)(s.tiles_m * s.tiles_n);
     const hipStream_t st = (hipStream_t)stream;
-    APM_HIP(s.which == kLarge   ? launch_product<Large>(a, p.transposed, s.direct, n, st)
+    APM_HIP(s.which == kLarge   ? (launch_product<Large, LargeAny>)(a, p.transposed, s.direct, n, st)
             : s.which == kSmall ? launch_product<Small>(a, p.transposed, s.direct, n, st)
-            : s.which == kTiny  ? launch_product<Tiny>(a, p.transposed, s.direct, n, st)
-                                : launch_product<Thin>(a, p.transposed, s.direct, n, st));
+            : s.which == kTiny  ? (launch_product<Tiny, TinyAny>)(a, p.transposed, s.direct, n, st)
+                                : launch_few<Strips>(a, p.transposed, s.direct, n, st));
     return APM_OK;
 }
 
