@@ -700,7 +700,7 @@ double cost_of(const apm_grouped_product_desc& p, const TileCost& c, bool direct
     const double groups = (double)std::min(std::max<int64_t>(1, p.n_groups), p.tokens), rows = std::max(groups, (double)p.tokens / c.rows + 0.5 * groups);
     const double load = rows * (double)div_up(p.out, c.cols) / kCus, stages = (double)div_up(p.in, 64);
     const double rounds = load <= 1.0 ? load : c.per_cu ? std::ceil(load / c.per_cu) * c.per_cu : load;
-    return c.start + std::max(0.0, rounds - 1.0) * c.round + stages * std::max(c.alone[direct], rounds * c.busy[direct] * (load <= 1.0 ? 1.2 : 1.0));
+    return c.start + std::max(0.0, rounds - 1.0) * c.round + stages * std::max(c.alone[direct], rounds * c.busy[direct] * (load <= 1.0 && c.per_cu > 1 ? 1.2 : 1.0));
 }
 ProductShape product_shape(const apm_grouped_product_desc& p) {
     ProductShape s{};
