@@ -1011,15 +1011,19 @@ def apm_lookup_backward(lookup, grads: "apm_lookup_grads", workspace=None, strea
 def make_grouped_product(x, w, y, *, offsets=None, bias=None, transposed=False, accumulate=False) -> apm_grouped_product_desc:
     """w: [out, in] (transposed: [in, out]), or with offsets (int64, groups + 1) [groups, ...]; bias: [out] or [groups, out]."""
     here = _here()
-    (tokens, k), out, groups, at = x.shape, y.shape[1], 0, 0
-    if offsets is not None:
-        groups = offsets.numel() - 1
-        if groups < 1 or w.dim() != 3 or w.shape[0] != groups:
-            raise ValueError(f"offsets of {tuple(offsets.shape)} for weights of {tuple(w.shape)}")
-        at = _whole("offsets", offsets, groups + 1, "torch.int64", here)
+    (tokens, k), out, groups, at, apart = x.shape, y.shape[1], 0, 0, 0
+    rows, cols = (k, out) if transposed else (out, k)
+    if offsets is None:
+        weights = _matrix("w", w, rows, cols, here)
+    else:                                  # as _matrix does, without a tensor for one group
+        groups, stride = offsets.numel() - 1, w.stride()
+        if groups < 1 or w.shape != (groups, rows, cols) or (stride[2] != 1 and cols > 1):
+            raise ValueError(f"offsets of {tuple(offsets.shape)} for weights of {tuple(w.shape)} with strides {stride}, {(groups, rows, cols)} are needed")
+        at, apart = _whole("offsets", offsets, groups + 1, "torch.int64", here), stride[0]
+        weights = _address("w", w, here), stride[1], _dtype(w), 0
     p = apm_grouped_product_desc.from_buffer_copy(_pack_product(
-        tokens, out, k, groups, at, *_matrix("x", x, tokens, k, here), *_matrix("w", w[0] if groups else w, *((k, out) if transposed else (out, k)), here),
-        *_matrix("y", y, tokens, out, here), w.stride(0) if groups else 0, *_vector("bias", bias, max(1, groups) * out, here), int(transposed), int(accumulate)))
+        tokens, out, k, groups, at, *_matrix("x", x, tokens, k, here), *weights, *_matrix("y", y, tokens, out, here), apart,
+        *_vector("bias", bias, max(1, groups) * out, here), int(transposed), int(accumulate)))
     p.tensors, p.device = (x, w, y, offsets, bias), here
     return p
 

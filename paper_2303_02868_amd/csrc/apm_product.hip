@@ -764,3 +764,7 @@ extern "C" size_t apm_grouped_product_workspace_bytes(const apm_grouped_product_
 extern "C" int apm_grouped_product(const apm_grouped_product_desc* p, void* workspace, size_t workspace_bytes, void* stream) {
     return apm::guarded([&]() -> int { return apm::grouped_product(p, workspace, workspace_bytes, stream); });
 }
+
+extern "C" int apm_test_grouped_product_tile(const apm_grouped_product_desc* p) {
+    return !p || apm::check_product(*p) != APM_OK ? 0 : apm::kCost[apm::product_shape(*p).which].rows;
+}
