@@ -339,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void apm_lookup_weights_kernel(WeightGrad
 constexpr int64_t kChunksWanted = 4096;
 int64_t chunk_of(const apm_lookup& l) {
     const int64_t n = l.tokens * l.per_token, slices = div_up(l.cols, kSlice);
-    int64_t chunk = kChunkLeast;
+    int64_t chunk = n <= 2 * kChunkLeast ? 2 * kChunkLeast : kChunkLeast;  // one chunk needs no second kernel
     while (chunk < kChunkMost && div_up(n, chunk) * slices > kChunksWanted) chunk *= 2;
     return chunk;
 }

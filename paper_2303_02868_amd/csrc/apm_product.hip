@@ -56,8 +56,9 @@ struct ProductArgs {
     int32_t y_type, accumulate;
 };
 
-// Rows of K elements in LDS are exchanged in vectors of eight, so that those of eight neighbouring rows that a fragment is read from lie in different banks.
-template <int K> __device__ __forceinline__ int exchange(int row) { return K == 32 ? (row >> 1) & 3 : row & 7; }
+// Rows of K elements in LDS are exchanged in vectors of eight, so that what 16 lanes read together of as many rows lies in all of the 64 banks: those that share banks,
+// every second row (K = 64) or every fourth, take different vectors.
+template <int K> __device__ __forceinline__ int exchange(int row) { return K == 32 ? (row >> 2) & 3 : (row >> 1) & 7; }
 template <int K> __device__ __forceinline__ int lds_at(int row, int vec) { return row * (K * 2) + ((vec ^ exchange<K>(row)) << 4); }
 template <int K> __device__ __forceinline__ bf16x8 read_fragment(const lds_char* tile, int frag, int step, int lane) {
     typedef __attribute__((address_space(3))) const bf16x8* lds_ptr;
@@ -131,7 +132,7 @@ template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinlin
 }
 
 // Which tile a workgroup has.  Workgroups go to the XCDs in turn; each XCD takes a stretch of the order, in which tiles come strip by strip.
-constexpr int kXcds = 8, kStrip = 4;  // tiles of rows that are walked together
+constexpr int kXcds = 8, kStrip = 8;  // tiles of rows that are walked together
 struct Place {
     int64_t row, end;  // the tile's first, and where its group ends
     int group, n_tile;
