@@ -29,6 +29,7 @@ APM_GATE_NONE, APM_GATE_CHANNEL, APM_GATE_TOKEN, APM_GATE_FULL = 0, 1, 2, 3
 APM_JOIN_MAX_COLS = 16384
 APM_I32, APM_I64 = 0, 1
 APM_MAX_POSITIONS = 2147483000
+APM_MAX_GROUPS = 65536
 ALL_STATES = 0b11111
 FP32_STATES = 0b00111
 B16_STATES = 0b11000
@@ -1039,7 +1040,7 @@ def apm_grouped_product(product: apm_grouped_product_desc, workspace=None, strea
 
 
 def make_dropout(x, y, *, p: float, seed: int, layer: int = 0, first_row: int = 0, residual=None, seed_at=None) -> apm_dropout:
-    """seed: 64 bits; seed_at: one int64 or uint64 in device memory that is added to it when the kernel runs."""
+    """seed: modulo 2^64; seed_at: one int64 or uint64 in device memory that is added to it when the kernel runs."""
     here = _here()
     rows, cols = x.shape
     at = 0
@@ -1047,7 +1048,7 @@ def make_dropout(x, y, *, p: float, seed: int, layer: int = 0, first_row: int = 
         if seed_at.numel() != 1 or seed_at.element_size() != 8:
             raise ValueError(f"seed_at: {seed_at.dtype} of {tuple(seed_at.shape)}, one word of 64 bits is needed")
         at = _address("seed_at", seed_at, here)
-    d = apm_dropout.from_buffer_copy(_pack_dropout(rows, cols, p, seed, at, first_row, layer, 0, *_matrix("x", x, rows, cols, here),
+    d = apm_dropout.from_buffer_copy(_pack_dropout(rows, cols, p, seed % (1 << 64), at, first_row, layer, 0, *_matrix("x", x, rows, cols, here),
                                                    *_matrix("residual", residual, rows, cols, here), *_matrix("y", y, rows, cols, here)))
     d.tensors, d.device = (x, residual, y, seed_at), here
     return d

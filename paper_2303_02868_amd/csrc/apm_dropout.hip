@@ -17,7 +17,7 @@ struct DropoutArgs {
     const uint64_t* seed_at;
     uint64_t seed;
     uint64_t first_row;
-    int64_t rows, first_item;
+    int64_t rows, first;  // of all launches; the first one of this
     uint32_t slices;
     int32_t cols;
     uint32_t bound, layer;
@@ -45,11 +45,11 @@ struct Philox {
 template <class X, class Y, bool RESIDUAL>
 __global__ __launch_bounds__(kThreads) void apm_dropout_kernel(DropoutArgs a) {
     const int lane = (int)threadIdx.x % kWave;
-    const int64_t item = a.first_item + (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const int64_t r0 = item / a.slices * kRows;
+    const uint32_t item = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), nth = item / a.slices;
+    const int64_t r0 = a.first + (int64_t)nth * kRows;
     if (r0 >= a.rows) return;
     LaneCols l;
-    l.set((int)(item % a.slices) * kSlice + lane * kVec, a.cols);
+    l.set((int)(item - nth * a.slices) * kSlice + lane * kVec, a.cols);
     Raw<X> x[kRows];
     Raw<Y> residual[kRows];
 #pragma unroll
@@ -90,9 +90,9 @@ int apply(const apm_dropout* dp, void* stream) {
     a.rows = d.rows, a.cols = (int32_t)d.cols, a.slices = (uint32_t)div_up(d.cols, kSlice);
     a.bound = (uint32_t)std::llround(d.p * 65536.0);
     a.scale = a.bound < 65536 ? (float)(65536.0 / (65536.0 - a.bound)) : 0.0f;
-    const int64_t items = div_up(d.rows, kRows) * a.slices, most = max_workgroups(kThreads) * kWaves / 2;
-    for (a.first_item = 0; a.first_item < items; a.first_item += most) {
-        const dim3 grid((unsigned)div_up(std::min(most, items - a.first_item), kWaves)), block(kThreads);
+    const int64_t most = max_workgroups(kThreads) / 2 * kWaves / a.slices * kRows;  // rows of a launch
+    for (a.first = 0; a.first < d.rows; a.first += most) {
+        const dim3 grid((unsigned)div_up(div_up(std::min(most, d.rows - a.first), kRows) * a.slices, kWaves)), block(kThreads);
         const hipStream_t s = (hipStream_t)stream;
         auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
         auto with = [&](auto x, auto y) {

@@ -19,7 +19,7 @@ struct LookupArgs {
     const void* ids;
     apm_matrix table, y;
     apm_vector weights;
-    int64_t tokens, first_item;
+    int64_t tokens, first;  // of all launches; the first one of this
     uint32_t slices, rows;
     int32_t cols, per_token, id_type, accumulate;
     float scale;
@@ -32,11 +32,11 @@ __device__ __forceinline__ float of_lane(float v, int lane) { return __builtin_b
 template <class T, class Y>
 __global__ __launch_bounds__(kThreads) void apm_lookup_kernel(LookupArgs a) {
     const int lane = (int)threadIdx.x % kWave;
-    const int64_t item = a.first_item + (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const int64_t t0 = item / a.slices * kTokens;
+    const uint32_t item = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), nth = item / a.slices;
+    const int64_t t0 = a.first + (int64_t)nth * kTokens;
     if (t0 >= a.tokens) return;
     LaneCols l;
-    l.set((int)(item % a.slices) * kSlice + lane * kVec, a.cols);
+    l.set((int)(item - nth * a.slices) * kSlice + lane * kVec, a.cols);
     float sum[kTokens][kVec] = {};
     for (int j0 = 0; j0 < a.per_token; j0 += kTurn) {
         const int64_t t = t0 + lane / kTurn, j = j0 + lane % kTurn;
@@ -102,9 +102,9 @@ int forward(const apm_lookup* lp, void* stream) {
     a.ids = l.ids.data, a.id_type = l.ids.type, a.table = l.table, a.y = l.y, a.weights = l.weights;
     a.tokens = l.tokens, a.slices = (uint32_t)div_up(l.cols, kSlice), a.cols = (int32_t)l.cols;
     a.rows = (uint32_t)l.rows, a.per_token = (int32_t)l.per_token, a.accumulate = l.accumulate, a.scale = (float)l.scale;
-    const int64_t items = div_up(l.tokens, kTokens) * a.slices, most = max_workgroups(kThreads) * kWaves / 2;
-    for (a.first_item = 0; a.first_item < items; a.first_item += most) {
-        const dim3 grid((unsigned)div_up(std::min(most, items - a.first_item), kWaves)), block(kThreads);
+    const int64_t most = max_workgroups(kThreads) / 2 * kWaves / a.slices * kTokens;  // tokens of a launch
+    for (a.first = 0; a.first < l.tokens; a.first += most) {
+        const dim3 grid((unsigned)div_up(div_up(std::min(most, l.tokens - a.first), kTokens) * a.slices, kWaves)), block(kThreads);
         const hipStream_t s = (hipStream_t)stream;
         auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
         if (l.table.dtype == APM_F32) l.y.dtype == APM_F32 ? start(apm_lookup_kernel<float, float>) : start(apm_lookup_kernel<float, bf16>);
@@ -295,20 +295,19 @@ struct WeightGradArgs {
     const void* ids;
     apm_matrix dy, table;
     apm_vector dweights;
-    int64_t n, first;
-    int32_t per_token, cols, id_type;
-    uint32_t rows;
+    uint32_t n, first, per_token, rows;
+    int32_t cols, id_type;
     float scale;
 };
 template <class D, class T>
 __global__ __launch_bounds__(kThreads) void apm_lookup_weights_kernel(WeightGradArgs a) {
     const int lane = (int)threadIdx.x % kWave;
-    const int64_t p = a.first + (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const uint32_t p = a.first + blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     if (p >= a.n) return;
     const uint32_t row = (uint32_t)__builtin_amdgcn_readfirstlane((int)row_of(a.ids, a.id_type, p, a.rows));
     float sum = 0.0f;
     if (row < a.rows) {
-        const int64_t token = p / a.per_token;
+        const uint32_t token = p / a.per_token;
         constexpr int kSlices = 2;  // under way
         for (int col = 0; col < a.cols; col += kSlices * kSlice) {
             LaneCols l[kSlices];
@@ -398,10 +397,11 @@ int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, 
     if (g.dweights.data && n > 0) {
         WeightGradArgs a{};
         a.ids = l.ids.data, a.id_type = l.ids.type, a.dy = g.dy, a.table = l.table, a.dweights = g.dweights;
-        a.n = n, a.per_token = (int32_t)l.per_token, a.cols = (int32_t)l.cols;
+        a.n = (uint32_t)n, a.per_token = (uint32_t)l.per_token, a.cols = (int32_t)l.cols;
         a.rows = (uint32_t)l.rows, a.scale = (float)l.scale;
-        for (a.first = 0; a.first < n; a.first += most_items) {
-            const dim3 grid((unsigned)div_up(std::min(most_items, n - a.first), kWaves)), block(kThreads);
+        for (int64_t at = 0; at < n; at += most_items) {
+            a.first = (uint32_t)at;
+            const dim3 grid((unsigned)div_up(std::min(most_items, n - at), kWaves)), block(kThreads);
             auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
             const bool wide = l.table.dtype == APM_F32;
             if (g.dy.dtype == APM_F32) wide ? start(apm_lookup_weights_kernel<float, float>) : start(apm_lookup_weights_kernel<float, bf16>);

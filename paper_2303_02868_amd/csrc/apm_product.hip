@@ -86,20 +86,24 @@ __device__ __forceinline__ void group_of(const ProductArgs& a, int g, int64_t* b
     *begin = min(max(a.offsets[g], (int64_t)0), a.tokens);
     *end = min(max(a.offsets[g + 1], *begin), a.tokens);
 }
-// The tiles of rows of 64 groups from g0 on: lane l gets how many there are in front of group g0 + l + 1.
-template <int M> __device__ __forceinline__ uint32_t tiles_up_to(const ProductArgs& a, int g0, int lane) {
+// Tiles of rows of groups g .. g + n - 1, M rows each.
+template <int M> __device__ __forceinline__ uint32_t row_tiles(const ProductArgs& a, int g, int n) {
     uint32_t t = 0;
-    if (g0 + lane < a.groups) {
-        int64_t begin, end;
-        group_of(a, g0 + lane, &begin, &end);
-        t = (uint32_t)((end - begin + M - 1) / M);
-    }
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const uint32_t o = __shfl_up(t, d);
-        if (lane >= d) t += o;
+#pragma unroll 4
+    for (const int end = min(g + n, a.groups); g < end; ++g) {
+        int64_t first, last;
+        group_of(a, g, &first, &last);
+        t += (uint32_t)((last - first + M - 1) / M);
     }
     return t;
+}
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t v, int lane) {  // of the lanes up to this one
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const uint32_t o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
 }
 
 // 16 bytes a lane from memory into LDS, to 16 lane bytes behind `to` (M0); zeros for what lies behind the buffer's end.  In assembly, which does not tell the
@@ -138,11 +142,12 @@ struct Place {
     int group, n_tile;
     // false: there are fewer tiles.  M: rows of a tile.
     template <int M> __device__ __forceinline__ bool find(const ProductArgs& a, int lane) {
-        uint32_t rows = 0;
+        // Each lane counts the tiles of a stretch of groups; then the lanes look through the stretch that has the tile.
+        const int each = (a.groups + kWave - 1) / kWave;
+        uint32_t up = 0, rows = (uint32_t)((a.tokens + M - 1) / M);
         if (a.offsets) {
-            for (int g = 0; g < a.groups; g += kWave) rows += (uint32_t)__builtin_amdgcn_readlane((int)tiles_up_to<M>(a, g, lane), kWave - 1);
-        } else {
-            rows = (uint32_t)((a.tokens + M - 1) / M);
+            up = sum_up_to(row_tiles<M>(a, lane * each, each), lane);
+            rows = (uint32_t)__builtin_amdgcn_readlane((int)up, kWave - 1);
         }
         const uint32_t tiles = rows * (uint32_t)a.tiles_n, nth = blockIdx.x;
         if (nth >= tiles) return false;
@@ -152,17 +157,22 @@ struct Place {
         n_tile = (int)(in_strip / high);
         group = 0;
         if (a.offsets) {
-            uint32_t before = 0;
-            for (int g = 0; g < a.groups; g += kWave) {
-                const uint32_t up = before + tiles_up_to<M>(a, g, lane);
+            auto step = [&](int from, int per) {  // lane l has groups from + l per ..; true: the tile is among them
                 const uint64_t further = __ballot(up > row_tile);
-                if (further) {
-                    const int l = __builtin_ctzll(further);
-                    group = g + l;
-                    row_tile -= l > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)up, l - 1) : before;
-                    break;
+                if (!further) return false;
+                const int l = __builtin_ctzll(further);
+                row_tile -= l > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)up, l - 1) : 0;
+                group = from + l * per;
+                return true;
+            };
+            step(0, each);
+            if (each > 1) {
+                const int from = group, behind = min(from + each, a.groups);
+                for (int g = from; g < behind; g += kWave) {
+                    up = sum_up_to(g + lane < behind ? row_tiles<M>(a, g + lane, 1) : 0, lane);
+                    if (step(g, 1)) break;
+                    row_tile -= (uint32_t)__builtin_amdgcn_readlane((int)up, kWave - 1);
                 }
-                before = (uint32_t)__builtin_amdgcn_readlane((int)up, kWave - 1);
             }
             group = __builtin_amdgcn_readfirstlane(group);
             row_tile = (uint32_t)__builtin_amdgcn_readfirstlane((int)row_tile);
@@ -654,7 +664,7 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_few_kernel(ProductArg
 }
 
 int check_product(const apm_grouped_product_desc& p) {
-    if (p.tokens < 0 || p.tokens > ((int64_t)1 << 40) || p.out < 1 || p.in < 1 || p.out > kMostCols || p.in > kMostCols || p.n_groups < 0 || p.n_groups > APM_MAX_POSITIONS)
+    if (p.tokens < 0 || p.tokens > ((int64_t)1 << 40) || p.out < 1 || p.in < 1 || p.out > kMostCols || p.in > kMostCols || p.n_groups < 0 || p.n_groups > APM_MAX_GROUPS)
         return fail(APM_EINVAL, "bad size: %lld tokens, %lld x %lld, %lld groups", (long long)p.tokens, (long long)p.out, (long long)p.in, (long long)p.n_groups);
     if ((p.n_groups > 0) != (p.offsets != nullptr)) return fail(APM_EINVAL, "offsets and n_groups contradict each other");
     if (!aligned_to(p.offsets, 8)) return fail(APM_EINVAL, "offsets are not aligned to their elements");

@@ -94,7 +94,7 @@ def product(**over):
 
 def test_grouped_product():
     go = lambda room=PTR, size=1 << 40, **o: apm.lib().apm_grouped_product(product(**o), room, size, None)
-    for bad in (dict(tokens=-1), dict(tokens=2 ** 41), dict(out=0), dict(out=2 ** 28 + 1), dict(n_groups=-1), dict(n_groups=2 ** 31), {"in": 0}, {"in": 2 ** 31}):
+    for bad in (dict(tokens=-1), dict(tokens=2 ** 41), dict(out=0), dict(out=2 ** 28 + 1), dict(n_groups=-1), dict(n_groups=apm.APM_MAX_GROUPS + 1), {"in": 0}, {"in": 2 ** 31}):
         refused(go(**bad), apm.APM_EINVAL, "bad size")
         assert apm.apm_grouped_product_workspace_bytes(product(**bad)) == 0
     refused(go(offsets=None), apm.APM_EINVAL, "contradict")
