@@ -4,6 +4,7 @@
 // written once and nothing is added atomically: the sorted positions are cut into chunks of equal size, whatever rows they belong to, a wavefront adds up what it
 // has of each row, and a row that goes beyond a chunk is put together from the chunks' parts, in their order.
 #include <algorithm>
+#include <type_traits>
 
 #include "apm_tok.h"
 
@@ -114,6 +115,51 @@ int forward(const apm_lookup* lp, void* stream) {
     return APM_OK;
 }
 
+// ---- the gradient of the weights ----------------------------------------------------------------
+struct WeightGradArgs {
+    const void* ids;
+    apm_matrix dy, table;
+    apm_vector dweights;
+    uint32_t n, per_token, rows;
+    int32_t cols, id_type;
+    float scale;
+};
+// Of one position, by a wavefront.
+template <class D, class T> __device__ __forceinline__ void weight_grad(const WeightGradArgs& a, uint32_t p, int lane) {
+    const uint32_t row = (uint32_t)__builtin_amdgcn_readfirstlane((int)row_of(a.ids, a.id_type, p, a.rows));
+    float sum = 0.0f;
+    if (row < a.rows) {
+        const uint32_t token = p / a.per_token;
+        constexpr int kSlices = 2;  // under way
+        for (int col = 0; col < a.cols; col += kSlices * kSlice) {
+            LaneCols l[kSlices];
+            Raw<D> d[kSlices];
+            Raw<T> t[kSlices];
+#pragma unroll
+            for (int s = 0; s < kSlices; ++s) {
+                l[s].set(col + s * kSlice + lane * kVec, a.cols);
+                const bool there = col + s * kSlice < a.cols;
+                load_row<0>(d[s], a.dy, token, a.cols, there, l[s]);
+                load_row<0>(t[s], a.table, row, a.cols, there, l[s]);
+            }
+#pragma unroll
+            for (int s = 0; s < kSlices; ++s) {
+                settle(d[s], l[s], a.cols);
+                settle(t[s], l[s], a.cols);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) sum = fmaf(d[s][i], t[s][i], sum);
+            }
+        }
+        sum = wave_sum(sum) * a.scale;
+    }
+    if (lane == 0) store1(a.dweights.data, a.dweights.dtype, p, sum);
+}
+template <class D, class T>
+__global__ __launch_bounds__(kThreads) void apm_lookup_weights_kernel(WeightGradArgs a, uint32_t first) {
+    const uint32_t p = first + blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    if (p < a.n) weight_grad<D, T>(a, p, (int)threadIdx.x % kWave);
+}
+
 // ---- the gradient of the table ------------------------------------------------------------------
 constexpr int kChunkMost = kWave;           // sorted positions of a wavefront, one of each lane to begin with
 constexpr int kChunkLeast = 8;
@@ -153,15 +199,21 @@ __device__ __forceinline__ uint32_t row_at(const TableGradArgs& a, uint32_t i) {
     return p < a.n ? row_of(a.ids, a.id_type, p, a.rows) : a.rows;
 }
 
-template <class D, class T>
-__global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs a) {
+// W: of the table, if the gradient of the weights is made by the same launch; void: it is not.
+template <class D, class T, class W>
+__global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs a, WeightGradArgs of_weights) {
     const int lane = (int)threadIdx.x % kWave;
     const uint32_t item = a.first_item + (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + threadIdx.x / kWave));
     const uint32_t summing = a.chunks * a.slices;
     LaneCols l;
     if (item >= summing) {  // rows without positions
         const uint32_t e = item - summing;
-        if (e >= a.empty) return;
+        if (e >= a.empty) {
+            if constexpr (!std::is_void<W>::value) {
+                if (e - a.empty < of_weights.n) weight_grad<D, W>(of_weights, e - a.empty, lane);
+            }
+            return;
+        }
         const uint32_t first = e * kEmptyRows, r = first + (uint32_t)lane;
         const bool none = lane < kEmptyRows && r < a.rows && a.offsets[r] >= a.offsets[r + 1];
         uint64_t mask = __ballot(none);
@@ -290,55 +342,13 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_join_kernel(TableGrad
     }
 }
 
-// ---- the gradient of the weights ----------------------------------------------------------------
-struct WeightGradArgs {
-    const void* ids;
-    apm_matrix dy, table;
-    apm_vector dweights;
-    uint32_t n, first, per_token, rows;
-    int32_t cols, id_type;
-    float scale;
-};
-template <class D, class T>
-__global__ __launch_bounds__(kThreads) void apm_lookup_weights_kernel(WeightGradArgs a) {
-    const int lane = (int)threadIdx.x % kWave;
-    const uint32_t p = a.first + blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    if (p >= a.n) return;
-    const uint32_t row = (uint32_t)__builtin_amdgcn_readfirstlane((int)row_of(a.ids, a.id_type, p, a.rows));
-    float sum = 0.0f;
-    if (row < a.rows) {
-        const uint32_t token = p / a.per_token;
-        constexpr int kSlices = 2;  // under way
-        for (int col = 0; col < a.cols; col += kSlices * kSlice) {
-            LaneCols l[kSlices];
-            Raw<D> d[kSlices];
-            Raw<T> t[kSlices];
-#pragma unroll
-            for (int s = 0; s < kSlices; ++s) {
-                l[s].set(col + s * kSlice + lane * kVec, a.cols);
-                const bool there = col + s * kSlice < a.cols;
-                load_row<0>(d[s], a.dy, token, a.cols, there, l[s]);
-                load_row<0>(t[s], a.table, row, a.cols, there, l[s]);
-            }
-#pragma unroll
-            for (int s = 0; s < kSlices; ++s) {
-                settle(d[s], l[s], a.cols);
-                settle(t[s], l[s], a.cols);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) sum = fmaf(d[s][i], t[s][i], sum);
-            }
-        }
-        sum = wave_sum(sum) * a.scale;
-    }
-    if (lane == 0) store1(a.dweights.data, a.dweights.dtype, p, sum);
-}
-
 // Positions of a wavefront: few, so that there are wavefronts for the whole chip, but no more of them than that, since rows that go beyond a chunk are
 // written and read once more.
 constexpr int64_t kChunksWanted = 4096;
 int64_t chunk_of(const apm_lookup& l) {
     const int64_t n = l.tokens * l.per_token, slices = div_up(l.cols, kSlice);
-    int64_t chunk = n <= 2 * kChunkLeast ? 2 * kChunkLeast : kChunkLeast;  // one chunk needs no second kernel
+    if (n <= kChunkMost / 2) return kChunkMost / 2;  // one chunk needs no second kernel
+    int64_t chunk = kChunkLeast;
     while (chunk < kChunkMost && div_up(n, chunk) * slices > kChunksWanted) chunk *= 2;
     return chunk;
 }
@@ -366,6 +376,12 @@ int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, 
     if (rc != APM_OK) return rc;
     const hipStream_t s = (hipStream_t)stream;
     const int64_t most_items = max_workgroups(kThreads) * kWaves / 2;
+    const bool wide_dy = n > 0 && g.dy.dtype == APM_F32, wide_dtable = g.dtable.dtype == APM_F32, wide_table = l.table.dtype == APM_F32;
+    WeightGradArgs of_weights{};
+    of_weights.ids = l.ids.data, of_weights.id_type = l.ids.type, of_weights.dy = g.dy, of_weights.table = l.table, of_weights.dweights = g.dweights;
+    of_weights.n = (uint32_t)n, of_weights.per_token = (uint32_t)l.per_token, of_weights.cols = (int32_t)l.cols, of_weights.rows = (uint32_t)l.rows;
+    of_weights.scale = (float)l.scale;
+    bool weights = g.dweights.data && n > 0;
     if (g.dtable.data) {
         TableGradArgs a{};
         a.ids = l.ids.data, a.id_type = l.ids.type, a.dy = g.dy, a.dtable = g.dtable, a.order = g.order, a.offsets = g.offsets;
@@ -373,39 +389,42 @@ int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, 
         a.n = (uint32_t)n, a.rows = (uint32_t)l.rows, a.per_token = (uint32_t)l.per_token, a.cols = (int32_t)l.cols, a.cols_8 = (int32_t)(div_up(l.cols, kVec) * kVec);
         a.chunk = (uint32_t)chunk_of(l), a.chunks = (uint32_t)div_up(n, a.chunk), a.slices = (uint32_t)div_up(l.cols, kSlice), a.empty = g.accumulate ? 0 : (uint32_t)div_up(l.rows, kEmptyRows);
         a.accumulate = g.accumulate, a.scale = (float)l.scale;
-        const int64_t summing = (int64_t)a.chunks * a.slices, items = summing + a.empty;
-        if (items > INT32_MAX) return fail(APM_EINVAL, "too many positions for so many columns");
+        const int64_t summing = (int64_t)a.chunks * a.slices;
+        if (summing + a.empty > INT32_MAX) return fail(APM_EINVAL, "too many positions for so many columns");
+        const bool both = weights && summing + a.empty + n <= most_items;  // by one launch
+        const int64_t items = summing + a.empty + (both ? n : 0);
         for (int64_t at = 0; at < items; at += most_items) {
             a.first_item = (uint32_t)at;
             const dim3 grid((unsigned)div_up(std::min(most_items, items - at), kWaves)), block(kThreads);
-            auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
-            const bool wide = g.dtable.dtype == APM_F32;
-            if (n > 0 && g.dy.dtype == APM_F32) wide ? start(apm_table_grad_kernel<float, float>) : start(apm_table_grad_kernel<float, bf16>);
-            else wide ? start(apm_table_grad_kernel<bf16, float>) : start(apm_table_grad_kernel<bf16, bf16>);
+            auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, of_weights); };
+            auto with = [&](auto d, auto t) {
+                typedef decltype(d) D;
+                typedef decltype(t) T;
+                if (!both) start(apm_table_grad_kernel<D, T, void>);
+                else if (wide_table) start(apm_table_grad_kernel<D, T, float>);
+                else start(apm_table_grad_kernel<D, T, bf16>);
+            };
+            if (wide_dy) wide_dtable ? with(float(), float()) : with(float(), bf16());
+            else wide_dtable ? with(bf16(), float()) : with(bf16(), bf16());
             APM_HIP(hipGetLastError());
         }
+        if (both) weights = false;
         if (a.chunks > 1) {
             for (int64_t at = 0; at < summing; at += most_items) {
                 a.first_item = (uint32_t)at, a.last_item = (uint32_t)std::min(summing, at + most_items);
                 const dim3 grid((unsigned)div_up(a.last_item - at, kWaves)), block(kThreads);
-                if (g.dtable.dtype == APM_F32) hipLaunchKernelGGL(apm_table_grad_join_kernel<float>, grid, block, 0, s, a);
+                if (wide_dtable) hipLaunchKernelGGL(apm_table_grad_join_kernel<float>, grid, block, 0, s, a);
                 else hipLaunchKernelGGL(apm_table_grad_join_kernel<bf16>, grid, block, 0, s, a);
                 APM_HIP(hipGetLastError());
             }
         }
     }
-    if (g.dweights.data && n > 0) {
-        WeightGradArgs a{};
-        a.ids = l.ids.data, a.id_type = l.ids.type, a.dy = g.dy, a.table = l.table, a.dweights = g.dweights;
-        a.n = (uint32_t)n, a.per_token = (uint32_t)l.per_token, a.cols = (int32_t)l.cols;
-        a.rows = (uint32_t)l.rows, a.scale = (float)l.scale;
+    if (weights) {
         for (int64_t at = 0; at < n; at += most_items) {
-            a.first = (uint32_t)at;
             const dim3 grid((unsigned)div_up(std::min(most_items, n - at), kWaves)), block(kThreads);
-            auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
-            const bool wide = l.table.dtype == APM_F32;
-            if (g.dy.dtype == APM_F32) wide ? start(apm_lookup_weights_kernel<float, float>) : start(apm_lookup_weights_kernel<float, bf16>);
-            else wide ? start(apm_lookup_weights_kernel<bf16, float>) : start(apm_lookup_weights_kernel<bf16, bf16>);
+            auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, of_weights, (uint32_t)at); };
+            if (wide_dy) wide_table ? start(apm_lookup_weights_kernel<float, float>) : start(apm_lookup_weights_kernel<float, bf16>);
+            else wide_table ? start(apm_lookup_weights_kernel<bf16, float>) : start(apm_lookup_weights_kernel<bf16, bf16>);
             APM_HIP(hipGetLastError());
         }
     }

@@ -73,7 +73,7 @@ template <class Key> __device__ __forceinline__ uint32_t first_of(const Key* key
 // ---- one workgroup ------------------------------------------------------------------------------
 // Positions lie in LDS in the order of the passes so far, each wavefront takes a stretch of them into registers: counts of each digit in each
 // stretch, what stands before, and back to LDS in the new order.
-constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / kWave, kOneMost = 2;  // positions of a thread
+constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / kWave, kOneMost = 4;  // positions of a thread
 constexpr uint32_t kOnePositions = kOneThreads * kOneMost;
 template <int PER>
 __global__ __launch_bounds__(kOneThreads) void apm_sort_one_kernel(SortArgs a, uint32_t* sorted) {
@@ -148,8 +148,32 @@ __global__ __launch_bounds__(kOneThreads) void apm_sort_one_kernel(SortArgs a, u
         put(a, i, pos[u], key[u]);
         if (!a.alone) sorted[i] = key[u];
     }
-    if (a.offsets && a.alone)
-        for (uint32_t r = (uint32_t)tid; r <= a.rows; r += kOneThreads) a.offsets[r] = first_of(keys, n, r);
+    if (!a.offsets || !a.alone) return;
+    // offsets[r] = i for the rows r behind the key in front of i, up to the key at i; those behind the last key belong to i = n.  A wavefront goes through its
+    // positions' stretches: short ones a lane each, longer ones together.
+    constexpr uint32_t kShort = 4;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const uint32_t i = first + (uint32_t)(u * kWave + lane);
+        uint32_t row = 0, stretch = 0;
+        if (i <= n && i < kMost) {
+            const uint32_t last = i < n ? key[u] : a.rows;
+            row = i > 0 ? keys[i - 1] + 1 : 0;
+            stretch = last + 1 - row;
+        }
+        for (uint32_t k = 0; k < kShort; ++k)
+            if (k < stretch && stretch <= kShort) a.offsets[row + k] = i;
+        uint64_t longer = __ballot(stretch > kShort);
+        while (longer) {
+            const int l = __builtin_ctzll(longer);
+            longer &= longer - 1;
+            const uint32_t from = (uint32_t)__builtin_amdgcn_readlane((int)row, l), count = (uint32_t)__builtin_amdgcn_readlane((int)stretch, l), at = first + (uint32_t)(u * kWave + l);
+            for (uint32_t k = (uint32_t)lane; k < count; k += kWave) a.offsets[from + k] = at;
+        }
+    }
+    if (n == kMost) {
+        for (uint32_t r = keys[n - 1] + 1 + (uint32_t)tid; r <= a.rows; r += kOneThreads) a.offsets[r] = n;
+    }
 }
 
 // ---- many workgroups ----------------------------------------------------------------------------
@@ -357,6 +381,7 @@ int sort_tokens(const apm_token_order* op, void* workspace, size_t workspace_byt
         sorted = (const uint32_t*)workspace, search = !a.alone;
         auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(1), dim3(kOneThreads), 0, st, a, (uint32_t*)workspace); };
         if (a.n <= kOneThreads) start(apm_sort_one_kernel<1>);
+        else if (a.n <= 2 * kOneThreads) start(apm_sort_one_kernel<2>);
         else start(apm_sort_one_kernel<kOneMost>);
         APM_HIP(hipGetLastError());
     } else {
