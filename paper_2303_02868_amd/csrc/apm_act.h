@@ -277,21 +277,21 @@ struct RowAny {
         }
     }
 };
-template <class T> __device__ __forceinline__ void store_row(const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l, const float (&v)[kVec]) {
+template <class T, int CACHE = kNT> __device__ __forceinline__ void store_row(const apm_matrix& m, int64_t row, int64_t cols, bool there, const LaneCols& l, const float (&v)[kVec]) {
     if constexpr (sizeof(T) == sizeof(float)) {
         const Rsrc r = row_buffer(m.data, row * m.stride * 4, there ? (uint32_t)cols * 4u : 0u);
         u32x4 w[2];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) w[i / 4][i % 4] = __builtin_bit_cast(uint32_t, v[i]);
         swap_halves(w[0], w[1]);
-        __builtin_amdgcn_raw_buffer_store_b128(w[0], r, (int)l.at4, 0, kNT);
-        __builtin_amdgcn_raw_buffer_store_b128(w[1], r, (int)(l.at4 + LaneCols::kStep4), 0, kNT);
+        __builtin_amdgcn_raw_buffer_store_b128(w[0], r, (int)l.at4, 0, CACHE);
+        __builtin_amdgcn_raw_buffer_store_b128(w[1], r, (int)(l.at4 + LaneCols::kStep4), 0, CACHE);
     } else {
         const Rsrc r = row_buffer(m.data, row * m.stride * 2, there ? l.whole * 2u : 0u);
         u32x4 w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = to_bf16x2(v[2 * i], v[2 * i + 1]);
-        __builtin_amdgcn_raw_buffer_store_b128(w, r, (int)((uint32_t)l.col * 2u), 0, kNT);
+        __builtin_amdgcn_raw_buffer_store_b128(w, r, (int)((uint32_t)l.col * 2u), 0, CACHE);
         if (l.whole != (uint32_t)cols && there && m.data && l.tail()) store_short((uint16_t*)((char*)m.data + row * m.stride * 2) + l.col, l.n, w);
     }
 }

@@ -189,7 +189,7 @@ template <class T> __device__ __forceinline__ void finish_row(const TableGradArg
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] += old[i];
     }
-    store_row<T>(a.dtable, row, a.cols, true, l, v);
+    store_row<T, 0>(a.dtable, row, a.cols, true, l, v);
 }
 __device__ __forceinline__ float* part_of(const TableGradArgs& a, uint32_t chunk, int which, int col) {
     return a.parts + ((uint64_t)chunk * 2 + (uint32_t)which) * (uint32_t)a.cols_8 + (uint32_t)col;
