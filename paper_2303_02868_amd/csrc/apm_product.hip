@@ -37,8 +37,15 @@ struct Tile {
     }
     static_assert(kA * 1024 * kWaves == kBytesA && kB * 1024 * kWaves == kBytesB, "whole vectors for every lane");
 };
+// 64 of k in a stage are whole cache lines of rows of x and w (16384 x 4096 x 4096 with 32 of k: 478 us, so 447).
+// 256 x 256: the least traffic between L2 and LDS, which bounds the others: loads alone take 341 of its 465 us at 16384 x 4096 x 4096, products and LDS reads alone 387;
+// 1.2 PFLOP/s, at a clock of 1.75 GHz that the matrix cores leave (a library product of that size: 423 to 432 us, w as rows of k 482 to 496, here 452 to 468).  Of the
+// CU's cycles the matrix cores are busy for 58 %, LDS for 28 %.  A half stage more in LDS: input gradients of 8 of 64 groups, 8192 x 1024 x 4096, 114 us without it, so 106.
+// One workgroup a CU that goes on from tile to tile, with the next one's loads under the stores, was no faster (8 groups, 16384 x 8192 x 2048: 575 and 578 us).
 typedef Tile<2, 4, 4, 2, 64, 5> Large;
+// 128 x 128, two of which share a CU: where 256 x 256 would leave CUs without one (2048 x 2048 x 2048: 43 us, so 25).
 typedef Tile<2, 2, 2, 2, 64, 4> Small;
+// 64 x 64: short ones (512 x 768 x 768: 8.9 us by 128 x 128, so 5.1), and groups of few tokens (512 tokens in 64 groups, 4096 x 1024: 107 and 97).
 typedef Tile<2, 2, 1, 1, 64, 6> Tiny;
 // Large where rows go through registers: stages of half the length, so that what is on its way fits beside the sums.
 typedef Tile<2, 4, 4, 2, 32, 4> LargeAny;
@@ -136,7 +143,8 @@ template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinlin
 }
 
 // Which tile a workgroup has.  Workgroups go to the XCDs in turn; each XCD takes a stretch of the order, in which tiles come strip by strip.
-constexpr int kXcds = 8, kStrip = 8;  // tiles of rows that are walked together
+// Eight rows of tiles at a time: most of a group's, whose weights then are met once (8 groups, 16384 x 8192 x 2048: 563 us with strips of four, 549 of eight, 565 of sixteen).
+constexpr int kXcds = 8, kStrip = 8;
 struct Place {
     int64_t row, end;  // the tile's first, and where its group ends
     int group, n_tile;
@@ -226,7 +234,7 @@ __device__ __forceinline__ u32x4 fit(u32x4 v, int64_t col, int width) {
 }
 
 // DIRECT: the tiles go from memory into LDS without passing through registers, which needs whole vectors of sixteen bytes: aligned rows, and widths of a multiple
-// of eight.  The other form takes any.
+// of eight.  The other form takes any (2299 tokens in 8 groups, 1664 x 1911: 54 us, 1664 x 1912: 44).
 template <class T, bool TRANSPOSED, bool DIRECT>
 __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a) {
     constexpr int FM = T::FM, FN = T::FN, S = T::kStages, kSteps = T::K / kStep;
@@ -471,7 +479,8 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
 }
 
 // Few rows: HBM-bound by the weights, and too few tiles for the chip unless they are small.  Each of a workgroup's wavefronts takes every fourth stage of k of the
-// same small tile, by a ring in LDS of its own, so that nobody waits for anybody until the four sums come together at the end.
+// same 32 x 32 tile, by a ring in LDS of its own, so that nobody waits for anybody until the four sums come together at the end.  Two tokens of two of 64 groups,
+// 4096 x 1024: 5.5 us (7.7 by 64 x 64), one token, 768 x 768: 3.7 (4.9), 56 tokens of 8 groups, 1152 x 3776: 11 (18).
 template <int FM_, int FN_, int STAGES_>
 struct Few {
     static constexpr int FM = FM_, FN = FN_, kStages = STAGES_, K = 64, kWaves = 4, kThreads = kWaves * kWave;
@@ -692,7 +701,8 @@ template <class T> void shape_as(const apm_grouped_product_desc& p, int which, P
     s->tiles_m = std::min(p.tokens, p.tokens / T::kM + std::min(groups, p.tokens));
     s->tiles_n = div_up(p.out, T::kN);
 }
-// Which tile: estimated in us, from calls that were timed.  A workgroup that has a CU for itself takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for
+// Which tile: estimated in us, from calls that were timed; over 75 drawn sizes and groups the choice is the fastest of the four or within 14 % of it, but for 8 groups of
+// which few have tokens (1.34 at worst).  A workgroup that has a CU for itself takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for
 // that of each workgroup it has, and `round` more for each.
 struct TileCost {
     int rows, cols;
@@ -700,15 +710,16 @@ struct TileCost {
     double start, round, alone[2], busy[2];  // through registers, direct
 };
 constexpr TileCost kCost[kTiles] = {
-    {Large::kM, Large::kN, 1, 8.0, 6.0, {1.9, 1.08}, {2.5, 1.7}},
-    {Small::kM, Small::kN, 2, 4.6, 1.0, {0.95, 0.39}, {0.8, 0.52}},
-    {Tiny::kM, Tiny::kN, 0, 2.6, 0.35, {0.5, 0.19}, {0.33, 0.205}},
+    {Large::kM, Large::kN, 1, 8.0, 6.0, {1.9, 1.08}, {2.5, 1.63}},
+    {Small::kM, Small::kN, 2, 4.6, 1.0, {0.95, 0.39}, {0.8, 0.49}},
+    {Tiny::kM, Tiny::kN, 0, 2.6, 0.35, {0.5, 0.19}, {0.33, 0.185}},
     {Strips::kM, Strips::kN, 0, 2.7, 2.2, {0.31, 0.085}, {0.13, 0.1}},
 };
 constexpr double kCus = 256.0;
 double cost_of(const apm_grouped_product_desc& p, const TileCost& c, bool direct) {
     // Groups may be empty, but that is not known here: half of the last tile of each is taken for used.
-    const double groups = (double)std::min(std::max<int64_t>(1, p.n_groups), p.tokens), rows = std::max(groups, (double)p.tokens / c.rows + 0.5 * groups);
+    const double groups = (double)std::min(p.n_groups, p.tokens);
+    const double rows = p.n_groups > 1 ? std::max(groups, (double)p.tokens / c.rows + 0.5 * groups) : (double)div_up(p.tokens, c.rows);
     const double load = rows * (double)div_up(p.out, c.cols) / kCus, stages = (double)div_up(p.in, 64);
     const double rounds = load <= 1.0 ? load : c.per_cu ? std::ceil(load / c.per_cu) * c.per_cu : load;
     return c.start + std::max(0.0, rounds - 1.0) * c.round + stages * std::max(c.alone[direct], rounds * c.busy[direct] * (load <= 1.0 && c.per_cu > 1 ? 1.2 : 1.0));

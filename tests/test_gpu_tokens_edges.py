@@ -43,7 +43,7 @@ def tile_of(tokens, out, k, groups, transposed, aligned):
     return apm.lib().apm_test_grouped_product_tile(C.byref(p))
 
 
-TILES = {256: (6100, 2056, 328), 128: (6100, 1032, 264), 64: (1300, 520, 136), 32: (40, 136, 1096)}
+TILES = {256: (6100, 2056, 328), 128: (6850, 1032, 136), 64: (1300, 520, 136), 32: (40, 136, 1096)}
 
 
 @pytest.mark.parametrize("transposed", [False, True])
@@ -64,6 +64,14 @@ def test_products_of_odd_sizes_on_every_tile(rows, transposed):
     tokens, out, k = tokens + 1, out - 3, k + 5
     assert tile_of(tokens, out, k, 0, transposed, False) == rows
     check_product(tokens, out, k, bias=BF16, dtype=F32, transposed=transposed, accumulate=True)
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("rows,sizes", [(256, (5000, 2056, 1096)), (128, (3000, 2048, 1032))])
+def test_products_of_long_sums(rows, sizes, transposed):
+    """More stages than are under way, again and again."""
+    assert tile_of(*sizes, 0, transposed, True) == rows
+    check_product(*sizes, transposed=transposed)
 
 
 class Step:
