@@ -61,6 +61,7 @@ struct ProductArgs {
     int64_t tokens;
     int32_t out, in, groups, tiles_n;
     int32_t y_type, accumulate;
+    int32_t whole_y;  // its rows, of bf16, are stored in whole vectors
 };
 
 // Rows of K elements in LDS are exchanged in vectors of eight, so that what 16 lanes read together of as many rows lies in all of the 64 banks: those that share banks,
@@ -115,8 +116,10 @@ __device__ __forceinline__ uint32_t sum_up_to(uint32_t v, int lane) {  // of the
 
 // 16 bytes a lane from memory into LDS, to 16 lane bytes behind `to` (M0); zeros for what lies behind the buffer's end.  In assembly, which does not tell the
 // compiler that it writes LDS: told so, it waits for these loads in front of transposing reads of other places (16384 x 4096 x 4096: 500 us).  wait_loads and meet wait.
-__device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t at, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(buffer));
+// ONCE: of what no other workgroup reads, which L2 need not keep.
+template <bool ONCE = false> __device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t at, uint32_t to) {
+    if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(at), "s"(buffer) : "m0");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(buffer) : "m0");
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 // The wavefront's accesses to LDS are done, and so are everyone's.
@@ -148,6 +151,7 @@ constexpr int kXcds = 8, kStrip = 8;
 struct Place {
     int64_t row, end;  // the tile's first, and where its group ends
     int group, n_tile;
+    bool once;  // the group has no other rows of tiles
     // false: there are fewer tiles.  M: rows of a tile.
     template <int M> __device__ __forceinline__ bool find(const ProductArgs& a, int lane) {
         // Each lane counts the tiles of a stretch of groups; then the lanes look through the stretch that has the tile.
@@ -188,7 +192,8 @@ struct Place {
         int64_t begin;
         group_of(a, group, &begin, &end);
         row = begin + (int64_t)row_tile * M;
-        return true;
+        once = end - begin <= M;
+        return row < end;  // groups that overlap can have more tiles than 32 bits count
     }
 };
 
@@ -216,6 +221,7 @@ struct Finish {
             for (int e = 0; e < kVec; ++e) v[e] += f[e];
         }
         if (a.y_type == APM_F32) store8<float>(to, col, n, v);
+        else if (a.whole_y) store8<bf16, true>(to, col, n, v);
         else store8<bf16>(to, col, n, v);
     }
 };
@@ -295,14 +301,14 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
             load_to_lds(buf_a, at, to + i * 1024u);
         }
     };
-    auto bring_b = [&](int j, auto whole) {
+    auto bring_b = [&](int j, auto whole, auto once) {
         const uint32_t to = lds_base + (uint32_t)T::place_of(j, true) + (uint32_t)wave * (T::kB * 1024u);
         const int k0 = j * T::K;
 #pragma unroll
         for (int i = 0; i < T::kB; ++i) {
             uint32_t at = at_b[i] + (uint32_t)k0 * (TRANSPOSED ? (uint32_t)a.w_stride : 1u) * 2u;
             if (!whole && k0 + (TRANSPOSED ? vec_b[i] : vec_b[i] * kVec) >= a.in) at = kNowhere;
-            load_to_lds(buf_b, at, to + i * 1024u);
+            load_to_lds<decltype(once)::value>(buf_b, at, to + i * 1024u);
         }
     };
     // Rows behind the group's last and columns behind the matrix's are some other ones: what comes of them is not stored.  Behind the end of k
@@ -378,18 +384,55 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
     };
     constexpr int kReads = FM + (TRANSPOSED ? 2 : 1) * FN, kLoads = T::kA + T::kB;
     constexpr int kExtra = T::kHalf ? T::kA : 0;  // loads of a stage of x that is under way beyond the whole ones
-    auto bring = [&](int j, auto whole_a, auto whole_b) {  // what takes the place of stage j - S: of w stage j, of x that or the next one
+    auto bring = [&](int j, auto whole_a, auto whole_b, auto once) {  // what takes the place of stage j - S: of w stage j, of x that or the next one
         const int ja = T::kHalf ? j + 1 : j;
-        if (whole_b || j < stages) bring_b(j, whole_b);
+        if (whole_b || j < stages) bring_b(j, whole_b, once);
         if (whole_a || ja < stages) bring_a(ja, whole_a);
     };
     auto is_whole = [&](int j) { return (j + 1) * T::K <= a.in; };
-    if constexpr (DIRECT) {
-        if (T::kHalf) bring_a(0, is_whole(0));
+    // Fragments are read a step ahead.  Before a stage's last step everybody has read that stage, whose place is filled anew, and the next stage is there.
+    auto others = [&](int j) {  // all steps of stage j but the last
 #pragma unroll
-        for (int j = 0; j < S; ++j) bring(j, is_whole(T::kHalf ? j + 1 : j), is_whole(j));
-        if (S + (T::kHalf ? 1 : 0) <= stages) wait_loads<(S - 1) * kLoads + kExtra>();
-        else wait_loads<0>();
+        for (int s = 0; s + 1 < kSteps; ++s) {
+            read(j, s + 1);
+            multiply(s);
+            in_turn<FM * FN, kReads, 0>();
+        }
+    };
+    auto turn = [&](int j, auto&& fill) {
+        meet();
+        read(j + 1, 0);
+        fill();
+        multiply(kSteps - 1);
+        in_turn<FM * FN, kReads, DIRECT ? kLoads : 0>();
+        others(j + 1);
+    };
+    if constexpr (DIRECT) {
+        auto all = [&](auto once) {
+            if (T::kHalf) bring_a(0, is_whole(0));
+#pragma unroll
+            for (int j = 0; j < S; ++j) bring(j, is_whole(T::kHalf ? j + 1 : j), is_whole(j), once);
+            if (S + (T::kHalf ? 1 : 0) <= stages) wait_loads<(S - 1) * kLoads + kExtra>();
+            else wait_loads<0>();
+            meet();
+            read(0, 0);
+            others(0);
+            int j = 0;
+            for (const int whole = a.in / T::K - (T::kHalf ? 1 : 0); j + S < whole; ++j) {
+                wait_loads<(S - 2) * kLoads + kExtra>();
+                turn(j, [&] { bring(j + S, std::true_type(), std::true_type(), once); });
+            }
+            for (; j + 1 < stages; ++j) {
+                if (j + S + (T::kHalf ? 1 : 0) <= stages) wait_loads<(S - 2) * kLoads + kExtra>();
+                else wait_loads<0>();
+                turn(j, [&] { bring(j + S, is_whole(T::kHalf ? j + S + 1 : j + S), is_whole(j + S), once); });
+            }
+        };
+        // Weights that one row of tiles reads, non-temporally: 4096 and 512 tokens in 64 groups, 4096 x 1024, 130 and 103 us, 137 and 111 without (weights that come more
+        // often are better kept: 16384 x 4096 x 4096 would take 474 instead of 456).  So is y stored where a
+        // wavefront's instruction fills whole lines (126 and 103, 448; fp32 rows of 4095 by halves of vectors: 183 us, so 163).
+        if (at.once) all(std::true_type());
+        else all(std::false_type());
     } else {
 #pragma unroll
         for (int j = 0; j < kSets; ++j)
@@ -400,41 +443,11 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
 #pragma unroll
         for (int j = kSets; j < 2 * kSets; ++j)
             if (j < stages) fetch(j, j % kSets);
-    }
-    meet();
-    // Fragments are read a step ahead.  Before a stage's last step everybody has read that stage, whose place is filled anew, and the next stage is there.
-    auto others = [&](int j) {  // all steps of stage j but the last
-#pragma unroll
-        for (int s = 0; s + 1 < kSteps; ++s) {
-            read(j, s + 1);
-            multiply(s);
-            in_turn<FM * FN, kReads, 0>();
-        }
-    };
-    read(0, 0);
-    others(0);
-    auto turn = [&](int j, auto&& fill) {
         meet();
-        read(j + 1, 0);
-        fill();
-        multiply(kSteps - 1);
-        in_turn<FM * FN, kReads, DIRECT ? kLoads : 0>();
-        others(j + 1);
-    };
-    int j = 0;
-    if constexpr (DIRECT) {
-        for (const int whole = a.in / T::K - (T::kHalf ? 1 : 0); j + S < whole; ++j) {
-            wait_loads<(S - 2) * kLoads + kExtra>();
-            turn(j, [&] { bring(j + S, std::true_type(), std::true_type()); });
-        }
-        for (; j + 1 < stages; ++j) {
-            if (j + S + (T::kHalf ? 1 : 0) <= stages) wait_loads<(S - 2) * kLoads + kExtra>();
-            else wait_loads<0>();
-            turn(j, [&] { bring(j + S, is_whole(T::kHalf ? j + S + 1 : j + S), is_whole(j + S)); });
-        }
-    } else {
+        read(0, 0);
+        others(0);
         static_assert(S == kSets, "a stage's set of registers goes where the stage two before it was");
-        for (; j + 1 < stages; j += kSets) {
+        for (int j = 0; j + 1 < stages; j += kSets) {
 #pragma unroll
             for (int u = 0; u < kSets; ++u) {
                 if (j + u + 1 >= stages) break;
@@ -732,7 +745,6 @@ ProductShape product_shape(const apm_grouped_product_desc& p) {
     int which = 0;
     for (int i = 1; i < kTiles; ++i)
         if (cost_of(p, kCost[i], s.direct) < cost_of(p, kCost[which], s.direct)) which = i;
-    //FORCE
     switch (which) {
         case kLarge: shape_as<Large>(p, which, &s); break;
         case kSmall: shape_as<Small>(p, which, &s); break;
@@ -766,6 +778,7 @@ int grouped_product(const apm_grouped_product_desc* pp, void* workspace, size_t 
     a.x_stride = p.x.stride, a.w_stride = p.w.stride, a.w_group_stride = p.n_groups > 1 ? p.w_group_stride : 0, a.y_stride = p.y.stride;
     a.tokens = p.tokens, a.out = (int32_t)p.out, a.in = (int32_t)p.in, a.groups = (int32_t)std::max<int64_t>(1, p.n_groups);
     a.y_type = p.y.dtype, a.accumulate = p.accumulate;
+    a.whole_y = p.y.dtype == APM_BF16 && aligned_to(p.y.data, 16) && p.y.stride % kVec == 0;
     const ProductShape s = product_shape(p);
     a.tiles_n = (int32_t)s.tiles_n;
     if (s.tiles_m > max_workgroups(Large::kThreads) / s.tiles_n) return fail(APM_EINVAL, "y is too large for one product");
