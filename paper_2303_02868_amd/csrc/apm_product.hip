@@ -43,6 +43,9 @@ struct Tile {
 // CU's cycles the matrix cores are busy for 58 %, LDS for 28 %.  A half stage more in LDS: input gradients of 8 of 64 groups, 8192 x 1024 x 4096, 114 us without it, so 106.
 // One workgroup a CU that goes on from tile to tile, with the next one's loads under the stores, was no faster (8 groups, 16384 x 8192 x 2048: 575 and 578 us).
 typedef Tile<2, 4, 4, 2, 64, 5> Large;
+// 192 x 256, where 256 x 256 would leave CUs without a tile and this one has one for each at most, as the time is that of a tile then: 6000 x 2048 x 2048
+// 53 us by 256 x 256, so 46; 1500 x 8192 x 2048 52 and 45.  Not through registers.
+typedef Tile<2, 4, 3, 2, 64, 4> Lower;
 // 128 x 128, two of which share a CU: where 256 x 256 would leave CUs without one (2048 x 2048 x 2048: 43 us, so 25).
 typedef Tile<2, 2, 2, 2, 64, 4> Small;
 // 64 x 64: short ones (512 x 768 x 768: 8.9 us by 128 x 128, so 5.1), and groups of few tokens (512 tokens in 64 groups, 4096 x 1024: 107 and 97).
@@ -701,7 +704,7 @@ int check_product(const apm_grouped_product_desc& p) {
     return rc;
 }
 
-enum { kLarge, kSmall, kTiny, kFew, kTiles };
+enum { kLarge, kLower, kSmall, kTiny, kFew, kTiles };
 struct ProductShape {
     int which;
     bool direct;
@@ -714,16 +717,18 @@ template <class T> void shape_as(const apm_grouped_product_desc& p, int which, P
     s->tiles_m = std::min(p.tokens, p.tokens / T::kM + std::min(groups, p.tokens));
     s->tiles_n = div_up(p.out, T::kN);
 }
-// Which tile: estimated in us, from calls that were timed; over 75 drawn sizes and groups the choice is the fastest of the four or within 14 % of it, but for 8 groups of
-// which few have tokens (1.34 at worst).  A workgroup that has a CU for itself takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for
-// that of each workgroup it has, and `round` more for each.
+// Which tile: estimated in us, from calls that were timed; over 100 drawn sizes and groups the choice is the fastest of the five or within 14 % or 1.5 us of it, but for 8
+// groups of which few have tokens (29 and 23 us at worst) and a short k of odd length (9557 tokens, 79 to 4983: 47 and 35).  A workgroup that has a CU for itself
+// takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for that of each workgroup it has, and `round` more for each.
 struct TileCost {
     int rows, cols;
     int per_cu;  // workgroups that start together
     double start, round, alone[2], busy[2];  // through registers, direct
 };
+constexpr double kNever = 1e30;
 constexpr TileCost kCost[kTiles] = {
     {Large::kM, Large::kN, 1, 8.0, 6.0, {1.9, 1.08}, {2.5, 1.63}},
+    {Lower::kM, Lower::kN, 1, 7.0, 0.0, {kNever, 0.85}, {kNever, 1.24}},
     {Small::kM, Small::kN, 2, 4.6, 1.0, {0.95, 0.39}, {0.8, 0.49}},
     {Tiny::kM, Tiny::kN, 0, 2.6, 0.35, {0.5, 0.19}, {0.33, 0.185}},
     {Strips::kM, Strips::kN, 0, 2.7, 2.2, {0.31, 0.085}, {0.13, 0.1}},
@@ -734,8 +739,12 @@ double cost_of(const apm_grouped_product_desc& p, const TileCost& c, bool direct
     const double groups = (double)std::min(p.n_groups, p.tokens);
     const double rows = p.n_groups > 1 ? std::max(groups, (double)p.tokens / c.rows + 0.5 * groups) : (double)div_up(p.tokens, c.rows);
     const double load = rows * (double)div_up(p.out, c.cols) / kCus, stages = (double)div_up(p.in, 64);
-    const double rounds = load <= 1.0 ? load : c.per_cu ? std::ceil(load / c.per_cu) * c.per_cu : load;
-    return c.start + std::max(0.0, rounds - 1.0) * c.round + stages * std::max(c.alone[direct], rounds * c.busy[direct] * (load <= 1.0 && c.per_cu > 1 ? 1.2 : 1.0));
+    if (c.rows == Lower::kM && load > 1.0) return kNever;
+    // Workgroups of a CU that is not full get in each other's way less than in proportion.
+    const bool part = load <= std::max(1, c.per_cu);
+    const double rounds = part || !c.per_cu ? load : std::ceil(load / c.per_cu) * c.per_cu;
+    const double crowd = part && c.per_cu > 1 ? 1.2 - 0.25 * std::max(0.0, load - 1.0) : 1.0;
+    return c.start + std::max(0.0, rounds - 1.0) * c.round + stages * std::max(c.alone[direct], rounds * c.busy[direct] * crowd);
 }
 ProductShape product_shape(const apm_grouped_product_desc& p) {
     ProductShape s{};
@@ -747,6 +756,7 @@ ProductShape product_shape(const apm_grouped_product_desc& p) {
         if (cost_of(p, kCost[i], s.direct) < cost_of(p, kCost[which], s.direct)) which = i;
     switch (which) {
         case kLarge: shape_as<Large>(p, which, &s); break;
+        case kLower: shape_as<Lower>(p, which, &s); break;
         case kSmall: shape_as<Small>(p, which, &s); break;
         case kTiny: shape_as<Tiny>(p, which, &s); break;
         default: shape_as<Strips>(p, which, &s);
@@ -785,6 +795,7 @@ int grouped_product(const apm_grouped_product_desc* pp, void* workspace, size_t 
     const unsigned n = (unsigned)(s.tiles_m * s.tiles_n);
     const hipStream_t st = (hipStream_t)stream;
     APM_HIP(s.which == kLarge   ? (launch_product<Large, LargeAny>)(a, p.transposed, s.direct, n, st)
+            : s.which == kLower ? (launch_product<Lower, LargeAny>)(a, p.transposed, s.direct, n, st)
             : s.which == kSmall ? launch_product<Small>(a, p.transposed, s.direct, n, st)
             : s.which == kTiny  ? (launch_product<Tiny, TinyAny>)(a, p.transposed, s.direct, n, st)
                                 : launch_few<Strips>(a, p.transposed, s.direct, n, st));

@@ -58,6 +58,17 @@ def test_products_on_every_tile(rows, aligned, transposed):
 
 
 @pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("k", [328, 448])
+def test_products_on_the_tile_of_192_rows(k, transposed):
+    tokens, out = 5100, 2056
+    for groups in (0, 3):
+        assert tile_of(tokens, out, k, groups, transposed, True) == 192
+        offsets = [0, tokens // 5, tokens // 5 + 1, tokens - 7] if groups else None
+        check_product(tokens, out, k, offsets, bias=F32, transposed=transposed, accumulate=bool(groups), seed=k)
+    assert tile_of(tokens, out, k, 0, transposed, False) != 192
+
+
+@pytest.mark.parametrize("transposed", [False, True])
 @pytest.mark.parametrize("rows", sorted(TILES))
 def test_products_of_odd_sizes_on_every_tile(rows, transposed):
     tokens, out, k = TILES[rows]
@@ -67,7 +78,7 @@ def test_products_of_odd_sizes_on_every_tile(rows, transposed):
 
 
 @pytest.mark.parametrize("transposed", [False, True])
-@pytest.mark.parametrize("rows,sizes", [(256, (5000, 2056, 1096)), (128, (3000, 2048, 1032))])
+@pytest.mark.parametrize("rows,sizes", [(256, (6100, 2056, 1096)), (192, (5000, 2056, 1096)), (128, (3000, 2048, 1032))])
 def test_products_of_long_sums(rows, sizes, transposed):
     """More stages than are under way, again and again."""
     assert tile_of(*sizes, 0, transposed, True) == rows
