@@ -3,7 +3,7 @@
 //
 // All latency: 16384 positions are 0.7 MB.  Few positions (up to kOnePositions) are sorted by one workgroup in LDS, where a pass costs four barriers and no launch
 // (16 positions 3.0 us, 4000 words 12.7).  More of them: each pass counts the digits of each tile of positions, and then each tile adds up what stands before it and puts its
-// positions where they belong (16384 words: 2 x (2.6 + 6.1) us and 4.7 for the offsets; by one workgroup 35, by tiles that count everything for themselves 2 x 9.5).
+// positions where they belong (16384 words 19.8 us; by one workgroup 35, by tiles that count everything for themselves 24.7).
 #include <algorithm>
 
 #include "apm_tok.h"
@@ -185,8 +185,9 @@ struct PassArgs {
     const int32_t* at;
     uint32_t* keys_out;    // nullptr: not needed any more
     int32_t* at_out;       // nullptr: the last pass
-    uint32_t* counts;      // [tiles][digits]
+    uint32_t* counts;      // [tiles][digits], and of the passes behind this one behind it
     uint32_t shift, tile, tiles;
+    uint32_t behind;       // passes whose counts are the placing kernel's
 };
 __device__ __forceinline__ uint32_t key_of(const SortArgs& a, const PassArgs& s, uint32_t i) {
     return s.keys ? s.keys[i] : row_of(a.ids, a.id_type, i, a.rows);
@@ -214,12 +215,17 @@ __global__ __launch_bounds__(kManyThreads) void apm_sort_count_kernel(SortArgs a
         if (base + kManyThreads < end) key = key_of(a, s, min(base + kManyThreads + threadIdx.x, end - 1));
     }
     __syncthreads();
-    if (threadIdx.x < kDigits) s.counts[(uint64_t)blockIdx.x * kDigits + threadIdx.x] = counts[threadIdx.x];
+    if (threadIdx.x >= kDigits) return;
+    for (uint32_t pass = 0; pass <= s.behind; ++pass) s.counts[((uint64_t)pass * s.tiles + blockIdx.x) * kDigits + threadIdx.x] = pass == 0 ? counts[threadIdx.x] : 0;
 }
 
-// ONCE: a tile is a position for each thread.  Otherwise each wavefront goes through its stretch twice, to count it and to put it in place.
-template <bool ONCE>
+// ONCE: a tile is a position for each thread.  TALLY: of few tiles, and where a position goes is counted for the next pass, too, in LDS and then in memory, by additions of
+// whole numbers, whose order does not matter (a kernel less; 16384 words 22.0 us, so 19.8, 5000 19.9 and 17).  Otherwise each wavefront goes through its stretch twice, to count it and to put it in place.
+constexpr uint32_t kTallied = 32;  // tiles
+template <bool ONCE, bool TALLY>
 __global__ __launch_bounds__(kManyThreads) void apm_sort_place_kernel(SortArgs a, PassArgs s) {
+    static_assert(ONCE || !TALLY, "a position for each thread");
+    __shared__ uint32_t tally[TALLY ? kTallied * kDigits : 1];
     __shared__ uint32_t next[kManyWaves][kDigits];
     __shared__ uint32_t seen[2][kDigits];  // positions with a digit: of the tiles before this one, of the others
     __shared__ uint32_t of_waves[kDigits / kWave];
@@ -239,6 +245,8 @@ __global__ __launch_bounds__(kManyThreads) void apm_sort_place_kernel(SortArgs a
     }
     for (int i = tid; i < kManyWaves * kDigits; i += kManyThreads) (&next[0][0])[i] = 0;
     if (tid < 2 * kDigits) (&seen[0][0])[tid] = 0;
+    if constexpr (TALLY)
+        for (uint32_t i = (uint32_t)tid; i < s.tiles * kDigits; i += kManyThreads) tally[i] = 0;
     __syncthreads();
     uint64_t same = 0;
     uint32_t below = 0;
@@ -273,7 +281,17 @@ __global__ __launch_bounds__(kManyThreads) void apm_sort_place_kernel(SortArgs a
         else put(a, at, p, key);
     };
     if constexpr (ONCE) {
-        if (from + (uint32_t)lane < to) place(next[wave][(key0 >> s.shift) & (kDigits - 1)] + below, key0, p0);
+        if (from + (uint32_t)lane < to) {
+            const uint32_t at = next[wave][(key0 >> s.shift) & (kDigits - 1)] + below;
+            if constexpr (TALLY) atomicAdd(&tally[at / kManyThreads * kDigits + ((key0 >> (s.shift + kDigitBits)) & (kDigits - 1))], 1u);
+            place(at, key0, p0);
+        }
+        if constexpr (TALLY) {
+            __syncthreads();
+            uint32_t* counts = s.counts + (uint64_t)s.tiles * kDigits;
+            for (uint32_t i = (uint32_t)tid; i < s.tiles * kDigits; i += kManyThreads)
+                if (tally[i]) atomicAdd(&counts[i], tally[i]);
+        }
         return;
     }
     for (uint32_t base = from; base < to; base += kWave) {
@@ -329,7 +347,7 @@ constexpr int64_t kTilesMost = 512, kTileLeast = kManyThreads;
 constexpr uint32_t kOneRows = 4096;        // offsets of so many rows are written by the one workgroup
 
 struct SortShape {
-    bool one;
+    bool one, tallied;
     uint32_t passes, tile, tiles;
 };
 SortShape sort_shape(int64_t n, int64_t rows) {
@@ -340,14 +358,16 @@ SortShape sort_shape(int64_t n, int64_t rows) {
     s.one = n <= kOnePositions;
     const int64_t tile = std::max(kTileLeast, div_up(div_up(n, kTilesMost), kTileLeast) * kTileLeast);
     s.tile = (uint32_t)tile, s.tiles = (uint32_t)div_up(n, tile);
+    s.tallied = s.tile == kManyThreads && s.tiles <= kTallied;
     return s;
 }
+size_t counts_of(const SortShape& s) { return (size_t)(s.tallied ? s.passes : 1) * s.tiles * kDigits; }
 size_t to_16(size_t bytes) { return (bytes + 15) / 16 * 16; }
 size_t room_of(int64_t n, int64_t rows) {
     const SortShape s = sort_shape(n, rows);
     const size_t words = to_16((size_t)n * 4);
     if (s.one) return words;
-    return (size_t)s.tiles * kDigits * 4 + 4 * words;  // keys and positions, of two passes
+    return counts_of(s) * 4 + 4 * words;  // keys and positions, of two passes
 }
 
 int check_order(const apm_token_order& o) {
@@ -389,7 +409,7 @@ int sort_tokens(const apm_token_order* op, void* workspace, size_t workspace_byt
         char* room = (char*)workspace;
         const size_t words = to_16((size_t)o.n * 4);
         uint32_t* counts = (uint32_t*)room;
-        room += (size_t)shape.tiles * kDigits * 4;
+        room += counts_of(shape) * 4;
         uint32_t* keys[2] = {(uint32_t*)room, (uint32_t*)(room + words)};
         int32_t* at[2] = {(int32_t*)(room + 2 * words), (int32_t*)(room + 3 * words)};
         for (uint32_t pass = 0; pass < shape.passes; ++pass) {
@@ -398,9 +418,11 @@ int sort_tokens(const apm_token_order* op, void* workspace, size_t workspace_byt
             s.keys = pass > 0 ? keys[(pass - 1) % 2] : nullptr, s.at = pass > 0 ? at[(pass - 1) % 2] : nullptr;
             s.keys_out = !last || (o.offsets && pass > 0) ? keys[pass % 2] : nullptr, s.at_out = last ? nullptr : at[pass % 2];
             s.counts = counts, s.shift = pass * kDigitBits, s.tile = shape.tile, s.tiles = shape.tiles;
-            hipLaunchKernelGGL(apm_sort_count_kernel, dim3(shape.tiles), dim3(kManyThreads), 0, st, a, s);
+            if (shape.tallied) s.counts += (size_t)pass * shape.tiles * kDigits, s.behind = shape.passes - 1;
+            if (pass == 0 || !shape.tallied) hipLaunchKernelGGL(apm_sort_count_kernel, dim3(shape.tiles), dim3(kManyThreads), 0, st, a, s);
             auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(shape.tiles), dim3(kManyThreads), 0, st, a, s); };
-            shape.tile == kManyThreads ? start(apm_sort_place_kernel<true>) : start(apm_sort_place_kernel<false>);
+            if (shape.tile > kManyThreads) start(apm_sort_place_kernel<false, false>);
+            else shape.tallied && !last ? start(apm_sort_place_kernel<true, true>) : start(apm_sort_place_kernel<true, false>);
             APM_HIP(hipGetLastError());
             if (last) sorted = s.keys_out, search = o.offsets && pass > 0;
         }
