@@ -46,6 +46,9 @@ typedef Tile<2, 4, 4, 2, 64, 5> Large;
 // 192 x 256, where 256 x 256 would leave CUs without a tile and this one has one for each at most, as the time is that of a tile then: 6000 x 2048 x 2048
 // 53 us by 256 x 256, so 46; 1500 x 8192 x 2048 52 and 45.  Not through registers.
 typedef Tile<2, 4, 3, 2, 64, 4> Lower;
+// 128 x 256, where more tiles than CUs or groups of few tokens leave 256 rows half empty: 4096 tokens of 64 experts, 1024 to 4096, 112 us (120 by 128 x 128, 155 by 256 x 256),
+// 4096 tokens in 8 groups, 4096 to 1024, 61 (71, 102).
+typedef Tile<2, 4, 2, 2, 64, 6> Low;
 // 128 x 128, two of which share a CU: where 256 x 256 would leave CUs without one (2048 x 2048 x 2048: 43 us, so 25).
 typedef Tile<2, 2, 2, 2, 64, 4> Small;
 // 64 x 64: short ones (512 x 768 x 768: 8.9 us by 128 x 128, so 5.1), and groups of few tokens (512 tokens in 64 groups, 4096 x 1024: 107 and 97).
@@ -708,7 +711,7 @@ int check_product(const apm_grouped_product_desc& p) {
     return rc;
 }
 
-enum { kLarge, kLower, kSmall, kTiny, kFew, kTiles };
+enum { kLarge, kLower, kLow, kSmall, kTiny, kFew, kTiles };
 struct ProductShape {
     int which;
     bool direct;
@@ -721,9 +724,9 @@ template <class T> void shape_as(const apm_grouped_product_desc& p, int which, P
     s->tiles_m = std::min(p.tokens, p.tokens / T::kM + std::min(groups, p.tokens));
     s->tiles_n = div_up(p.out, T::kN);
 }
-// Which tile: estimated in us, from calls that were timed; over 100 drawn sizes and groups the choice is the fastest of the five or within 14 % or 1.5 us of it, but for 8
-// groups of which few have tokens (29 and 23 us at worst) and a short k of odd length (9557 tokens, 79 to 4983: 47 and 35).  A workgroup that has a CU for itself
-// takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for that of each workgroup it has, and `round` more for each.
+// Which tile: estimated in us, from calls that were timed; over 110 drawn sizes and groups the choice is the fastest of the six or within 15 % or 1.5 us of it, but for 8
+// groups of which few have tokens or which share few tokens (29 and 23, 32 and 22 us at worst) and a short k of odd length (9557 tokens, 79 to 4983: 47 and 35). A
+// workgroup that has a CU for itself takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for that of each workgroup it has, and `round` more for each.
 struct TileCost {
     int rows, cols;
     int per_cu;  // workgroups that start together
@@ -733,6 +736,7 @@ constexpr double kNever = 1e30;
 constexpr TileCost kCost[kTiles] = {
     {Large::kM, Large::kN, 1, 8.0, 6.0, {1.9, 1.08}, {2.5, 1.63}},
     {Lower::kM, Lower::kN, 1, 7.0, 0.0, {kNever, 0.85}, {kNever, 1.24}},
+    {Low::kM, Low::kN, 1, 7.0, 3.0, {kNever, 0.6}, {kNever, 0.88}},
     {Small::kM, Small::kN, 2, 4.6, 1.0, {0.95, 0.39}, {0.8, 0.49}},
     {Tiny::kM, Tiny::kN, 0, 2.6, 0.35, {0.5, 0.19}, {0.33, 0.185}},
     {Strips::kM, Strips::kN, 0, 2.7, 2.2, {0.31, 0.085}, {0.13, 0.1}},
@@ -761,6 +765,7 @@ ProductShape product_shape(const apm_grouped_product_desc& p) {
     switch (which) {
         case kLarge: shape_as<Large>(p, which, &s); break;
         case kLower: shape_as<Lower>(p, which, &s); break;
+        case kLow: shape_as<Low>(p, which, &s); break;
         case kSmall: shape_as<Small>(p, which, &s); break;
         case kTiny: shape_as<Tiny>(p, which, &s); break;
         default: shape_as<Strips>(p, which, &s);
@@ -800,6 +805,7 @@ int grouped_product(const apm_grouped_product_desc* pp, void* workspace, size_t 
     const hipStream_t st = (hipStream_t)stream;
     APM_HIP(s.which == kLarge   ? (launch_product<Large, LargeAny>)(a, p.transposed, s.direct, n, st)
             : s.which == kLower ? (launch_product<Lower, LargeAny>)(a, p.transposed, s.direct, n, st)
+            : s.which == kLow   ? (launch_product<Low, LargeAny>)(a, p.transposed, s.direct, n, st)
             : s.which == kSmall ? launch_product<Small>(a, p.transposed, s.direct, n, st)
             : s.which == kTiny  ? (launch_product<Tiny, TinyAny>)(a, p.transposed, s.direct, n, st)
                                 : launch_few<Strips>(a, p.transposed, s.direct, n, st));
@@ -816,5 +822,7 @@ extern "C" int apm_grouped_product(const apm_grouped_product_desc* p, void* work
 }
 
 extern "C" int apm_test_grouped_product_tile(const apm_grouped_product_desc* p) {
-    return !p || apm::check_product(*p) != APM_OK ? 0 : apm::kCost[apm::product_shape(*p).which].rows;
+    if (!p || apm::check_product(*p) != APM_OK) return 0;
+    const apm::TileCost& c = apm::kCost[apm::product_shape(*p).which];
+    return c.rows == apm::Low::kM && c.cols == apm::Low::kN ? -c.rows : c.rows;
 }

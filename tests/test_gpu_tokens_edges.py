@@ -58,14 +58,24 @@ def test_products_on_every_tile(rows, aligned, transposed):
 
 
 @pytest.mark.parametrize("transposed", [False, True])
-@pytest.mark.parametrize("k", [328, 448])
-def test_products_on_the_tile_of_192_rows(k, transposed):
-    tokens, out = 5100, 2056
+@pytest.mark.parametrize("rows,tokens,k", [(192, 5100, 328), (192, 5100, 448), (-128, 7900, 1096)])
+def test_products_on_tiles_for_whole_vectors(rows, tokens, k, transposed):
+    out = 2056
     for groups in (0, 3):
-        assert tile_of(tokens, out, k, groups, transposed, True) == 192
+        assert tile_of(tokens, out, k, groups, transposed, True) == rows
         offsets = [0, tokens // 5, tokens // 5 + 1, tokens - 7] if groups else None
         check_product(tokens, out, k, offsets, bias=F32, transposed=transposed, accumulate=bool(groups), seed=k)
-    assert tile_of(tokens, out, k, 0, transposed, False) != 192
+    assert tile_of(tokens, out, k, 0, transposed, False) != rows
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("out,k", [(1024, 1024), (1032, 1088), (520, 1100)])
+def test_products_of_groups_that_begin_at_different_k(out, k, transposed):
+    """Groups of one row of tiles each, more of them than stages; whole and not."""
+    sizes = [(37 * g) % 97 for g in range(40)]
+    ends = [0]
+    for s in sizes: ends.append(ends[-1] + s)
+    check_product(ends[-1] + 3, out, k, ends, bias=F32, transposed=transposed, accumulate=True, seed=k)
 
 
 @pytest.mark.parametrize("transposed", [False, True])
@@ -78,7 +88,7 @@ def test_products_of_odd_sizes_on_every_tile(rows, transposed):
 
 
 @pytest.mark.parametrize("transposed", [False, True])
-@pytest.mark.parametrize("rows,sizes", [(256, (6100, 2056, 1096)), (192, (5000, 2056, 1096)), (128, (3000, 2048, 1032))])
+@pytest.mark.parametrize("rows,sizes", [(256, (6100, 2056, 1096)), (192, (5000, 2056, 1096)), (128, (2048, 2048, 1032)), (-128, (3000, 2048, 1032))])
 def test_products_of_long_sums(rows, sizes, transposed):
     """More stages than are under way, again and again."""
     assert tile_of(*sizes, 0, transposed, True) == rows
