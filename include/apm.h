@@ -936,7 +936,7 @@ int apm_grouped_product(const apm_grouped_product_desc* p, void* workspace, size
  * The mask depends on these alone: the gradient (x: dy, y: dx, no residual) and a recomputed forward pass are the same call, a batch may
  * be cut into calls with first_row.  seed_at: a device word that is read when the kernel runs, so that replays of a graph differ; NULL: 0.
  * x: bf16 or fp32; residual (optional) and y: bf16 or fp32, the same.  Arithmetic is fp32, rounded once.  What is dropped is not read as a number:
- * an infinity or a NaN there leaves no trace.  y may be x itself or residual itself (same address, stride and type).  cols: at most 2^28.
+ * an infinity or a NaN there leaves no trace.  y may be x itself or residual itself (same address, stride and type; another form at that address is refused).  cols: at most 2^28.
  */
 typedef struct {
     int64_t rows, cols;

@@ -86,6 +86,8 @@ int apply(const apm_dropout* dp, void* stream) {
     if (rc == APM_OK && d.residual.data) rc = check_matrix("residual", d.residual, d.rows, d.cols, false);
     if (rc != APM_OK || d.rows == 0) return rc;
     if (d.residual.data && d.residual.dtype != d.y.dtype) return fail(APM_EINVAL, "residual and y have different types");
+    for (const apm_matrix& m : {d.x, d.residual})
+        if (m.data == d.y.data && (m.dtype != d.y.dtype || (m.stride != d.y.stride && d.rows > 1))) return fail(APM_EINVAL, "y is where x or the residual is, in another form");
     DropoutArgs a{};
     a.x = d.x, a.residual = d.residual, a.y = d.y;
     a.seed_at = d.seed_at, a.seed = d.seed, a.layer = d.layer, a.first_row = (uint64_t)d.first_row;

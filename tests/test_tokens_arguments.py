@@ -129,6 +129,9 @@ def test_dropout():
     refused(go(y=matrix(stride=32)), apm.APM_EINVAL, "y: a row stride")
     refused(go(residual=matrix(dtype=apm.APM_F32)), apm.APM_EINVAL, "different types")
     refused(go(residual=matrix(PTR + 1)), apm.APM_EINVAL, "residual is not aligned")
+    refused(go(x=matrix(dtype=apm.APM_F32)), apm.APM_EINVAL, "in another form")
+    refused(go(x=matrix(stride=128), rows=2), apm.APM_EINVAL, "in another form")
+    refused(go(x=matrix(PTR + 16), residual=matrix(stride=128), rows=2), apm.APM_EINVAL, "in another form")
     refused(apm.lib().apm_dropout_apply(None, None), apm.APM_EINVAL, "missing")
     assert go(rows=0) == apm.APM_OK
 
