@@ -111,13 +111,19 @@ template <int M> __device__ __forceinline__ uint32_t row_tiles(const ProductArgs
     }
     return t;
 }
-__device__ __forceinline__ uint32_t sum_up_to(uint32_t v, int lane) {  // of the lanes up to this one
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const uint32_t o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
-    return v;
+template <int DPP, int ROWS> __device__ __forceinline__ uint32_t add_from(uint32_t v) {
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, DPP, ROWS, 0xf, false);
+}
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t v) {  // of the lanes up to this one
+    v = add_from<0x111, 0xf>(v);  // from 1, 2, 4 and 8 lanes below in a row of 16
+    v = add_from<0x112, 0xf>(v);
+    v = add_from<0x114, 0xf>(v);
+    v = add_from<0x118, 0xf>(v);
+    v = add_from<0x142, 0xa>(v);  // a row's last lane to the second and fourth row
+    return add_from<0x143, 0xc>(v);  // lane 31 to the upper half
+}
+__device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane));
 }
 
 // 16 bytes a lane from memory into LDS, to 16 lane bytes behind `to` (M0); zeros for what lies behind the buffer's end.  In assembly, which does not tell the
@@ -163,8 +169,15 @@ struct Place {
         // Each lane counts the tiles of a stretch of groups; then the lanes look through the stretch that has the tile.
         const int each = (a.groups + kWave - 1) / kWave;
         uint32_t up = 0, rows = (uint32_t)((a.tokens + M - 1) / M);
+        int64_t begin = 0;
+        end = a.tokens;
+        auto count = [&](int g) {  // of one group, or none, which the lane then has in begin and end
+            begin = end = 0;
+            if (g < a.groups) group_of(a, g, &begin, &end);
+            return sum_up_to((uint32_t)((end - begin + M - 1) / M));
+        };
         if (a.offsets) {
-            up = sum_up_to(row_tiles<M>(a, lane * each, each), lane);
+            up = each == 1 ? count(lane) : sum_up_to(row_tiles<M>(a, lane * each, each));
             rows = (uint32_t)__builtin_amdgcn_readlane((int)up, kWave - 1);
         }
         const uint32_t tiles = rows * (uint32_t)a.tiles_n, nth = blockIdx.x;
@@ -175,10 +188,11 @@ struct Place {
         n_tile = (int)(in_strip / high);
         group = 0;
         if (a.offsets) {
+            int l = 0;
             auto step = [&](int from, int per) {  // lane l has groups from + l per ..; true: the tile is among them
                 const uint64_t further = __ballot(up > row_tile);
                 if (!further) return false;
-                const int l = __builtin_ctzll(further);
+                l = __builtin_ctzll(further);
                 row_tile -= l > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)up, l - 1) : 0;
                 group = from + l * per;
                 return true;
@@ -187,16 +201,16 @@ struct Place {
             if (each > 1) {
                 const int from = group, behind = min(from + each, a.groups);
                 for (int g = from; g < behind; g += kWave) {
-                    up = sum_up_to(g + lane < behind ? row_tiles<M>(a, g + lane, 1) : 0, lane);
+                    up = count(g + lane < behind ? g + lane : a.groups);
                     if (step(g, 1)) break;
                     row_tile -= (uint32_t)__builtin_amdgcn_readlane((int)up, kWave - 1);
                 }
             }
             group = __builtin_amdgcn_readfirstlane(group);
             row_tile = (uint32_t)__builtin_amdgcn_readfirstlane((int)row_tile);
+            l = __builtin_amdgcn_readfirstlane(l);
+            begin = of_lane(begin, l), end = of_lane(end, l);
         }
-        int64_t begin;
-        group_of(a, group, &begin, &end);
         row = begin + (int64_t)row_tile * M;
         once = end - begin <= M;
         return row < end;  // groups that overlap can have more tiles than 32 bits count
