@@ -173,6 +173,7 @@ struct TableGradArgs {
     const int32_t* order;
     const int64_t* offsets;
     float* parts;  // [chunks][2][cols_8]: of the row that began before the chunk, and of the row that goes on behind it
+    u32x2* on;     // [chunks]: the row that begins in the chunk and goes on behind it, and how many chunks have parts of it; 0 of no row
     apm_matrix dy, dtable;
     apm_vector weights;
     uint32_t n, rows, per_token, chunk, chunks, slices, empty;  // empty: wavefronts that write zeros
@@ -246,10 +247,15 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs 
             if (my_row < a.rows) my_weight = weight_of(a.weights, p);
         }
     }
+    const bool notes = item == chunk * a.slices && lane == 0;
     uint32_t row = of_lane(my_row, 0);
-    if (row >= a.rows) return;  // so are all behind it
+    if (row >= a.rows) {  // so are all behind it
+        if (notes) a.on[chunk] = u32x2{0u, 0u};
+        return;
+    }
     bool before = start > 0 && row_at(a, start - 1) == row;  // the row began in an earlier chunk
-    const uint32_t after = start + a.chunk < a.n ? row_at(a, start + a.chunk) : a.rows;
+    const uint32_t next = start + a.chunk, after = next < a.n ? row_at(a, next) : a.rows;
+    const int64_t end = min(max(a.offsets[min(after, a.rows - 1) + 1], (int64_t)next + 1), (int64_t)a.n);  // of `after`, if it is a row
     float sum[kVec] = {};
     auto flush = [&](bool goes_on) {
         if (!before && !goes_on) return finish_row<T>(a, row, l, sum);
@@ -275,7 +281,10 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs 
             const uint32_t r = of_lane(my_row, i);
             if (r != row) {
                 flush(false);
-                if (r >= a.rows) return;
+                if (r >= a.rows) {
+                    if (notes) a.on[chunk] = u32x2{0u, 0u};
+                    return;
+                }
                 row = r, before = false;
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) sum[e] = 0.0f;
@@ -287,11 +296,12 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_kernel(TableGradArgs 
         }
     }
     flush(after == row);
+    if (notes) a.on[chunk] = u32x2{row, after == row && !before ? (uint32_t)(end - 1) / a.chunk - chunk + 1 : 0u};
 }
 
-// A row that goes beyond the chunk in which it begins: that chunk's part and those of the chunks behind it.  Each wavefront looks at a chunk; what there is
-// to do, which is little, the workgroup does together, a stretch of the parts for each wavefront.  7.6 us for the embedding above: launch, a look at the order
-// (three dependent loads) and the longest row's 72 parts.
+// A row that goes beyond the chunk in which it begins: that chunk's part and those of the chunks behind it.  Each wavefront looks at what a chunk noted; what there is
+// to do, which is little, the workgroup does together, a stretch of the parts for each wavefront.  6.4 us for the embedding above: launch, the note, and the longest
+// row's 72 parts (7.9 where the order was looked at anew, three loads one after the other).
 constexpr int kPartsAhead = 8;
 template <class T>
 __global__ __launch_bounds__(kThreads) void apm_table_grad_join_kernel(TableGradArgs a) {
@@ -301,16 +311,9 @@ __global__ __launch_bounds__(kThreads) void apm_table_grad_join_kernel(TableGrad
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     auto item_of = [&](uint32_t w) { return a.first_item + blockIdx.x + w * gridDim.x; };  // neighbours, which may have the same row's slices, are for different workgroups
     {
-        const uint32_t item = item_of(wave), chunk = item / a.slices, start = chunk * a.chunk, next = start + a.chunk;
-        uint32_t row = 0, parts = 0;
-        if (item < a.last_item && next < a.n) {
-            row = row_at(a, next - 1);
-            const uint32_t behind = row_at(a, next), ahead = start > 0 ? row_at(a, start - 1) : a.rows;
-            if (row < a.rows && behind == row && ahead != row) {  // neither ends here nor began earlier still
-                const int64_t end = min(max(a.offsets[row + 1], (int64_t)next + 1), (int64_t)a.n);
-                parts = (uint32_t)(end - 1) / a.chunk - chunk + 1;
-            }
-        }
+        const uint32_t item = item_of(wave);
+        const u32x2 on = item < a.last_item ? a.on[item / a.slices] : u32x2{0u, 0u};
+        const uint32_t row = on.x, parts = on.y;
         if (lane == 0) rows[wave] = row, parts_of[wave] = parts;
     }
     __syncthreads();
@@ -357,9 +360,8 @@ int64_t chunk_of(const apm_lookup& l) {
     while (chunk < kChunkMost && div_up(n, chunk) * slices > kChunksWanted) chunk *= 2;
     return chunk;
 }
-size_t room_of(const apm_lookup& l) {
-    return (size_t)div_up(l.tokens * l.per_token, chunk_of(l)) * 2 * (size_t)div_up(l.cols, kVec) * kVec * sizeof(float);
-}
+size_t parts_of(const apm_lookup& l) { return (size_t)div_up(l.tokens * l.per_token, chunk_of(l)) * 2 * (size_t)div_up(l.cols, kVec) * kVec; }
+size_t room_of(const apm_lookup& l) { return parts_of(l) * sizeof(float) + (size_t)div_up(l.tokens * l.per_token, chunk_of(l)) * sizeof(u32x2); }
 
 int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, size_t workspace_bytes, void* stream) {
     if (!lp || !gp) return fail(APM_EINVAL, "missing argument");
@@ -390,7 +392,7 @@ int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, 
     if (g.dtable.data) {
         TableGradArgs a{};
         a.ids = l.ids.data, a.id_type = l.ids.type, a.dy = g.dy, a.dtable = g.dtable, a.order = g.order, a.offsets = g.offsets;
-        a.parts = (float*)workspace, a.weights = l.weights;
+        a.parts = (float*)workspace, a.on = (u32x2*)(a.parts + parts_of(l)), a.weights = l.weights;
         a.n = (uint32_t)n, a.rows = (uint32_t)l.rows, a.per_token = (uint32_t)l.per_token, a.cols = (int32_t)l.cols, a.cols_8 = (int32_t)(div_up(l.cols, kVec) * kVec);
         a.chunk = (uint32_t)chunk_of(l), a.chunks = (uint32_t)div_up(n, a.chunk), a.slices = (uint32_t)div_up(l.cols, kSlice), a.empty = g.accumulate ? 0 : (uint32_t)div_up(l.rows, kEmptyRows);
         a.accumulate = g.accumulate, a.scale = (float)l.scale;
