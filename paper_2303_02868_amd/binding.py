@@ -910,25 +910,30 @@ def _address(name, t, here) -> int:
     return t.data_ptr() if (t.is_cuda if here is None else t.get_device() == here) else _elsewhere(name, t, here)
 
 
-def _indices(name, t, here):
-    """Words of an apm_indices, of any shape."""
+def _index_type(t):
+    """An apm_index_type, or -1."""
     code = _INDEX_TYPES.get(t.dtype)
     if code is None:
-        code = {"torch.int32": APM_I32, "torch.int64": APM_I64}.get(str(t.dtype))
-        if code is None:
-            raise ValueError(f"{name}: a tensor of {t.dtype}, int32 or int64 is needed")
-        _INDEX_TYPES[t.dtype] = code
+        code = _INDEX_TYPES[t.dtype] = {"torch.int32": APM_I32, "torch.int64": APM_I64}.get(str(t.dtype), -1)
+    return code
+
+
+def _indices(name, t, here):
+    """Words of an apm_indices, of any shape."""
+    code = _index_type(t)
+    if code < 0:
+        raise ValueError(f"{name}: a tensor of {t.dtype}, int32 or int64 is needed")
     if not t.is_contiguous():
         raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()}, contiguous elements are needed")
     return _address(name, t, here), code, 0
 
 
-def _whole(name, t, n, dtype, here) -> int:
+def _whole(name, t, n, code, here) -> int:
     """Address of n whole numbers of one type (None: not given)."""
     if t is None:
         return 0
-    if t.numel() != n or not t.is_contiguous() or str(t.dtype) != dtype:
-        raise ValueError(f"{name}: {t.dtype} of {tuple(t.shape)} with strides {t.stride()}, {n} contiguous elements of {dtype} are needed")
+    if t.numel() != n or not t.is_contiguous() or _index_type(t) != code:
+        raise ValueError(f"{name}: {t.dtype} of {tuple(t.shape)} with strides {t.stride()}, {n} contiguous elements of torch.int{64 if code == APM_I64 else 32} are needed")
     return _address(name, t, here)
 
 
@@ -946,9 +951,9 @@ def make_token_order(ids, rows: int, order, *, offsets=None, place=None, token=N
     here = _here()
     tokens, per = _per_token("ids", ids)
     n = tokens * per
-    o = apm_token_order.from_buffer_copy(_pack_order(n, per, rows, *_indices("ids", ids, here), _whole("order", order, n, "torch.int32", here),
-                                                     _whole("offsets", offsets, rows + 1, "torch.int64", here), _whole("place", place, n, "torch.int32", here),
-                                                     _whole("token", token, n, "torch.int32", here)))
+    o = apm_token_order.from_buffer_copy(_pack_order(n, per, rows, *_indices("ids", ids, here), _whole("order", order, n, APM_I32, here),
+                                                     _whole("offsets", offsets, rows + 1, APM_I64, here), _whole("place", place, n, APM_I32, here),
+                                                     _whole("token", token, n, APM_I32, here)))
     o.tensors, o.device = (ids, order, offsets, place, token), here
     return o
 
@@ -1020,7 +1025,7 @@ def make_grouped_product(x, w, y, *, offsets=None, bias=None, transposed=False, 
         groups, stride = offsets.numel() - 1, w.stride()
         if groups < 1 or w.shape != (groups, rows, cols) or (stride[2] != 1 and cols > 1):
             raise ValueError(f"offsets of {tuple(offsets.shape)} for weights of {tuple(w.shape)} with strides {stride}, {(groups, rows, cols)} are needed")
-        at, apart = _whole("offsets", offsets, groups + 1, "torch.int64", here), stride[0]
+        at, apart = _whole("offsets", offsets, groups + 1, APM_I64, here), stride[0]
         weights = _address("w", w, here), stride[1], _dtype(w), 0
     p = apm_grouped_product_desc.from_buffer_copy(_pack_product(
         tokens, out, k, groups, at, *_matrix("x", x, tokens, k, here), *weights, *_matrix("y", y, tokens, out, here), apart,
