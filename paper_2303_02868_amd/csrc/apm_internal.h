@@ -661,5 +661,5 @@ extern "C" int apm_test_set_wait_limit(apm_pool* pool, int32_t wait_limit);
 extern "C" int apm_test_set_call_number(apm_pool* pool, uint32_t number);
 // The side of the tiles that apm_ckpt_weight_grad takes for a call (0: it would refuse it), so that tests know which kernel they run.
 extern "C" int apm_test_weight_grad_tile(const apm_weight_grad* w);
-// Rows of the tile of y that a product per group takes (-128: of 128 x 256; 0: it would be refused), for the tests that go through all of them.
+// Rows of the tile of y that a product per group takes (-128: of 128 x 256, -64: with the sum split over the wavefronts; 0: it would be refused), for the tests that go through all of them.
 extern "C" int apm_test_grouped_product_tile(const apm_grouped_product_desc* p);

@@ -525,6 +525,9 @@ struct Few {
     static constexpr int kA = kBytesA / 1024, kB = kBytesB / 1024;
 };
 typedef Few<1, 1, 4> Strips;
+// 64 x 64, for few tiles and long sums: 64 tokens, 2048 to 8192: 10.5 us (15.7 by four wavefronts that share the stages, 11.7 by 32 x 32), 512 tokens, 4096 to 1024: 16.0 (18.7, 16.3).
+// Not through registers.
+typedef Few<2, 2, 2> Squares;
 
 template <class T, bool TRANSPOSED, bool DIRECT>
 __global__ __launch_bounds__(T::kThreads) void apm_product_few_kernel(ProductArgs a) {
@@ -725,7 +728,7 @@ int check_product(const apm_grouped_product_desc& p) {
     return rc;
 }
 
-enum { kLarge, kLower, kLow, kSmall, kTiny, kFew, kTiles };
+enum { kLarge, kLower, kLow, kSmall, kTiny, kSquares, kFew, kTiles };
 struct ProductShape {
     int which;
     bool direct;
@@ -738,7 +741,7 @@ template <class T> void shape_as(const apm_grouped_product_desc& p, int which, P
     s->tiles_m = std::min(p.tokens, p.tokens / T::kM + std::min(groups, p.tokens));
     s->tiles_n = div_up(p.out, T::kN);
 }
-// Which tile: estimated in us, from calls that were timed; over 110 drawn sizes and groups the choice is the fastest of the six or within 15 % or 1.5 us of it, but for 8
+// Which tile: estimated in us, from calls that were timed; over 110 drawn sizes and groups the choice is the fastest of the seven or within 15 % or 1.5 us of it, but for 8
 // groups of which few have tokens or which share few tokens (29 and 23, 32 and 22 us at worst) and a short k of odd length (9557 tokens, 79 to 4983: 47 and 35). A
 // workgroup that has a CU for itself takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for that of each workgroup it has, and `round` more for each.
 struct TileCost {
@@ -752,7 +755,8 @@ constexpr TileCost kCost[kTiles] = {
     {Lower::kM, Lower::kN, 1, 7.0, 0.0, {kNever, 0.85}, {kNever, 1.24}},
     {Low::kM, Low::kN, 1, 7.0, 3.0, {kNever, 0.6}, {kNever, 0.88}},
     {Small::kM, Small::kN, 2, 4.6, 1.0, {0.95, 0.39}, {0.8, 0.49}},
-    {Tiny::kM, Tiny::kN, 0, 2.6, 0.35, {0.5, 0.19}, {0.33, 0.185}},
+    {Tiny::kM, Tiny::kN, 0, 2.6, 0.35, {0.5, 0.25}, {0.33, 0.185}},
+    {Squares::kM, Squares::kN, 1, 5.2, 3.0, {kNever, 0.165}, {kNever, 0.2}},
     {Strips::kM, Strips::kN, 0, 2.7, 2.2, {0.31, 0.085}, {0.13, 0.1}},
 };
 constexpr double kCus = 256.0;
@@ -782,6 +786,7 @@ ProductShape product_shape(const apm_grouped_product_desc& p) {
         case kLow: shape_as<Low>(p, which, &s); break;
         case kSmall: shape_as<Small>(p, which, &s); break;
         case kTiny: shape_as<Tiny>(p, which, &s); break;
+        case kSquares: shape_as<Squares>(p, which, &s); break;
         default: shape_as<Strips>(p, which, &s);
     }
     return s;
@@ -793,10 +798,10 @@ template <class T, class ANY = T> hipError_t launch_product(const ProductArgs& a
     else direct ? start(apm_product_kernel<T, false, true>) : start(apm_product_kernel<ANY, false, false>);
     return hipGetLastError();
 }
-template <class T> hipError_t launch_few(const ProductArgs& a, bool transposed, bool direct, unsigned workgroups, hipStream_t s) {
+template <class T, class ANY = T> hipError_t launch_few(const ProductArgs& a, bool transposed, bool direct, unsigned workgroups, hipStream_t s) {
     auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(workgroups), dim3(T::kThreads), 0, s, a); };
-    if (transposed) direct ? start(apm_product_few_kernel<T, true, true>) : start(apm_product_few_kernel<T, true, false>);
-    else direct ? start(apm_product_few_kernel<T, false, true>) : start(apm_product_few_kernel<T, false, false>);
+    if (transposed) direct ? start(apm_product_few_kernel<T, true, true>) : start(apm_product_few_kernel<ANY, true, false>);
+    else direct ? start(apm_product_few_kernel<T, false, true>) : start(apm_product_few_kernel<ANY, false, false>);
     return hipGetLastError();
 }
 
@@ -822,7 +827,8 @@ int grouped_product(const apm_grouped_product_desc* pp, void* workspace, size_t 
             : s.which == kLow   ? (launch_product<Low, LargeAny>)(a, p.transposed, s.direct, n, st)
             : s.which == kSmall ? launch_product<Small>(a, p.transposed, s.direct, n, st)
             : s.which == kTiny  ? (launch_product<Tiny, TinyAny>)(a, p.transposed, s.direct, n, st)
-                                : launch_few<Strips>(a, p.transposed, s.direct, n, st));
+            : s.which == kSquares ? (launch_few<Squares, Strips>)(a, p.transposed, s.direct, n, st)
+                                  : launch_few<Strips>(a, p.transposed, s.direct, n, st));
     return APM_OK;
 }
 
@@ -837,6 +843,6 @@ extern "C" int apm_grouped_product(const apm_grouped_product_desc* p, void* work
 
 extern "C" int apm_test_grouped_product_tile(const apm_grouped_product_desc* p) {
     if (!p || apm::check_product(*p) != APM_OK) return 0;
-    const apm::TileCost& c = apm::kCost[apm::product_shape(*p).which];
-    return c.rows == apm::Low::kM && c.cols == apm::Low::kN ? -c.rows : c.rows;
+    const int which = apm::product_shape(*p).which, rows = apm::kCost[which].rows;
+    return which == apm::kLow || which == apm::kSquares ? -rows : rows;
 }

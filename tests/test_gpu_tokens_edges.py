@@ -58,7 +58,7 @@ def test_products_on_every_tile(rows, aligned, transposed):
 
 
 @pytest.mark.parametrize("transposed", [False, True])
-@pytest.mark.parametrize("rows,tokens,k", [(192, 5100, 328), (192, 5100, 448), (-128, 7900, 1096)])
+@pytest.mark.parametrize("rows,tokens,k", [(192, 5100, 328), (192, 5100, 448), (-128, 7900, 1096), (-64, 255, 4168)])
 def test_products_on_tiles_for_whole_vectors(rows, tokens, k, transposed):
     out = 2056
     for groups in (0, 3):
