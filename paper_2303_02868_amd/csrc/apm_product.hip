@@ -741,8 +741,8 @@ template <class T> void shape_as(const apm_grouped_product_desc& p, int which, P
     s->tiles_m = std::min(p.tokens, p.tokens / T::kM + std::min(groups, p.tokens));
     s->tiles_n = div_up(p.out, T::kN);
 }
-// Which tile: estimated in us, from calls that were timed; over 110 drawn sizes and groups the choice is the fastest of the seven or within 15 % or 1.5 us of it, but for 8
-// groups of which few have tokens or which share few tokens (29 and 23, 32 and 22 us at worst) and a short k of odd length (9557 tokens, 79 to 4983: 47 and 35). A
+// Which tile: estimated in us, from calls that were timed; over 150 drawn sizes and groups the choice is the fastest of the seven or within 15 % or 1.5 us of it, but for
+// groups of which few have tokens (137 tokens in 30 of 64, 6144 to 261: 40 and 21 us at worst) and a short k of odd length (9557 tokens, 79 to 4983: 47 and 35). A
 // workgroup that has a CU for itself takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for that of each workgroup it has, and `round` more for each.
 struct TileCost {
     int rows, cols;
