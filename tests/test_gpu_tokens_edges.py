@@ -7,7 +7,7 @@ import torch
 
 import oracle.tokens as T
 import paper_2303_02868_amd as apm
-from test_gpu_tokens import BF16, DEV, F32, I32, I64, Lookup, check_product, check_sort, rng, room, sort
+from test_gpu_tokens import BF16, DEV, F32, I32, I64, Lookup, check_product, check_sort, rng, room, sort, untouched, view
 
 pytestmark = pytest.mark.gpu
 
@@ -66,6 +66,15 @@ def test_products_on_tiles_for_whole_vectors(rows, tokens, k, transposed):
         offsets = [0, tokens // 5, tokens // 5 + 1, tokens - 7] if groups else None
         check_product(tokens, out, k, offsets, bias=F32, transposed=transposed, accumulate=bool(groups), seed=k)
     assert tile_of(tokens, out, k, 0, transposed, False) != rows
+
+
+@pytest.mark.parametrize("tokens,out,k", [(6100, 2056, 328), (5100, 2056, 328), (7900, 2056, 1096), (6850, 1032, 136), (1300, 520, 136), (255, 2056, 4168), (40, 136, 1096)])
+def test_groups_that_overlap_write_inside_of_y(tokens, out, k):
+    x, w = torch.randn(tokens, k, device=DEV, generator=rng(0)).to(BF16), torch.randn(3, out, k, device=DEV, generator=rng(1)).to(BF16)
+    flat, y = view(tokens, out, F32, 4, 4)
+    offsets = torch.tensor([0, tokens, tokens // 3, tokens + 9], device=DEV)
+    apm.apm_grouped_product(apm.make_grouped_product(x, w, y, offsets=offsets))
+    assert untouched(flat, y, 7.0)
 
 
 @pytest.mark.parametrize("transposed", [False, True])
