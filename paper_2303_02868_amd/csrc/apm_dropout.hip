@@ -19,7 +19,7 @@ struct DropoutArgs {
     const uint64_t* seed_at;
     uint64_t seed;
     uint64_t first_row;
-    int64_t rows, first;  // of all launches; the first one of this
+    int64_t first, end;  // rows of this launch
     uint32_t slices;
     int32_t cols;
     uint32_t bound, layer;
@@ -49,15 +49,15 @@ __global__ __launch_bounds__(kThreads) void apm_dropout_kernel(DropoutArgs a) {
     const int lane = (int)threadIdx.x % kWave;
     const uint32_t item = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), nth = item / a.slices;
     const int64_t r0 = a.first + (int64_t)nth * kRows;
-    if (r0 >= a.rows) return;
+    if (r0 >= a.end) return;
     LaneCols l;
     l.set((int)(item - nth * a.slices) * kSlice + lane * kVec, a.cols);
     Raw<X> x[kRows];
     Raw<Y> residual[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
-        load_row(x[u], a.x, r0 + u, a.cols, r0 + u < a.rows, l);
-        if constexpr (RESIDUAL) load_row(residual[u], a.residual, r0 + u, a.cols, r0 + u < a.rows, l);
+        load_row(x[u], a.x, r0 + u, a.cols, r0 + u < a.end, l);
+        if constexpr (RESIDUAL) load_row(residual[u], a.residual, r0 + u, a.cols, r0 + u < a.end, l);
     }
     const uint64_t seed = a.seed + (a.seed_at ? *a.seed_at : 0);
 #pragma unroll
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kThreads) void apm_dropout_kernel(DropoutArgs a) {
             v[i] = random[i] < a.bound ? 0.0f : x[u][i] * a.scale;
             if constexpr (RESIDUAL) v[i] += residual[u][i];
         }
-        store_row<Y>(a.y, r0 + u, a.cols, r0 + u < a.rows, l, v);
+        store_row<Y>(a.y, r0 + u, a.cols, r0 + u < a.end, l, v);
     }
 }
 
@@ -91,12 +91,13 @@ int apply(const apm_dropout* dp, void* stream) {
     DropoutArgs a{};
     a.x = d.x, a.residual = d.residual, a.y = d.y;
     a.seed_at = d.seed_at, a.seed = d.seed, a.layer = d.layer, a.first_row = (uint64_t)d.first_row;
-    a.rows = d.rows, a.cols = (int32_t)d.cols, a.slices = (uint32_t)div_up(d.cols, kSlice);
+    a.cols = (int32_t)d.cols, a.slices = (uint32_t)div_up(d.cols, kSlice);
     a.bound = (uint32_t)std::llround(d.p * 65536.0);
     a.scale = a.bound < 65536 ? (float)(65536.0 / (65536.0 - a.bound)) : 0.0f;
-    const int64_t most = max_workgroups(kThreads) / 2 * kWaves / a.slices * kRows;  // rows of a launch
-    for (a.first = 0; a.first < d.rows; a.first += most) {
-        const dim3 grid((unsigned)div_up(div_up(std::min(most, d.rows - a.first), kRows) * a.slices, kWaves)), block(kThreads);
+    const int64_t most = std::max<int64_t>(1, workgroups_of_launch(kThreads) * kWaves / a.slices) * kRows;  // rows of a launch
+    for (a.first = 0; a.first < d.rows; a.first = a.end) {
+        a.end = std::min(d.rows, a.first + most);  // the last workgroup can have wavefronts to spare, whose rows are the next launch's: in place they would be dropped out twice
+        const dim3 grid((unsigned)div_up(div_up(a.end - a.first, kRows) * a.slices, kWaves)), block(kThreads);
         const hipStream_t s = (hipStream_t)stream;
         auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
         auto with = [&](auto x, auto y) {

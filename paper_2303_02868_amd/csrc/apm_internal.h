@@ -659,6 +659,8 @@ extern "C" int apm_test_set_max_workgroups(apm_pool* pool, int64_t max_workgroup
 extern "C" int apm_test_set_wait_limit(apm_pool* pool, int32_t wait_limit);
 // The number of the pool's last call that handed results on under one (0: the next one clears them).
 extern "C" int apm_test_set_call_number(apm_pool* pool, uint32_t number);
+// Workgroups of a launch of the lookups, their gradients and dropout, for calls of this thread (0: what a grid holds), so that small ones take several launches.
+extern "C" int apm_test_set_launch_workgroups(int64_t workgroups);
 // The side of the tiles that apm_ckpt_weight_grad takes for a call (0: it would refuse it), so that tests know which kernel they run.
 extern "C" int apm_test_weight_grad_tile(const apm_weight_grad* w);
 // Rows of the tile of y that a product per group takes (-128: of 128 x 256, -64: with the sum split over the wavefronts; 0: it would be refused), for the tests that go through all of them.

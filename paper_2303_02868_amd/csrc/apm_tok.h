@@ -24,6 +24,8 @@ inline int check_room(const void* workspace, size_t bytes, size_t need) {
     if (need > 0 && (!workspace || (uintptr_t)workspace % 16 != 0)) return fail(APM_EINVAL, "the workspace is missing or not aligned to 16 bytes");
     return APM_OK;
 }
+// Workgroups of one launch, where a call may take several.
+int64_t workgroups_of_launch(int threads);
 inline bool aligned_to(const void* p, uintptr_t n) { return (uintptr_t)p % n == 0; }
 
 }  // namespace apm

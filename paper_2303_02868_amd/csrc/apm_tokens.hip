@@ -434,8 +434,19 @@ int sort_tokens(const apm_token_order* op, void* workspace, size_t workspace_byt
     return APM_OK;
 }
 
+thread_local int64_t t_launch_workgroups = 0;
+
 }  // namespace
+
+int64_t workgroups_of_launch(int threads) { return t_launch_workgroups > 0 ? t_launch_workgroups : max_workgroups(threads) / 2; }
+
 }  // namespace apm
+
+extern "C" int apm_test_set_launch_workgroups(int64_t workgroups) {
+    if (workgroups < 0) return apm::fail(APM_EINVAL, "bad argument");
+    apm::t_launch_workgroups = workgroups;
+    return APM_OK;
+}
 
 extern "C" size_t apm_sort_tokens_workspace_bytes(const apm_token_order* o) {
     return !o || apm::check_order(*o) != APM_OK ? 0 : apm::room_of(o->n, o->rows);
