@@ -20,7 +20,7 @@ struct LookupArgs {
     const void* ids;
     apm_matrix table, y;
     apm_vector weights;
-    int64_t tokens, first;  // of all launches; the first one of this
+    int64_t first, end;  // tokens of this launch
     uint32_t slices, rows;
     int32_t cols, per_token, id_type, accumulate;
     float scale;
@@ -37,7 +37,7 @@ __global__ __launch_bounds__(kThreads) void apm_lookup_kernel(LookupArgs a) {
     const int lane = (int)threadIdx.x % kWave;
     const uint32_t item = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), nth = item / a.slices;
     const int64_t t0 = a.first + (int64_t)nth * kTokens;
-    if (t0 >= a.tokens) return;
+    if (t0 >= a.end) return;
     LaneCols l;
     l.set((int)(item - nth * a.slices) * kSlice + lane * kVec, a.cols);
     float sum[kTokens][kVec] = {};
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads) void apm_lookup_kernel(LookupArgs a) {
         const int64_t t = t0 + lane / kTurn, j = j0 + lane % kTurn;
         uint32_t my_row = a.rows;
         float my_weight = 0.0f;
-        if (t < a.tokens && j < a.per_token) {
+        if (t < a.end && j < a.per_token) {
             const int64_t p = t * a.per_token + j;
             my_row = row_of(a.ids, a.id_type, p, a.rows);
             if (my_row < a.rows) my_weight = weight_of(a.weights, p);
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void apm_lookup_kernel(LookupArgs a) {
     }
 #pragma unroll
     for (int u = 0; u < kTokens; ++u) {
-        const bool there = t0 + u < a.tokens;
+        const bool there = t0 + u < a.end;
         float v[kVec];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] = sum[u][i] * a.scale;
@@ -103,11 +103,12 @@ int forward(const apm_lookup* lp, void* stream) {
     if (rc != APM_OK || l.tokens == 0) return rc;
     LookupArgs a{};
     a.ids = l.ids.data, a.id_type = l.ids.type, a.table = l.table, a.y = l.y, a.weights = l.weights;
-    a.tokens = l.tokens, a.slices = (uint32_t)div_up(l.cols, kSlice), a.cols = (int32_t)l.cols;
+    a.slices = (uint32_t)div_up(l.cols, kSlice), a.cols = (int32_t)l.cols;
     a.rows = (uint32_t)l.rows, a.per_token = (int32_t)l.per_token, a.accumulate = l.accumulate, a.scale = (float)l.scale;
-    const int64_t most = max_workgroups(kThreads) / 2 * kWaves / a.slices * kTokens;  // tokens of a launch
-    for (a.first = 0; a.first < l.tokens; a.first += most) {
-        const dim3 grid((unsigned)div_up(div_up(std::min(most, l.tokens - a.first), kTokens) * a.slices, kWaves)), block(kThreads);
+    const int64_t most = std::max<int64_t>(1, workgroups_of_launch(kThreads) * kWaves / a.slices) * kTokens;  // tokens of a launch
+    for (a.first = 0; a.first < l.tokens; a.first = a.end) {
+        a.end = std::min(l.tokens, a.first + most);  // the last workgroup can have wavefronts to spare, whose tokens are the next launch's: with accumulate they would be added twice
+        const dim3 grid((unsigned)div_up(div_up(a.end - a.first, kTokens) * a.slices, kWaves)), block(kThreads);
         const hipStream_t s = (hipStream_t)stream;
         auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
         if (l.table.dtype == APM_F32) l.y.dtype == APM_F32 ? start(apm_lookup_kernel<float, float>) : start(apm_lookup_kernel<float, bf16>);

@@ -42,3 +42,16 @@ def test_dropout_in_place(workgroups, cols, dtype):
                 apm.apm_dropout_apply(apm.make_dropout(x, in_r, p=0.25, seed=3, residual=in_r))
                 assert torch.equal(in_r, want)
         assert torch.equal(in_x, want)
+
+
+@pytest.mark.parametrize("y", [BF16, F32])
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("workgroups", WORKGROUPS)
+def test_lookup_that_adds(workgroups, cols, y):
+    ids = torch.randint(-1, 40, (101, 2), device=DEV, generator=rng(2))
+    table, before = randn(40, cols), randn(101, cols, dtype=y, seed=1)
+    want, got = before.clone(), before.clone()
+    apm.apm_lookup_forward(apm.make_lookup(ids, table, want, accumulate=True))
+    with launches_of(workgroups):
+        apm.apm_lookup_forward(apm.make_lookup(ids, table, got, accumulate=True))
+    assert torch.equal(got, want)
