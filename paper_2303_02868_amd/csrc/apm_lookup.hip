@@ -383,7 +383,7 @@ int backward(const apm_lookup* lp, const apm_lookup_grads* gp, void* workspace, 
     }
     if (rc != APM_OK) return rc;
     const hipStream_t s = (hipStream_t)stream;
-    const int64_t most_items = max_workgroups(kThreads) * kWaves / 2;
+    const int64_t most_items = workgroups_of_launch(kThreads) * kWaves;  // whole workgroups: what one has to spare would be the next launch's, whose rows are added once
     const bool wide_dy = n > 0 && g.dy.dtype == APM_F32, wide_dtable = g.dtable.dtype == APM_F32, wide_table = l.table.dtype == APM_F32;
     WeightGradArgs of_weights{};
     of_weights.ids = l.ids.data, of_weights.id_type = l.ids.type, of_weights.dy = g.dy, of_weights.table = l.table, of_weights.dweights = g.dweights;

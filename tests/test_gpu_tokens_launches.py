@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2303_02868_amd as apm
-from test_gpu_tokens import BF16, DEV, F32, rng
+from test_gpu_tokens import BF16, DEV, F32, rng, room, sort
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,27 @@ def test_lookup_that_adds(workgroups, cols, y):
     with launches_of(workgroups):
         apm.apm_lookup_forward(apm.make_lookup(ids, table, got, accumulate=True))
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("workgroups", WORKGROUPS)
+def test_gradients(workgroups, cols, dtype, accumulate):
+    """Rows inside of a chunk of positions, rows that go over several, rows without any."""
+    ids = torch.randint(-1, 300, (211, 2), device=DEV, generator=rng(2))
+    ids[::5] = 7
+    table, weights, dy, before = randn(300, cols), randn(211, 2, dtype=F32, seed=1), randn(211, cols, seed=3), randn(300, cols, dtype=dtype, seed=4)
+    order = sort(ids, 300)[0]
+    lookup = apm.make_lookup(ids, table, weights=weights)
+    workspace = room(apm.apm_lookup_workspace_bytes(lookup))
+
+    def gradients():
+        dtable, dweights = before.clone(), torch.full((211, 2), 7.0, dtype=dtype, device=DEV)
+        apm.apm_lookup_backward(lookup, apm.make_lookup_grads(lookup, dy, order=order, dtable=dtable, dweights=dweights, accumulate=accumulate), workspace)
+        return dtable, dweights
+
+    want = gradients()
+    with launches_of(workgroups):
+        got = gradients()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
