@@ -144,7 +144,7 @@ __device__ __forceinline__ u32x4 buffer_of(const char* p, uint32_t bytes) {
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32));
     return u32x4{lo, hi & 0xffffu, (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00027000u};
 }
-constexpr uint32_t kNowhere = 0x80000000u;  // behind the end of any buffer here, and so is what is less than 2^30 further on
+constexpr uint32_t kNowhere = 0x80000000u;  // behind the end of any buffer here, which product_shape sees to, and so is what is less than 2^30 further on
 
 // The order that the scheduler is to keep in a step: in front of each product its part of the LDS reads for the next step, behind it its part of the loads.
 template <int PRODUCTS, int READS, int LOADS, int I = 0> __device__ __forceinline__ void in_turn() {
@@ -775,8 +775,11 @@ double cost_of(const apm_grouped_product_desc& p, const TileCost& c, bool direct
 ProductShape product_shape(const apm_grouped_product_desc& p) {
     ProductShape s{};
     const int64_t reach = (int64_t)1 << 30, w_rows = p.transposed ? p.in + 4 * Large::K : Large::kN;
+    // Rows that overlap can be wider than they are apart: what a tile's loads go by ends at 2^31 bytes all the same.
+    auto ends = [&](int64_t rows, const apm_matrix& m, int64_t cols) { return (rows - 1) * m.stride + cols <= reach; };
     s.direct = aligned_to(p.x.data, 16) && aligned_to(p.w.data, 16) && p.x.stride % kVec == 0 && p.w.stride % kVec == 0 && (p.n_groups < 2 || p.w_group_stride % kVec == 0) &&
-               p.in % kVec == 0 && (!p.transposed || p.out % kVec == 0) && p.x.stride < reach / Large::kM && p.w.stride < reach / w_rows && p.in < reach / 4 && p.out < reach / 4;
+               p.in % kVec == 0 && (!p.transposed || p.out % kVec == 0) && p.x.stride < reach / Large::kM && p.w.stride < reach / w_rows && p.in < reach / 4 && p.out < reach / 4 &&
+               ends(Large::kM, p.x, p.in) && ends(p.transposed ? p.in : Large::kN, p.w, p.transposed ? p.out : p.in);
     int which = 0;
     for (int i = 1; i < kTiles; ++i)
         if (cost_of(p, kCost[i], s.direct) < cost_of(p, kCost[which], s.direct)) which = i;
