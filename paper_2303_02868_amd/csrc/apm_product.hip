@@ -795,16 +795,29 @@ ProductShape product_shape(const apm_grouped_product_desc& p) {
     return s;
 }
 
+// ANY: the tile through registers, of the same rows and columns, which the grid is counted for; void: there is no such form, and cost_of never takes it.
 template <class T, class ANY = T> hipError_t launch_product(const ProductArgs& a, bool transposed, bool direct, unsigned workgroups, hipStream_t s) {
     auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(workgroups), dim3(T::kThreads), 0, s, a); };
-    if (transposed) direct ? start(apm_product_kernel<T, true, true>) : start(apm_product_kernel<ANY, true, false>);
-    else direct ? start(apm_product_kernel<T, false, true>) : start(apm_product_kernel<ANY, false, false>);
+    if (direct) {
+        transposed ? start(apm_product_kernel<T, true, true>) : start(apm_product_kernel<T, false, true>);
+    } else if constexpr (std::is_void<ANY>::value) {
+        return hipErrorInvalidValue;
+    } else {
+        static_assert(ANY::kM == T::kM && ANY::kN == T::kN && ANY::kThreads == T::kThreads, "the same tile of y");
+        transposed ? start(apm_product_kernel<ANY, true, false>) : start(apm_product_kernel<ANY, false, false>);
+    }
     return hipGetLastError();
 }
 template <class T, class ANY = T> hipError_t launch_few(const ProductArgs& a, bool transposed, bool direct, unsigned workgroups, hipStream_t s) {
     auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(workgroups), dim3(T::kThreads), 0, s, a); };
-    if (transposed) direct ? start(apm_product_few_kernel<T, true, true>) : start(apm_product_few_kernel<ANY, true, false>);
-    else direct ? start(apm_product_few_kernel<T, false, true>) : start(apm_product_few_kernel<ANY, false, false>);
+    if (direct) {
+        transposed ? start(apm_product_few_kernel<T, true, true>) : start(apm_product_few_kernel<T, false, true>);
+    } else if constexpr (std::is_void<ANY>::value) {
+        return hipErrorInvalidValue;
+    } else {
+        static_assert(ANY::kM == T::kM && ANY::kN == T::kN && ANY::kThreads == T::kThreads, "the same tile of y");
+        transposed ? start(apm_product_few_kernel<ANY, true, false>) : start(apm_product_few_kernel<ANY, false, false>);
+    }
     return hipGetLastError();
 }
 
@@ -826,11 +839,11 @@ int grouped_product(const apm_grouped_product_desc* pp, void* workspace, size_t 
     const unsigned n = (unsigned)(s.tiles_m * s.tiles_n);
     const hipStream_t st = (hipStream_t)stream;
     APM_HIP(s.which == kLarge   ? (launch_product<Large, LargeAny>)(a, p.transposed, s.direct, n, st)
-            : s.which == kLower ? (launch_product<Lower, LargeAny>)(a, p.transposed, s.direct, n, st)
-            : s.which == kLow   ? (launch_product<Low, LargeAny>)(a, p.transposed, s.direct, n, st)
+            : s.which == kLower ? (launch_product<Lower, void>)(a, p.transposed, s.direct, n, st)
+            : s.which == kLow   ? (launch_product<Low, void>)(a, p.transposed, s.direct, n, st)
             : s.which == kSmall ? launch_product<Small>(a, p.transposed, s.direct, n, st)
             : s.which == kTiny  ? (launch_product<Tiny, TinyAny>)(a, p.transposed, s.direct, n, st)
-            : s.which == kSquares ? (launch_few<Squares, Strips>)(a, p.transposed, s.direct, n, st)
+            : s.which == kSquares ? (launch_few<Squares, void>)(a, p.transposed, s.direct, n, st)
                                   : launch_few<Strips>(a, p.transposed, s.direct, n, st));
     return APM_OK;
 }

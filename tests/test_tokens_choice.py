@@ -32,3 +32,20 @@ def test_overlapping_rows_of_transposed_weights_behind_the_reach_of_a_load_go_th
     most = (1 << 30) - (k - 1) * apart
     assert tile(1, most - most % 8, k, w=apart, transposed=True) == 64
     assert tile(1, most - most % 8 + 8, k, w=apart, transposed=True) == 32
+
+
+def test_tiles_without_a_form_through_registers_are_not_taken_for_one():
+    """Sizes at which whole vectors take those tiles (192, -128, -64), and around them; x is not aligned to a vector."""
+    def through_registers(tokens, out, k, transposed):
+        p = product(tokens, out, k, transposed=transposed)
+        p.x.data += 2
+        return apm.lib().apm_test_grouped_product_tile(C.byref(p))
+
+    seen = set()
+    for transposed in (False, True):
+        for tokens in (1, 40, 255, 1300, 5100, 6100, 7900, 1 << 17):
+            for out in (8, 136, 520, 1032, 2056, 8192):
+                for k in (8, 328, 1096, 4168, 65536):
+                    seen.add(tile(tokens, out, k, transposed=transposed))
+                    assert through_registers(tokens, out, k, transposed) in (256, 128, 64, 32)
+    assert {192, -128, -64} <= seen
