@@ -795,6 +795,8 @@ ProductShape product_shape(const apm_grouped_product_desc& p) {
     return s;
 }
 
+bool in_a_grid(const ProductShape& s) { return s.tiles_m <= max_workgroups(Large::kThreads) / s.tiles_n; }
+
 // ANY: the tile through registers, of the same rows and columns, which the grid is counted for; void: there is no such form, and cost_of never takes it.
 template <class T, class ANY = T> hipError_t launch_product(const ProductArgs& a, bool transposed, bool direct, unsigned workgroups, hipStream_t s) {
     auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(workgroups), dim3(T::kThreads), 0, s, a); };
@@ -835,7 +837,7 @@ int grouped_product(const apm_grouped_product_desc* pp, void* workspace, size_t 
     a.whole_y = p.y.dtype == APM_BF16 && aligned_to(p.y.data, 16) && p.y.stride % kVec == 0;
     const ProductShape s = product_shape(p);
     a.tiles_n = (int32_t)s.tiles_n;
-    if (s.tiles_m > max_workgroups(Large::kThreads) / s.tiles_n) return fail(APM_EINVAL, "y is too large for one product");
+    if (!in_a_grid(s)) return fail(APM_EINVAL, "y is too large for one product");
     const unsigned n = (unsigned)(s.tiles_m * s.tiles_n);
     const hipStream_t st = (hipStream_t)stream;
     APM_HIP(s.which == kLarge   ? (launch_product<Large, LargeAny>)(a, p.transposed, s.direct, n, st)
@@ -859,6 +861,7 @@ extern "C" int apm_grouped_product(const apm_grouped_product_desc* p, void* work
 
 extern "C" int apm_test_grouped_product_tile(const apm_grouped_product_desc* p) {
     if (!p || apm::check_product(*p) != APM_OK) return 0;
-    const int which = apm::product_shape(*p).which, rows = apm::kCost[which].rows;
-    return which == apm::kLow || which == apm::kSquares ? -rows : rows;
+    const apm::ProductShape s = apm::product_shape(*p);
+    const int rows = apm::kCost[s.which].rows;
+    return !apm::in_a_grid(s) ? 0 : s.which == apm::kLow || s.which == apm::kSquares ? -rows : rows;
 }

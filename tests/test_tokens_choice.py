@@ -49,3 +49,12 @@ def test_tiles_without_a_form_through_registers_are_not_taken_for_one():
                     seen.add(tile(tokens, out, k, transposed=transposed))
                     assert through_registers(tokens, out, k, transposed) in (256, 128, 64, 32)
     assert {192, -128, -64} <= seen
+
+
+def test_products_of_more_tiles_than_a_grid_holds_are_refused():
+    """Rows that strides allow (2^56 elements), and too many of them for one launch; x is one row for all tokens."""
+    for tokens, out in ((1 << 30, 1 << 20), (1 << 36, 1 << 10), (1 << 28, 1 << 28)):
+        p = product(tokens, out, 64, x=0)
+        assert tile(tokens, out, 64, x=0) == 0
+        assert apm.lib().apm_grouped_product(C.byref(p), None, 0, None) == apm.APM_EINVAL
+        assert "y is too large for one product" in apm.apm_last_error()
