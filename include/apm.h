@@ -910,7 +910,8 @@ int apm_lookup_backward(const apm_lookup* l, const apm_lookup_grads* g, void* wo
  * x, w: bf16.  w's groups are w_group_stride elements apart, bias's [n_groups][out] contiguous (optional, bf16 or fp32).  y: bf16 or fp32; accumulate:
  * added to what y holds.  Products are exact where they and their factors are zero or of size 2^-126 and up (smaller ones may be taken as zero), sums fp32; the
  * bias is added to the sum in fp32, then what y held; the result is rounded to y's type.  A second call gives the same bits.
- * out and in: at most 2^28; n_groups: at most APM_MAX_GROUPS.
+ * out and in: at most 2^28; n_groups: at most APM_MAX_GROUPS.  Of 2^31 rows of y and more for each 256 columns, groups' rows rounded up to 256, the product is
+ * refused (APM_EINVAL).
  * workspace: apm_grouped_product_workspace_bytes(p) bytes (may be 0, as it is where the call would refuse p), 16-byte aligned.
  */
 #define APM_MAX_GROUPS 65536

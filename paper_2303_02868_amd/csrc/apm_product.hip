@@ -730,34 +730,27 @@ int check_product(const apm_grouped_product_desc& p) {
 
 enum { kLarge, kLower, kLow, kSmall, kTiny, kSquares, kFew, kTiles };
 struct ProductShape {
-    int which;
+    int which;  // kTiles: no tile of which a grid holds enough
     bool direct;
     int64_t tiles_m, tiles_n;
 };
-template <class T> void shape_as(const apm_grouped_product_desc& p, int which, ProductShape* s) {
-    s->which = which;
-    // tokens fill whole tiles but for the last of each group
-    const int64_t groups = std::max<int64_t>(1, p.n_groups);
-    s->tiles_m = std::min(p.tokens, p.tokens / T::kM + std::min(groups, p.tokens));
-    s->tiles_n = div_up(p.out, T::kN);
-}
 // Which tile: estimated in us, from calls that were timed; over 150 drawn sizes and groups the choice is the fastest of the seven or within 15 % or 1.5 us of it, but for
 // groups of which few have tokens (137 tokens in 30 of 64, 6144 to 261: 40 and 21 us at worst) and a short k of odd length (9557 tokens, 79 to 4983: 47 and 35). A
 // workgroup that has a CU for itself takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for that of each workgroup it has, and `round` more for each.
 struct TileCost {
-    int rows, cols;
+    int rows, cols, threads;
     int per_cu;  // workgroups that start together
     double start, round, alone[2], busy[2];  // through registers, direct
 };
 constexpr double kNever = 1e30;
 constexpr TileCost kCost[kTiles] = {
-    {Large::kM, Large::kN, 1, 8.0, 6.0, {1.9, 1.08}, {2.5, 1.63}},
-    {Lower::kM, Lower::kN, 1, 7.0, 0.0, {kNever, 0.85}, {kNever, 1.24}},
-    {Low::kM, Low::kN, 1, 7.0, 3.0, {kNever, 0.6}, {kNever, 0.88}},
-    {Small::kM, Small::kN, 2, 4.6, 1.0, {0.95, 0.39}, {0.8, 0.49}},
-    {Tiny::kM, Tiny::kN, 0, 2.6, 0.35, {0.5, 0.25}, {0.33, 0.185}},
-    {Squares::kM, Squares::kN, 1, 5.2, 3.0, {kNever, 0.165}, {kNever, 0.2}},
-    {Strips::kM, Strips::kN, 0, 2.7, 2.2, {0.31, 0.085}, {0.13, 0.1}},
+    {Large::kM, Large::kN, Large::kThreads, 1, 8.0, 6.0, {1.9, 1.08}, {2.5, 1.63}},
+    {Lower::kM, Lower::kN, Lower::kThreads, 1, 7.0, 0.0, {kNever, 0.85}, {kNever, 1.24}},
+    {Low::kM, Low::kN, Low::kThreads, 1, 7.0, 3.0, {kNever, 0.6}, {kNever, 0.88}},
+    {Small::kM, Small::kN, Small::kThreads, 2, 4.6, 1.0, {0.95, 0.39}, {0.8, 0.49}},
+    {Tiny::kM, Tiny::kN, Tiny::kThreads, 0, 2.6, 0.35, {0.5, 0.25}, {0.33, 0.185}},
+    {Squares::kM, Squares::kN, Squares::kThreads, 1, 5.2, 3.0, {kNever, 0.165}, {kNever, 0.2}},
+    {Strips::kM, Strips::kN, Strips::kThreads, 0, 2.7, 2.2, {0.31, 0.085}, {0.13, 0.1}},
 };
 constexpr double kCus = 256.0;
 double cost_of(const apm_grouped_product_desc& p, const TileCost& c, bool direct) {
@@ -780,22 +773,17 @@ ProductShape product_shape(const apm_grouped_product_desc& p) {
     s.direct = aligned_to(p.x.data, 16) && aligned_to(p.w.data, 16) && p.x.stride % kVec == 0 && p.w.stride % kVec == 0 && (p.n_groups < 2 || p.w_group_stride % kVec == 0) &&
                p.in % kVec == 0 && (!p.transposed || p.out % kVec == 0) && p.x.stride < reach / Large::kM && p.w.stride < reach / w_rows && p.in < reach / 4 && p.out < reach / 4 &&
                ends(Large::kM, p.x, p.in) && ends(p.transposed ? p.in : Large::kN, p.w, p.transposed ? p.out : p.in);
-    int which = 0;
-    for (int i = 1; i < kTiles; ++i)
-        if (cost_of(p, kCost[i], s.direct) < cost_of(p, kCost[which], s.direct)) which = i;
-    switch (which) {
-        case kLarge: shape_as<Large>(p, which, &s); break;
-        case kLower: shape_as<Lower>(p, which, &s); break;
-        case kLow: shape_as<Low>(p, which, &s); break;
-        case kSmall: shape_as<Small>(p, which, &s); break;
-        case kTiny: shape_as<Tiny>(p, which, &s); break;
-        case kSquares: shape_as<Squares>(p, which, &s); break;
-        default: shape_as<Strips>(p, which, &s);
+    s.which = kTiles;
+    double least = kNever;
+    for (int i = 0; i < kTiles; ++i) {
+        // tokens fill whole tiles but for the last of each group
+        const int64_t groups = std::max<int64_t>(1, p.n_groups), m = std::min(p.tokens, p.tokens / kCost[i].rows + std::min(groups, p.tokens)), n = div_up(p.out, kCost[i].cols);
+        const double cost = cost_of(p, kCost[i], s.direct);
+        if (cost >= least || m > max_workgroups(kCost[i].threads) / n) continue;
+        s.which = i, s.tiles_m = m, s.tiles_n = n, least = cost;
     }
     return s;
 }
-
-bool in_a_grid(const ProductShape& s) { return s.tiles_m <= max_workgroups(Large::kThreads) / s.tiles_n; }
 
 // ANY: the tile through registers, of the same rows and columns, which the grid is counted for; void: there is no such form, and cost_of never takes it.
 template <class T, class ANY = T> hipError_t launch_product(const ProductArgs& a, bool transposed, bool direct, unsigned workgroups, hipStream_t s) {
@@ -837,7 +825,7 @@ int grouped_product(const apm_grouped_product_desc* pp, void* workspace, size_t 
     a.whole_y = p.y.dtype == APM_BF16 && aligned_to(p.y.data, 16) && p.y.stride % kVec == 0;
     const ProductShape s = product_shape(p);
     a.tiles_n = (int32_t)s.tiles_n;
-    if (!in_a_grid(s)) return fail(APM_EINVAL, "y is too large for one product");
+    if (s.which == kTiles) return fail(APM_EINVAL, "y is too large for one product");
     const unsigned n = (unsigned)(s.tiles_m * s.tiles_n);
     const hipStream_t st = (hipStream_t)stream;
     APM_HIP(s.which == kLarge   ? (launch_product<Large, LargeAny>)(a, p.transposed, s.direct, n, st)
@@ -862,6 +850,7 @@ extern "C" int apm_grouped_product(const apm_grouped_product_desc* p, void* work
 extern "C" int apm_test_grouped_product_tile(const apm_grouped_product_desc* p) {
     if (!p || apm::check_product(*p) != APM_OK) return 0;
     const apm::ProductShape s = apm::product_shape(*p);
+    if (s.which == apm::kTiles) return 0;
     const int rows = apm::kCost[s.which].rows;
-    return !apm::in_a_grid(s) ? 0 : s.which == apm::kLow || s.which == apm::kSquares ? -rows : rows;
+    return s.which == apm::kLow || s.which == apm::kSquares ? -rows : rows;
 }

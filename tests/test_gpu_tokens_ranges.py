@@ -1,9 +1,9 @@
-"""Products of weights whose rows overlap: read-only matrices may, and then they can be wider than their rows are apart."""
+"""Products at the ends of their ranges: weights whose rows overlap, as read-only matrices may, and are wider than they are apart; very many rows."""
 import pytest
 import torch
 
 import paper_2303_02868_amd as apm
-from test_gpu_tokens import BF16, DEV
+from test_gpu_tokens import BF16, DEV, rng
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +25,17 @@ def test_what_is_behind_the_end_of_the_sum_stays_out_of_it():
     assert int(want.sum()) > 8 and not bool(want[:1 << 20].any())
     there, elsewhere = int(((y[0] == float("inf")) & want).sum()), int(((y[0] == 0) & ~want).sum())
     assert there == int(want.sum()) and elsewhere == out - there
+
+
+@pytest.mark.parametrize("tokens", [(1 << 29) + 3, (1 << 30) + 70])
+def test_more_rows_than_a_grid_of_the_smallest_tiles_holds(tokens):
+    """w changes the order of the columns, so that y is x to the bit."""
+    x = torch.empty(tokens, 8, dtype=BF16, device=DEV)
+    x.view(torch.int16).random_(0, 0x4000, generator=rng(1))
+    x.masked_fill_(x.abs() < 2.0 ** -100, 1.0)                 # the smallest may be taken as zero
+    w = torch.eye(8, dtype=BF16, device=DEV).flip(0).contiguous()
+    y = torch.empty_like(x)
+    apm.apm_grouped_product(apm.make_grouped_product(x, w, y))
+    step = 1 << 27
+    for at in range(0, tokens, step):
+        assert bool((y[at:at + step] == x[at:at + step].flip(1)).all()), at

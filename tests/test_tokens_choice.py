@@ -58,3 +58,9 @@ def test_products_of_more_tiles_than_a_grid_holds_are_refused():
         assert tile(tokens, out, 64, x=0) == 0
         assert apm.lib().apm_grouped_product(C.byref(p), None, 0, None) == apm.APM_EINVAL
         assert "y is too large for one product" in apm.apm_last_error()
+
+
+@pytest.mark.parametrize("tokens,out,k", [(1 << 29, 8, 8), (1 << 30, 32, 32), ((1 << 31) - 512, 136, 64), ((1 << 31) - 512, 8, 1), ((1 << 24) - 512, 1 << 15, 8)])
+def test_products_that_a_grid_holds_with_another_tile_are_not_refused(tokens, out, k):
+    for transposed in (False, True):
+        assert tile(tokens, out, k, x=0, transposed=transposed) > 0
