@@ -1050,8 +1050,8 @@ def make_dropout(x, y, *, p: float, seed: int, layer: int = 0, first_row: int = 
     rows, cols = x.shape
     at = 0
     if seed_at is not None:
-        if seed_at.numel() != 1 or seed_at.element_size() != 8:
-            raise ValueError(f"seed_at: {seed_at.dtype} of {tuple(seed_at.shape)}, one word of 64 bits is needed")
+        if seed_at.numel() != 1 or (_index_type(seed_at) != APM_I64 and str(seed_at.dtype) != "torch.uint64"):
+            raise ValueError(f"seed_at: {seed_at.dtype} of {tuple(seed_at.shape)}, one int64 or uint64 is needed")
         at = _address("seed_at", seed_at, here)
     d = apm_dropout.from_buffer_copy(_pack_dropout(rows, cols, p, seed % (1 << 64), at, first_row, layer, 0, *_matrix("x", x, rows, cols, here),
                                                    *_matrix("residual", residual, rows, cols, here), *_matrix("y", y, rows, cols, here)))
