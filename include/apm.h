@@ -930,7 +930,7 @@ int apm_grouped_product(const apm_grouped_product_desc* p, void* workspace, size
 
 /*
  * Dropout whose mask is made of the element's place and never stored:
- *     y[r, c] = residual[r, c] + (u[r, c] < T ? 0 : x[r, c] 65536 / (65536 - T)),      T = 65536 p rounded to nearest
+ *     y[r, c] = residual[r, c] + (u[r, c] < T ? 0 : x[r, c] 65536 / (65536 - T)),      T = 65536 p rounded to nearest, halves up
  * u: 16 bits of Philox4x32 of ten rounds (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", SC 2011) with counter words c / 8,
  * the low and the high half of first_row + r, layer, and for key the two halves of seed + *seed_at modulo 2^64, low first: of the four words that
  * come out, the low halves are for the even columns of the eight, the high ones for the odd, so columns 8 i and 8 i + 1 share word 0.

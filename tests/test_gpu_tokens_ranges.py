@@ -1,7 +1,9 @@
-"""Products at the ends of their ranges: weights whose rows overlap, as read-only matrices may, and are wider than they are apart; very many rows."""
+"""Calls on tokens at the ends of their ranges: weights whose rows overlap, as read-only matrices may, and are wider than they are apart; very many rows; probabilities between two."""
+import numpy as np
 import pytest
 import torch
 
+import oracle.tokens as T
 import paper_2303_02868_amd as apm
 from test_gpu_tokens import BF16, DEV, rng
 
@@ -39,3 +41,17 @@ def test_more_rows_than_a_grid_of_the_smallest_tiles_holds(tokens):
     step = 1 << 27
     for at in range(0, tokens, step):
         assert bool((y[at:at + step] == x[at:at + step].flip(1)).all()), at
+
+
+@pytest.mark.parametrize("bound", [1, 3, 4, 16385, 32769, 65535, 65536])
+def test_probabilities_between_two_bounds_take_the_upper_one(bound):
+    """What is kept is multiplied by 65536 / (65536 - T), of which T can be told, in fp32 rounded twice at most."""
+    x = torch.ones(8, 4096, device=DEV)
+    y = torch.empty_like(x)
+    p = (bound - 0.5) / 65536
+    apm.apm_dropout_apply(apm.make_dropout(x, y, p=p, seed=4))
+    kept = T.dropout_bits(8, 4096, 4) >= bound
+    want = T.dropout(np.ones((8, 4096)), p, 4)
+    got = y.double().cpu().numpy()
+    assert np.array_equal(got != 0, kept) and np.array_equal(want != 0, kept)
+    assert np.all(np.abs(got - want) <= 2.0 ** -23 * want)
