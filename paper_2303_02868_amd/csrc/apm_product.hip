@@ -38,20 +38,20 @@ struct Tile {
     static_assert(kA * 1024 * kWaves == kBytesA && kB * 1024 * kWaves == kBytesB, "whole vectors for every lane");
 };
 // 64 of k in a stage are whole cache lines of rows of x and w (16384 x 4096 x 4096 with 32 of k: 478 us, so 447).
-// 256 x 256: the least traffic between L2 and LDS, which bounds the others: loads alone take 341 of its 465 us at 16384 x 4096 x 4096, products and LDS reads alone 387;
-// 1.2 PFLOP/s, at a clock of 1.75 GHz that the matrix cores leave (a library product of that size: 423 to 432 us, w as rows of k 482 to 496, here 452 to 468).  Of the
-// CU's cycles the matrix cores are busy for 58 %, LDS for 28 %.  A half stage more in LDS: input gradients of 8 of 64 groups, 8192 x 1024 x 4096, 114 us without it, so 106.
+// 256 x 256: the least traffic between L2 and LDS, which bounds the others: loads alone take 341 us of 16384 x 4096 x 4096, products and LDS reads alone 387, together 442 to 489 by
+// the card, 1.12 to 1.24 PFLOP/s, at a clock of 1.6 to 1.75 GHz that the matrix cores leave (a library product of that size 415 to 432 on the better card, w as rows of k 479 to 496).
+// Of the cycles that a CU is busy the matrix cores are for 73 %, LDS for 29 %.  A half stage more in LDS: input gradients of 8 of 64 groups, 8192 x 1024 x 4096, 114 us without it, so 106.
 // One workgroup a CU that goes on from tile to tile, with the next one's loads under the stores, was no faster (8 groups, 16384 x 8192 x 2048: 575 and 578 us).
 typedef Tile<2, 4, 4, 2, 64, 5> Large;
 // 192 x 256, where 256 x 256 would leave CUs without a tile and this one has one for each at most, as the time is that of a tile then: 6000 x 2048 x 2048
-// 53 us by 256 x 256, so 46; 1500 x 8192 x 2048 52 and 45.  Not through registers.
+// 53 us by 256 x 256, so 46 to 49; 1500 x 8192 x 2048 52 and 45.  Not through registers.
 typedef Tile<2, 4, 3, 2, 64, 4> Lower;
-// 128 x 256, where more tiles than CUs or groups of few tokens leave 256 rows half empty: 4096 tokens of 64 experts, 1024 to 4096, 112 us (120 by 128 x 128, 155 by 256 x 256),
+// 128 x 256, where more tiles than CUs or groups of few tokens leave 256 rows half empty: 4096 tokens of 64 experts, 1024 to 4096, 107 to 114 us (108 to 120 by 128 x 128, 157 by 256 x 256),
 // 4096 tokens in 8 groups, 4096 to 1024, 61 (71, 102).
 typedef Tile<2, 4, 2, 2, 64, 6> Low;
 // 128 x 128, two of which share a CU: where 256 x 256 would leave CUs without one (2048 x 2048 x 2048: 43 us, so 25).
 typedef Tile<2, 2, 2, 2, 64, 4> Small;
-// 64 x 64: short ones (512 x 768 x 768: 8.9 us by 128 x 128, so 5.1), and groups of few tokens (512 tokens in 64 groups, 4096 x 1024: 107 and 97).
+// 64 x 64: short ones (512 x 768 x 768: 8.9 us by 128 x 128, so 5.1), and groups of few tokens (512 tokens of 64 experts, 1024 to 4096: 94 and 85 to 104 by the card).
 typedef Tile<2, 2, 1, 1, 64, 6> Tiny;
 // Large where rows go through registers: stages of half the length, so that what is on its way fits beside the sums.
 typedef Tile<2, 4, 4, 2, 32, 4> LargeAny;
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
         }
     }
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
-    // Where a group's weights are read once, groups begin at different k: they would all read the same columns of rows at a time, which lie in few of the memory's channels
+    // Where a group's weights are read once, groups begin at different k: they would all read the same columns of rows at a time, as a group's own tiles still do, which lie in few of the memory's channels
     // (8000 tokens of 64 experts, 4096 to 1024: 167 us, so 153).
     const int first = !TRANSPOSED && at.once && a.in % T::K == 0 ? (int)((uint32_t)group % (uint32_t)stages) : 0;
     auto stage_at = [&](int j, auto once) { return !once ? j : j + first < stages ? j + first : j + first - stages; };
@@ -517,7 +517,7 @@ __global__ __launch_bounds__(T::kThreads) void apm_product_kernel(ProductArgs a)
 
 // Few rows: HBM-bound by the weights, and too few tiles for the chip unless they are small.  Each of a workgroup's wavefronts takes every fourth stage of k of the
 // same 32 x 32 tile, by a ring in LDS of its own, so that nobody waits for anybody until the four sums come together at the end.  Two tokens of two of 64 groups,
-// 4096 x 1024: 5.5 us (7.7 by 64 x 64), one token, 768 x 768: 3.7 (4.9), 56 tokens of 8 groups, 1152 x 3776: 11 (18).
+// 4096 x 1024: 4.5 us a call among others, 6.2 by itself (8.6 among others by 64 x 64), one token, 768 x 768: 3.7 (4.9), 56 tokens of 8 groups, 1152 x 3776: 11 (18).
 template <int FM_, int FN_, int STAGES_>
 struct Few {
     static constexpr int FM = FM_, FN = FN_, kStages = STAGES_, K = 64, kWaves = 4, kThreads = kWaves * kWave;
@@ -734,8 +734,9 @@ struct ProductShape {
     bool direct;
     int64_t tiles_m, tiles_n;
 };
-// Which tile: estimated in us, from calls that were timed; over 150 drawn sizes and groups the choice is the fastest of the seven or within 15 % or 1.5 us of it, but for
-// groups of which few have tokens (137 tokens in 30 of 64, 6144 to 261: 40 and 21 us at worst) and a short k of odd length (9557 tokens, 79 to 4983: 47 and 35). A
+// Which tile: estimated in us, from calls that were timed; over 151 drawn sizes and groups the choice is the fastest of the seven or within 15 % or 1.5 us of it, but for
+// groups of which few have tokens (2970 tokens in 10 of 64, 768 to 7836: 93 and 73 us) and a short k of odd length (9557 tokens, 79 to 4983: 47 and 36).  There is no term for
+// memory, and groups of some 200 tokens with a long k, where it decides, can do better, too (1600 tokens of 8 groups, 4096 to 4096: 106 and 85).  A
 // workgroup that has a CU for itself takes `start` and `alone` for each 64 of k; a CU that is full, `busy` for that of each workgroup it has, and `round` more for each.
 struct TileCost {
     int rows, cols, threads;
